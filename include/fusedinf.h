@@ -461,6 +461,127 @@ fi_status fi_unload(fi_dag* dag);
  * NULL is allowed. */
 void fi_destroy(fi_dag* dag);
 
+/* ---- decoder operators ----
+ * What a decoder member runs on every step, as operators of their own on the caller's device tensors: the norms of its
+ * queries and keys with the position rotation (the step's keys and values go to their slots of a paged cache), attention
+ * over whole prompts, attention of drafted trees (or single tokens) over that cache, and products with 4-bit weights.
+ *
+ * Common to all of them
+ *  - Every call is asynchronous on hip_stream (a hipStream_t of the current device, NULL = default stream), allocates
+ *    nothing, synchronises nothing and may be recorded into a HIP graph.  The argument struct is read during the call only.
+ *  - dtype is FI_BF16 or FI_F32 and holds for every tensor of data; sums, softmax statistics and norms are fp32, and a
+ *    result is rounded once, when it is stored (attention on bf16 also rounds the weights it multiplies the values with).
+ *  - All tensor pointers are device pointers.  Strides are in elements of the tensor's type; the last dimension (head_dim,
+ *    inputs, outputs) is contiguous.  Inputs may have any strides >= 0; rows that start on 16-byte boundaries take the fast kernels.
+ *    Outputs must not overlap themselves or an input, except that q_out may be q, k_out k and v_out v with equal strides.
+ *  - What sits in device memory (offsets, lengths, page and slot numbers) cannot be checked by the call: the kernels clamp
+ *    it to the sizes given here, so that nothing outside the tensors is read or written, and the rows concerned are unspecified.
+ *  - FI_EINVAL for a null or misaligned pointer, a negative size or stride or sizes that contradict each other,
+ *    FI_EUNSUPPORTED for well-formed sizes that the kernels do not cover, FI_EHIP when a launch fails.  Nothing is
+ *    written then.  Sizes of zero (no tokens, no rows, no sequences) are no error: there is nothing to do.
+ */
+#define FI_MAX_AXES 4
+#define FI_MAX_HEAD_DIM 256
+
+/* y = rotate(x * w / sqrt(mean(x^2) + eps)) for every head of every token's q and k, in one launch; v is copied.
+ * The first rot_dim values of a head are rotated in pairs: pair i is (i, i + rot_dim / 2), or (2i, 2i + 1) when
+ * interleaved, and turns by the angle positions[token][axis of i] * inv_freq[i] (fp32): (a, b) -> (a cos - b sin,
+ * b cos + a sin).  The pairs are dealt to the axes in order, sections[a] of them to axis a (time, height, width of an image or
+ * video patch; one axis for text): the first n_axes sections add up to rot_dim / 2.  The values behind rot_dim are normed only. */
+typedef struct {
+  int32_t dtype;                 /* fi_dtype of q, k, v and of the outputs */
+  int32_t tokens, q_heads, kv_heads, head_dim; /* head_dim in [1, FI_MAX_HEAD_DIM] */
+  int32_t rot_dim;               /* even, in [0, head_dim] */
+  int32_t interleaved;           /* 0 / 1 */
+  int32_t n_axes;                /* in [1, FI_MAX_AXES] */
+  int32_t sections[FI_MAX_AXES];
+  float eps;                     /* >= 0 */
+  int32_t page_size;             /* with slots: tokens per page (>= 1) */
+  int64_t n_slots;               /* with slots: slots of the cache (pages x page_size); a token whose slot lies outside [0, n_slots)
+                                  * leaves the cache as it is (padding), its q is still written */
+  const void *q, *k, *v;         /* [tokens, heads, head_dim]; v may be NULL (then v_out is, too); k is not NULL where kv_heads > 0 */
+  const float *q_weight, *k_weight; /* [head_dim], fp32; NULL = ones */
+  const int32_t* positions;      /* [tokens, n_axes], contiguous */
+  const float* inv_freq;         /* [rot_dim / 2], fp32 */
+  const int64_t* slots;          /* [tokens]: where the token's k and v go, page * page_size + place in the page; no two tokens share a
+                                  * slot.  NULL = k_out and v_out are [tokens, kv_heads, head_dim] */
+  void *q_out, *k_out, *v_out;
+  int64_t q_strides[2], k_strides[2], v_strides[2], q_out_strides[2]; /* token, head */
+  int64_t k_out_strides[3], v_out_strides[3];                        /* page (unused without slots), token, head */
+} fi_qk_norm_rope_args;
+fi_status fi_qk_norm_rope(const fi_qk_norm_rope_args* args, void* hip_stream);
+
+/* out = softmax(scale * q k^T) v over packed sequences: sequence b has the queries [cu_q[b], cu_q[b + 1]) and the keys
+ * [cu_k[b], cu_k[b + 1]); query head h reads key head h / (q_heads / kv_heads).  causal: the sequence's last query sees every key and
+ * each one before it a key less (with more keys than queries the first keys are a prefix that all see; with fewer, the first
+ * queries see nothing).  A query that sees nothing yields zeros, and what a key or value holds that a query does not see, were it NaN,
+ * has no influence on it. */
+typedef struct {
+  int32_t dtype;
+  int32_t n_seqs, q_heads, kv_heads, head_dim; /* kv_heads divides q_heads; head_dim in [1, FI_MAX_HEAD_DIM] */
+  int32_t causal;                /* 0 / 1 */
+  float scale;                   /* finite, > 0 */
+  int32_t reserved;
+  int64_t q_tokens, k_tokens;    /* rows of q and out, of k and v; below 2^31 */
+  const void *q, *k, *v;         /* [tokens, heads, head_dim] */
+  const int32_t *cu_q, *cu_k;    /* [n_seqs + 1], ascending from 0 to q_tokens / k_tokens */
+  void* out;                     /* [q_tokens, q_heads, head_dim] */
+  int64_t q_strides[2], k_strides[2], v_strides[2], out_strides[2]; /* token, head */
+} fi_prompt_attention_args;
+fi_status fi_prompt_attention(const fi_prompt_attention_args* args, void* hip_stream);
+
+/* The same for trees of drafted tokens over a paged cache.  Sequence b has cached[b] committed tokens and the nodes
+ * [cu_nodes[b], cu_nodes[b + 1]) of q, whose own keys and values are in the cache already, at the places cached[b] ... behind the
+ * committed ones (fi_qk_norm_rope puts them there).  Place p of the sequence is row p % page_size of page
+ * block_table[b][p / page_size].  A node sees every committed token, and node j of its own sequence where bit j % 64 of
+ * mask[node][j / 64] is set (its ancestors and itself); without a mask, the nodes up to itself (a chain).  A tree of one node is
+ * a decoding step.  Rows that see nothing and unseen NaNs: as above.
+ * With long histories and few nodes the keys are shared out over workgroups, whose parts a second launch joins, always in
+ * the same order; they are kept in `workspace` meanwhile, the caller's, of at least fi_tree_attention_workspace bytes (0: may be
+ * NULL).  Calls that overlap in time need a workspace each. */
+typedef struct {
+  int32_t dtype;
+  int32_t n_seqs, q_heads, kv_heads, head_dim;
+  int32_t page_size, n_pages;    /* tokens per page, pages of the caches */
+  int32_t table_columns;         /* pages that a row of block_table names; page_size * table_columns below 2^31 */
+  int32_t mask_words;            /* 64-bit words per node; a sequence has at most 64 * mask_words nodes (later ones are not seen).  0 without a mask */
+  int32_t max_nodes;             /* most nodes of a sequence: later ones are not computed */
+  int32_t max_length;            /* most committed tokens and nodes of a sequence together; only guides how the work is shared out */
+  float scale;                   /* finite, > 0 */
+  int64_t nodes;                 /* rows of q and out, of all sequences; below 2^31 */
+  const void *q, *k_cache, *v_cache; /* [nodes, q_heads, head_dim], [n_pages, page_size, kv_heads, head_dim] */
+  const int32_t* block_table;    /* [n_seqs, table_columns], rows table_stride apart */
+  const int32_t* cached;         /* [n_seqs] */
+  const int32_t* cu_nodes;       /* [n_seqs + 1], ascending from 0 to nodes */
+  const uint64_t* mask;          /* [nodes, mask_words], contiguous, or NULL */
+  void* out;                     /* [nodes, q_heads, head_dim] */
+  void* workspace;               /* 16-byte aligned */
+  uint64_t workspace_bytes;
+  int64_t q_strides[2], out_strides[2]; /* token, head */
+  int64_t k_strides[3], v_strides[3];   /* page, token, head */
+  int64_t table_stride;
+} fi_tree_attention_args;
+/* Bytes of workspace that fi_tree_attention needs for these sizes (pointers and strides are not looked at). */
+fi_status fi_tree_attention_workspace(const fi_tree_attention_args* args, uint64_t* bytes);
+fi_status fi_tree_attention(const fi_tree_attention_args* args, void* hip_stream);
+
+/* y[m][n] = sum over groups g of scales[n][g] * sum over k in g of (w[n][k] - zeros[n][g]) * x[m][k]: a few rows times a
+ * matrix of 4-bit weights, read once per 64 rows.  w holds two weights in [0, 15] per byte, the even one in the low half;
+ * a group is `group` consecutive inputs.  The weights enter the products exactly, scales are applied to fp32 sums. */
+typedef struct {
+  int32_t dtype;                 /* of x and out */
+  int32_t rows, inputs, outputs;
+  int32_t group;                 /* 32, 64 or a multiple of 128; divides inputs */
+  int32_t reserved;
+  const void* x;                 /* [rows, inputs] */
+  const uint8_t* w;              /* [outputs, inputs / 2] */
+  const float* scales;           /* [outputs, inputs / group] */
+  const uint8_t* zeros;          /* [outputs, inputs / group], values in [0, 15]; NULL = 8 */
+  void* out;                     /* [rows, outputs] */
+  int64_t x_stride, w_stride, scales_stride, zeros_stride, out_stride; /* between rows */
+} fi_q4_matmul_args;
+fi_status fi_q4_matmul(const fi_q4_matmul_args* args, void* hip_stream);
+
 const char* fi_last_error(void); /* thread-local, valid until the next call on this thread */
 const char* fi_version(void);
 

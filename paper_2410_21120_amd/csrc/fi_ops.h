@@ -1,0 +1,17 @@
+// Launchers of the decoder operators: implemented in fi_rope.hip, fi_attn.hip and fi_q4.hip, called by fi_ops.cpp once the
+// arguments are checked.  Each returns a hipError_t as int.
+#pragma once
+
+#include "fi_internal.h"
+
+namespace fi {
+
+inline int32_t elem_size(int32_t dtype) { return dtype == FI_F32 ? 4 : 2; }
+
+int launch_qk_norm_rope(const fi_qk_norm_rope_args& a, void* stream);
+int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream);
+int launch_tree_attention(const fi_tree_attention_args& a, void* stream);
+int launch_q4_matmul(const fi_q4_matmul_args& a, void* stream);
+uint64_t tree_workspace(const fi_tree_attention_args& a);
+
+}  // namespace fi
