@@ -110,20 +110,697 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
       a.scale, lds, seen, [&](int j) { return at(a.k_cache, a.k_strides, j); }, [&](int j) { return at(a.v_cache, a.v_strides, j); });
 }
 
+// ---------------------------------------------------------------------------------------------------
+// Tiles on the matrix cores
+// ---------------------------------------------------------------------------------------------------
+// A wave has 32 queries as the columns of everything: scores S^T = K Q^T (keys x queries), outputs O^T = V^T P^T (values x queries).  A lane then
+// holds scores of ONE query (lanes l and l + 32 share it), so the running maximum and sum of the softmax are sums inside a lane and one
+// exchange, and the scores' registers are, rounded, the operand of the second product as they stand: its reduction runs over keys
+// in the order that the first product leaves them in (key 8 g + 4 h + i is element 4 g + i of half h).
+// Keys and values come into LDS by direct loads, 16-byte pieces permuted at the source so that operand reads meet no bank twice; values are read
+// transposed (16 lanes get columns of 4 x 16 elements), fp32 ones column by column.
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+template <typename T, int DB_>   // DB: blocks of 32 values of a head
+struct Tile {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int DB = DB_, ES = sizeof(T), EP = 16 / ES;                          // bytes of an element, elements of a piece
+  static constexpr int PB = (DB <= 2 ? 64 : DB <= 4 ? 128 : 256) * ES, NP = PB / 16;    // bytes and pieces of a row in LDS
+  static constexpr int KS = DB * 32 / (2 * EP);                                         // steps of two pieces in a score's sum
+  static constexpr int RPI = 1024 / PB;                                                 // rows that one load instruction brings
+  static constexpr int FV = F32 ? 2 : 4;                                                // values' addresses that differ by more than a constant
+
+  struct Addr { uint32_t k[KS < 8 ? KS : 8], v[FV]; };   // of the lane's operands in a tile of keys / values
+  static __device__ __forceinline__ int swizzle_k(int row) { return NP >= 16 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int swizzle_v(int row) { return F32 ? ((row >> 2) & 1) << 3 : NP >= 16 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+
+  static __device__ __forceinline__ void addresses(Addr& a) {
+    const int lane = threadIdx.x & 63, r31 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int kk = 0; kk < (KS < 8 ? KS : 8); ++kk) a.k[kk] = r31 * PB + (((2 * kk + half) ^ swizzle_k(r31)) << 4);
+#pragma unroll
+    for (int f = 0; f < FV; ++f) {
+      if constexpr (F32) a.v[f] = 4 * half * PB + (((f * 8) ^ (half << 3)) << 4) + r31 * 4;
+      else {
+        const int i = lane & 15, row = 4 * half + (i >> 2);
+        a.v[f] = row * PB + (((f * 4) ^ swizzle_v(row)) << 4) + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+      }
+    }
+  }
+
+  // The queries as operands: q[kk] = values (2 kk + half) * EP .. of this lane's query; zeros past D (a multiple of EP).
+  static __device__ __forceinline__ void load_q(const T* row, int D, u32x4 (&q)[KS]) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      const int at = (2 * kk + half) * EP;
+      q[kk] = u32x4{0, 0, 0, 0};
+      if (at < D) q[kk] = *reinterpret_cast<const u32x4*>(row + at);
+    }
+  }
+
+  // Rows [0, 32 KB) of a tile, instruction by instruction: `waves` waves share them, this is number `wave`.  rows(r): where key r's row begins, in pieces.
+  template <int KB, int WAVES, typename Rows>
+  static __device__ __forceinline__ void load_tile(const T* k, const T* v, uint8_t* tile, int wave, int D, Rows rows) {
+    const int lane = threadIdx.x & 63;
+    constexpr int NI = KB * 32 / RPI;
+#pragma unroll
+    for (int u = 0; u < (NI + WAVES - 1) / WAVES; ++u) {
+      const int i = u * WAVES + wave;
+      if (NI % WAVES && i >= NI) break;
+      const int row = i * RPI + lane / NP, pos = lane % NP;
+      uint32_t ko, vo;
+      rows(u, row, ko, vo);
+      const int pk = pos ^ swizzle_k(row), pv = pos ^ swizzle_v(row);
+      uint8_t* const at = tile + i * 1024;
+      if (pk * EP < D) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k + ((uint64_t)ko + pk) * EP), (lds_void*)at, 16, 0, 0);
+      if (pv * EP < D) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + ((uint64_t)vo + pv) * EP), (lds_void*)(at + KB * 32 * PB), 16, 0, 0);
+    }
+  }
+
+  static __device__ __forceinline__ f32x16 product(const u32x4 a, const u32x4 b, f32x16 c) {
+    if constexpr (F32) {
+      const float4 x = __builtin_bit_cast(float4, a), y = __builtin_bit_cast(float4, b);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, c, 0, 0, 0);
+      return __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, c, 0, 0, 0);
+    } else {
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+  }
+
+  struct State {
+    f32x16 o[DB];
+    float top, total;   // the maximum that the weights are taken against; the lane's share of their sum
+  };
+  static __device__ __forceinline__ void clear(State& s) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s.o[db][e] = 0.0f;
+    s.top = -INFINITY;
+    s.total = 0.0f;
+  }
+
+  // An infinity or a NaN among the values times a weight that is zero would be NaN, for queries that do not see the key too.  In tiles where some query
+  // does not see every key such values are taken out before the product, by all threads that share the tile (add_strange gives them to the queries that
+  // see them).  Tells whether the thread found one.
+  template <int KB>
+  static __device__ __forceinline__ bool take_out(uint8_t* tile, int thread, int threads) {
+    bool found = false;
+    for (int i = thread * 16; i < KB * 32 * PB; i += threads * 16) {
+      u32x4* const at = reinterpret_cast<u32x4*>(tile + KB * 32 * PB + i);
+      u32x4 a = *at;
+      uint32_t x = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x |= F32 ? (a[e] & 0x7F800000u) + 0x00800000u : (a[e] & 0x7F807F80u) + 0x00800080u;   // an exponent of ones carries into the sign's place
+      if (x & (F32 ? 0x80000000u : 0x80008000u)) {
+        found = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (F32) a[e] = (a[e] & 0x7F800000u) == 0x7F800000u ? 0u : a[e];
+          else a[e] = ((a[e] & 0x7F80u) == 0x7F80u ? 0u : a[e] & 0xFFFFu) | ((a[e] & 0x7F800000u) == 0x7F800000u ? 0u : a[e] & 0xFFFF0000u);
+        }
+        *at = a;
+      }
+    }
+    return found;
+  }
+  // Adds the values of the keys [from, to) that are no finite numbers to the sums of the queries that see them.
+  template <typename Row, typename Seen>
+  static __device__ __forceinline__ void add_strange(State& st, int D, int from, int to, Row row, Seen seen) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll 1
+    for (int key = from; key < to; ++key) {
+      const T* const v = row(key);
+      const bool see = seen(key);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int d = db * 32 + 8 * g + 4 * half, at = d < D ? d : 0;   // (sums past D are not stored)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float f = ld(v + at + i);
+            st.o[db][4 * g + i] += see && (__float_as_uint(f) & 0x7F800000u) == 0x7F800000u ? f : 0.0f;
+          }
+          __builtin_amdgcn_sched_barrier(0);   // (rare: not worth registers for a row in flight)
+        }
+    }
+  }
+
+  // One tile of 32 KB keys.  c: scale * log2(e).  MASKED: bit 8 g + 4 half + i of visible(kb) (half: this lane's) tells whether the lane's query sees key
+  // 32 kb + 8 g + 4 half + i.
+  template <int KB, bool MASKED, typename Visible>
+  static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, Visible visible) {
+    const int half = (threadIdx.x & 63) >> 5;
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk)
+        s[kb] = product(*reinterpret_cast<const u32x4*>(tile + at.k[kk & 7] + (kk >> 3) * 256 + kb * 32 * PB), q[kk], s[kb]);
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const uint32_t bits = visible(kb) >> (4 * half);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kb][e] = (bits >> (8 * (e >> 2) + (e & 3))) & 1 ? s[kb][e] : -INFINITY;
+      }
+    }
+    float m = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    // The weights may be taken against any number that keeps them in range: the maximum moves only when it has grown by a factor of 2^8 in weight.
+    if (__any((m - st.top) * c > 8.0f || (st.top == -INFINITY && m > -INFINITY))) {
+      const float now = fmaxf(st.top, m), shrink = __builtin_amdgcn_exp2f((st.top - (now == -INFINITY ? 0.0f : now)) * c);
+      st.total *= shrink;
+      st.top = now;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st.o[db][e] *= shrink;
+    }
+    const float base = st.top == -INFINITY ? 0.0f : st.top * c;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[kb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], c, -base));
+        st.total += s[kb][e];
+      }
+    const uint8_t* const values = tile + KB * 32 * PB;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const u32x4 p = {__float_as_uint(s[kb][4 * g]), __float_as_uint(s[kb][4 * g + 1]), __float_as_uint(s[kb][4 * g + 2]), __float_as_uint(s[kb][4 * g + 3])};
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            u32x4 a;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const uint32_t*>(values + at.v[db & 1] + (db >> 1) * 256 + (kb * 32 + 8 * g + i) * PB);
+            st.o[db] = product(a, p, st.o[db]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 p;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = pack_bf16x2(s[kb][8 * h + 2 * i], s[kb][8 * h + 2 * i + 1]);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const uint8_t* const from = values + at.v[db & 3] + (db >> 2) * 256 + (kb * 32 + 16 * h) * PB;
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)from));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(from + 8 * PB)));
+            u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
+            st.o[db] = product(a, p, st.o[db]);
+          }
+        }
+      }
+    }
+  }
+
+  // The lane's outputs: o[db][4 g ..] are values 32 db + 8 g + 4 half .. of its query.
+  static __device__ __forceinline__ void store(const State& st, T* row, int D, float inv) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = db * 32 + 8 * g + 4 * half;
+        if (d >= D) continue;
+        if constexpr (F32) *reinterpret_cast<float4*>(row + d) = make_float4(st.o[db][4 * g] * inv, st.o[db][4 * g + 1] * inv, st.o[db][4 * g + 2] * inv, st.o[db][4 * g + 3] * inv);
+        else *reinterpret_cast<uint2*>(row + d) = make_uint2(pack_bf16x2(st.o[db][4 * g] * inv, st.o[db][4 * g + 1] * inv), pack_bf16x2(st.o[db][4 * g + 2] * inv, st.o[db][4 * g + 3] * inv));
+      }
+  }
+};
+
+__device__ __forceinline__ float both_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+// This wave's direct loads have arrived and its reads are done; behind the barrier that holds for all waves.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void meet() {
+  arrived();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// The same for what the waves wrote to LDS themselves; loads stay in flight.
+__device__ __forceinline__ void meet_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+template <typename TL, int BYTES>
+__device__ __forceinline__ void clear_pads(uint8_t* smem, int D, int threads) {   // pieces past D are never loaded: zeros
+  if (D == TL::PB / TL::ES) return;
+  for (int i = threadIdx.x * 16; i < BYTES; i += threads * 16) *reinterpret_cast<u32x4*>(smem + i) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+}
+
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
+
+// A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS.
+template <typename T, int DB>
+__global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_tile_kernel(fi_prompt_attention_args a) {
+  using TL = Tile<T, DB>;
+  constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
+  int* const strange = reinterpret_cast<int*>(smem + 2 * BYTES);   // a masked tile held values that are no finite numbers
+  if (threadIdx.x == 0) *strange = 0;
+  // heads of one key head on one die (workgroups go to the eight dies in turn), late rows first: they see most keys
+  const int hq = a.q_heads, tile_id = (int)(gridDim.x / hq) - 1 - (int)(blockIdx.x / hq);
+  int h = blockIdx.x % hq;
+  if (hq % NXCD == 0) h = h % NXCD * (hq / NXCD) + h / NXCD;
+  // sequence b has the tiles from cu_q[b] / 128 + b on: enough for its rows wherever they start
+  int lo = 0, hi = a.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.cu_q[mid] / PROMPT_ROWS + mid <= tile_id) lo = mid;
+    else hi = mid - 1;
+  }
+  const int b = lo, nq = (int)a.q_tokens, nk = (int)a.k_tokens;
+  const int q0 = clamp_int(a.cu_q[b], 0, nq), q1 = clamp_int(a.cu_q[b + 1], q0, nq), k0 = clamp_int(a.cu_k[b], 0, nk), k1 = clamp_int(a.cu_k[b + 1], k0, nk);
+  const int first = (tile_id - (q0 / PROMPT_ROWS + b)) * PROMPT_ROWS, rows = q1 - q0, keys = k1 - k0;
+  if (first < 0 || first >= rows) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1;
+  // the last key that a query sees (-1: none), of this lane's, of the wave's first and last, of the workgroup's last
+  auto last_of = [&](int r) { return a.causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; };
+  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + PROMPT_ROWS - 1);
+  const int hk = h / (hq / a.kv_heads), D = a.head_dim;
+  const T* const k = static_cast<const T*>(a.k) + k0 * a.k_strides[0] + hk * a.k_strides[1];
+  const T* const v = static_cast<const T*>(a.v) + k0 * a.v_strides[0] + hk * a.v_strides[1];
+  const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
+  clear_pads<TL, 2 * BYTES>(smem, D, 64 * PROMPT_WAVES);
+  u32x4 q[TL::KS];
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(q0 + mine) * a.q_strides[0] + h * a.q_strides[1], D, q);
+  typename TL::Addr at;
+  TL::addresses(at);
+  typename TL::State st;
+  TL::clear(st);
+  const float c = a.scale * 1.44269504f;
+  const int tiles = (most + KEYS) / KEYS;   // 0 where nobody sees a key
+  auto load = [&](int t) {
+    TL::template load_tile<KB, PROMPT_WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+      const uint32_t key = (uint32_t)(t * KEYS + r < keys ? t * KEYS + r : keys - 1);   // (rows past the end: the last key once more, unseen)
+      ko = key * ks;
+      vo = key * vs;
+    });
+  };
+  if (tiles > 0) load(0);
+  for (int t = 0; t < tiles; ++t) {
+    meet();
+    if (t + 1 < tiles) load(t + 1);
+    uint8_t* const tile = smem + (t & 1) * BYTES;
+    if (t * KEYS + KEYS - 1 > least) {
+      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * PROMPT_WAVES)) *strange = 1;
+      meet_lds();
+    }
+    if (t * KEYS + KEYS - 1 <= wave_least) TL::template attend<KB, false>(st, q, tile, at, c, [](int) { return ~0u; });
+    else if (t * KEYS <= wave_most) TL::template attend<KB, true>(st, q, tile, at, c, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
+  }
+  if (tiles > 0 && *strange)   // (written before the last barrier)
+    TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
+  const float total = both_halves(st.total);
+  if (row < rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(q0 + row) * a.out_strides[0] + h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+}
+
+// What a workgroup of the tree kernels works on: the rows (node, head) of one key head of one sequence, and a share of its keys.
+struct TreeWork {
+  int b, hk, cached, keys, n0, nodes, split, splits;
+};
+
+// Shares of a sequence's keys: as many as there are, but none below `least` keys.
+__device__ __forceinline__ int shares(int keys, int splits, int least) { return clamp_int((keys + least - 1) / least, 1, splits); }
+
+__device__ __forceinline__ TreeWork tree_work(const fi_tree_attention_args& a, int id, int splits, int least) {
+  TreeWork w;
+  w.split = id % splits;
+  id /= splits;
+  w.hk = id % a.kv_heads;
+  w.b = id / a.kv_heads;
+  const int total = (int)a.nodes, places = a.n_pages ? a.page_size * a.table_columns : 0;
+  w.n0 = clamp_int(a.cu_nodes[w.b], 0, total);
+  w.nodes = clamp_int(a.cu_nodes[w.b + 1], w.n0, total) - w.n0;
+  if (w.nodes > a.max_nodes) w.nodes = a.max_nodes;
+  w.cached = clamp_int(a.cached[w.b], 0, places);
+  w.keys = w.nodes < places - w.cached ? w.cached + w.nodes : places;
+  w.splits = shares(w.keys, splits, least);
+  return w;
+}
+
+// Which of the 32 keys from `key` on a node (place `node` in its tree, mask row `words`) sees.
+__device__ __forceinline__ uint32_t tree_visible(const fi_tree_attention_args& a, const TreeWork& w, int node, const uint64_t* words, int key) {
+  const int base = key - w.cached;   // the tree's node that the first key is; below zero: committed
+  uint32_t bits;
+  if (!a.mask) bits = low_bits(node + 1 - base);
+  else if (base < 0) bits = base <= -32 ? ~0u : low_bits(-base) | (uint32_t)words[0] << -base;
+  else {
+    const int at = base >> 6, sh = base & 63;
+    uint64_t x = at < a.mask_words ? words[at] >> sh : 0;
+    if (sh > 32 && at + 1 < a.mask_words) x |= words[at + 1] << (64 - sh);
+    bits = (uint32_t)x;
+  }
+  return bits & low_bits(w.keys - key);
+}
+
+// Where key `key` of the sequence is, in pieces from the caches' beginnings (the key head's).
+__device__ __forceinline__ void tree_row(const fi_tree_attention_args& a, const int32_t* table, int key, int ep, uint32_t& ko, uint32_t& vo) {
+  const int column = key / a.page_size, place = key - column * a.page_size;
+  const int page = clamp_int(table[column], 0, a.n_pages - 1);
+  ko = (uint32_t)((page * a.k_strides[0] + place * a.k_strides[1]) / ep);
+  vo = (uint32_t)((page * a.v_strides[0] + place * a.v_strides[1]) / ep);
+}
+
+// Parts of a row (node, head) in the workspace: `splits` times head_dim sums, then for all rows the maximum and the weights' sum of each.
+__device__ __forceinline__ float* part_sums(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
+  return static_cast<float*>(a.workspace) + (row * splits + split) * a.head_dim;
+}
+__device__ __forceinline__ float* part_stats(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
+  return static_cast<float*>(a.workspace) + a.nodes * a.q_heads * splits * a.head_dim + (row * splits + split) * 2;
+}
+
+// TL::add_strange for the keys [from, to) of a tree: of those only the tiles that were masked.
+template <typename TL, typename T>
+__device__ __forceinline__ void tree_strange(const fi_tree_attention_args& a, const TreeWork& w, typename TL::State& st, const T* v, const int32_t* table, const uint64_t* words,
+                                             int node, int from, int to, int tile) {
+  const int masked = w.cached / tile * tile;
+  TL::add_strange(st, a.head_dim, from > masked ? from : masked, to < w.keys ? to : w.keys,
+                  [&](int key) {
+                    uint32_t ko, vo;
+                    tree_row(a, table, key, TL::EP, ko, vo);
+                    return v + (uint64_t)vo * TL::EP;
+                  },
+                  [&](int key) { return (tree_visible(a, w, node, words, key) & 1) != 0; });
+}
+
+template <typename TL, typename T>
+__device__ __forceinline__ void finish(const fi_tree_attention_args& a, const TreeWork& w, int splits, typename TL::State& st, float total, bool there, int node, int head) {
+  if (!there) return;
+  if (w.splits == 1) {
+    TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1], a.head_dim, total == 0.0f ? 0.0f : 1.0f / total);
+    return;
+  }
+  const int64_t row = (int64_t)(w.n0 + node) * a.q_heads + head;
+  float* const sums = part_sums(a, row, splits, w.split);
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = db * 32 + 8 * g + 4 * half;
+      if (d < a.head_dim) *reinterpret_cast<float4*>(sums + d) = make_float4(st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]);
+    }
+  if (half == 0) *reinterpret_cast<float2*>(part_stats(a, row, splits, w.split)) = make_float2(st.top, total);
+}
+
+constexpr int TREE_WAVES = 4;
+
+// Many rows: the waves have 32 rows each and share the tiles, as for a prompt.
+template <typename T, int DB>
+__global__ void __launch_bounds__(64 * TREE_WAVES, DB <= 4 ? 2 : 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least) {
+  using TL = Tile<T, DB>;
+  constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
+  int* const strange = reinterpret_cast<int*>(smem + 2 * BYTES);
+  if (threadIdx.x == 0) *strange = 0;
+  const int D = a.head_dim, group = a.q_heads / a.kv_heads;
+  const int units = a.n_seqs * a.kv_heads * splits, block = blockIdx.x / units;
+  const TreeWork w = tree_work(a, blockIdx.x % units, splits, least);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = w.nodes * group, first = block * 32 * TREE_WAVES;
+  if (first >= rows || w.split >= w.splits) return;
+  const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
+  const int all = (w.keys + KEYS - 1) / KEYS, t0 = (int)((int64_t)all * w.split / w.splits), t1 = (int)((int64_t)all * (w.split + 1) / w.splits);
+  const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
+  const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
+  const int32_t* const table = a.block_table + w.b * a.table_stride;
+  const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
+  clear_pads<TL, 2 * BYTES>(smem, D, 64 * TREE_WAVES);
+  u32x4 q[TL::KS];
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, q);
+  typename TL::Addr at;
+  TL::addresses(at);
+  typename TL::State st;
+  TL::clear(st);
+  const float c = a.scale * 1.44269504f;
+  auto load = [&](int t) {
+    TL::template load_tile<KB, TREE_WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+      tree_row(a, table, t * KEYS + r < w.keys ? t * KEYS + r : w.keys - 1, TL::EP, ko, vo);
+    });
+  };
+  if (t0 < t1) load(t0);
+  for (int t = t0; t < t1; ++t) {
+    meet();
+    if (t + 1 < t1) load(t + 1);
+    uint8_t* const tile = smem + (t & 1) * BYTES;
+    if ((t + 1) * KEYS > w.cached) {
+      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * TREE_WAVES)) *strange = 1;
+      meet_lds();
+    }
+    if (first + 32 * wave >= rows) continue;
+    if ((t + 1) * KEYS <= w.cached) TL::template attend<KB, false>(st, q, tile, at, c, [](int) { return ~0u; });
+    else TL::template attend<KB, true>(st, q, tile, at, c, [&](int kb) { return tree_visible(a, w, node, words, t * KEYS + 32 * kb); });
+  }
+  if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, table, words, node, t0 * KEYS, t1 * KEYS, KEYS);
+  finish<TL, T>(a, w, splits, st, both_halves(st.total), row < rows, node, head);
+}
+
+// Few rows: every wave has the same 32 rows and keys of its own, 32 at a time, loaded by itself (no barriers); joined in LDS at the end.
+template <typename T, int DB>
+struct Own {
+  using TL = Tile<T, DB>;
+  static constexpr int BYTES = 2 * 32 * TL::PB;                                        // a tile
+  static constexpr int WAVES = TL::PB <= 256 ? 4 : TL::PB == 512 ? 2 : 1;              // 128 KB of tiles at most
+};
+template <typename T, int DB>
+__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, int splits, int least) {
+  using TL = Tile<T, DB>;
+  constexpr int BYTES = Own<T, DB>::BYTES, WAVES = Own<T, DB>::WAVES;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES * WAVES + WAVES * 512];
+  const int D = a.head_dim, group = a.q_heads / a.kv_heads;
+  const int units = a.n_seqs * a.kv_heads * splits, block = blockIdx.x / units;
+  const TreeWork w = tree_work(a, blockIdx.x % units, splits, least);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = w.nodes * group, first = block * 32;
+  if (first >= rows || w.split >= w.splits) return;
+  const int row = first + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
+  const int all = (w.keys + 31) / 32, share = w.split * WAVES + wave, total_shares = w.splits * WAVES;
+  const int t0 = (int)((int64_t)all * share / total_shares), t1 = (int)((int64_t)all * (share + 1) / total_shares);
+  const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
+  const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
+  const int32_t* const table = a.block_table + w.b * a.table_stride;
+  const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
+  uint8_t* const tiles = smem + wave * 2 * BYTES;
+  clear_pads<TL, 2 * BYTES * WAVES>(smem, D, 64 * WAVES);
+  u32x4 q[TL::KS];
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, q);
+  typename TL::Addr at;
+  TL::addresses(at);
+  typename TL::State st;
+  TL::clear(st);
+  const float c = a.scale * 1.44269504f;
+  auto load = [&](int t) {   // lane r finds row r, the lanes that load it ask for it
+    const int key = t * 32 + (lane & 31);
+    uint32_t mk, mv;
+    tree_row(a, table, key < w.keys ? key : w.keys - 1, TL::EP, mk, mv);
+    TL::template load_tile<1, 1>(k, v, tiles + (t & 1) * BYTES, 0, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+      ko = __shfl(mk, r);
+      vo = __shfl(mv, r);
+    });
+  };
+  bool strange = false;
+  if (t0 < t1) load(t0);
+  for (int t = t0; t < t1; ++t) {
+    arrived();
+    if (t + 1 < t1) load(t + 1);
+    uint8_t* const tile = tiles + (t & 1) * BYTES;
+    if ((t + 1) * 32 > w.cached) strange |= __any(TL::template take_out<1>(tile, lane, 64)) != 0;
+    if ((t + 1) * 32 <= w.cached) TL::template attend<1, false>(st, q, tile, at, c, [](int) { return ~0u; });
+    else TL::template attend<1, true>(st, q, tile, at, c, [&](int) { return tree_visible(a, w, node, words, t * 32); });
+  }
+  if (strange) tree_strange<TL, T>(a, w, st, v, table, words, node, t0 * 32, t1 * 32, 32);
+  float total = both_halves(st.total);
+  if constexpr (WAVES > 1) {
+    // the waves' sums against the largest maximum, added in the order of the waves by wave 0
+    float* const own = reinterpret_cast<float*>(smem + wave * 2 * BYTES);
+    float2* const stats = reinterpret_cast<float2*>(smem + 2 * BYTES * WAVES);
+    arrived();
+    if (wave) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) own[(db * 16 + e) * 64 + lane] = st.o[db][e];
+    }
+    stats[wave * 64 + lane] = make_float2(st.top, total);
+    __syncthreads();
+    if (wave) return;
+    float top = st.top;
+#pragma unroll
+    for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[x * 64 + lane].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+    const float f0 = __builtin_amdgcn_exp2f((st.top - base) * c);
+    total *= f0;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st.o[db][e] *= f0;
+#pragma unroll
+    for (int x = 1; x < WAVES; ++x) {
+      const float f = __builtin_amdgcn_exp2f((stats[x * 64 + lane].x - base) * c);
+      total += stats[x * 64 + lane].y * f;
+      const float* const other = reinterpret_cast<const float*>(smem + x * 2 * BYTES);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st.o[db][e] += other[(db * 16 + e) * 64 + lane] * f;
+    }
+    st.top = top;
+  }
+  finish<TL, T>(a, w, splits, st, total, row < rows, node, head);
+}
+
+// Joins the parts of a row, in their order: one wave per (node, head).
+template <typename T>
+__global__ void __launch_bounds__(256) tree_join_kernel(fi_tree_attention_args a, int splits, int least) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.nodes * a.q_heads) return;
+  const int node = (int)(row / a.q_heads), head = (int)(row - (int64_t)node * a.q_heads), lane = threadIdx.x & 63;
+  const int b = find_seq(a.cu_nodes, a.n_seqs, node);
+  const TreeWork w = tree_work(a, b * a.kv_heads * splits, splits, least);
+  if (w.splits == 1 || node < w.n0 || node - w.n0 >= w.nodes) return;
+  const float c = a.scale * 1.44269504f;
+  const float2* const stats = reinterpret_cast<const float2*>(part_stats(a, row, splits, 0));
+  const float* const sums = part_sums(a, row, splits, 0);
+  float top = -INFINITY;
+  for (int s = 0; s < w.splits; ++s) top = fmaxf(top, stats[s].x);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f, acc[RUN] = {};
+  for (int s = 0; s < w.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f((stats[s].x - base) * c);
+    total += stats[s].y * f;
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+      if (lane + 64 * i < a.head_dim) acc[i] += sums[(int64_t)s * a.head_dim + lane + 64 * i] * f;
+  }
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  T* const out = static_cast<T*>(a.out) + node * a.out_strides[0] + head * a.out_strides[1];
+#pragma unroll
+  for (int i = 0; i < RUN; ++i)
+    if (lane + 64 * i < a.head_dim) st(out + lane + 64 * i, acc[i] * inv);
+}
+
+// Whether every row of a tensor starts on 16 bytes and its last one, counted in 16-byte pieces, has a 32-bit offset.
+bool pieces(const void* p, const int64_t* strides, const int64_t* counts, int n, int es) {
+  if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  double reach = 0;
+  for (int i = 0; i < n; ++i) {
+    if (strides[i] * es % 16) return false;
+    reach += (double)strides[i] * es / 16 * (counts[i] > 0 ? counts[i] - 1 : 0);
+  }
+  return reach + 64 < 4294967296.0;
+}
+bool starts(const void* p, const int64_t* strides, int n, int es, int bytes) {
+  if (reinterpret_cast<uintptr_t>(p) % bytes) return false;
+  for (int i = 0; i < n; ++i)
+    if (strides[i] * es % bytes) return false;
+  return true;
+}
+int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 96 ? 3 : head_dim <= 128 ? 4 : 8; }
+
+bool prompt_on_tiles(const fi_prompt_attention_args& a) {
+  const int es = elem_size(a.dtype);
+  const int64_t n[2] = {a.k_tokens, a.kv_heads};
+  return a.head_dim * es % 16 == 0 && starts(a.q, a.q_strides, 2, es, 16) && starts(a.out, a.out_strides, 2, es, 4 * es) && pieces(a.k, a.k_strides, n, 2, es) &&
+         pieces(a.v, a.v_strides, n, 2, es);
+}
+template <typename T>
+int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
+  const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
+  switch (blocks_of(a.head_dim)) {
+    case 2: prompt_tile_kernel<T, 2><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    case 3: prompt_tile_kernel<T, 3><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    case 4: prompt_tile_kernel<T, 4><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    default: prompt_tile_kernel<T, 8><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a);
+  }
+  return (int)hipGetLastError();
+}
+
+bool tree_on_tiles(const fi_tree_attention_args& a) {
+  const int es = elem_size(a.dtype);
+  const int64_t n[3] = {a.n_pages, a.page_size, a.kv_heads};
+  return a.n_pages > 0 && a.table_columns > 0 && a.head_dim * es % 16 == 0 && starts(a.q, a.q_strides, 2, es, 16) && starts(a.out, a.out_strides, 2, es, 4 * es) &&
+         pieces(a.k_cache, a.k_strides, n, 3, es) && pieces(a.v_cache, a.v_strides, n, 3, es);
+}
+
+// How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 that share
+// them; parts of every sequence's keys, and the least keys of a part.
+struct TreePlan { bool own; int blocks, splits, least; };
+TreePlan plan_tree(const fi_tree_attention_args& a) {
+  TreePlan p;
+  const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
+  p.own = rows <= 32;
+  p.blocks = (int)((rows + (p.own ? 31 : 127)) / (p.own ? 32 : 128));
+  p.least = p.own ? 256 : 512;
+  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, want = units > 0 ? (512 + units - 1) / units : 1;
+  const int64_t most = ((int64_t)a.max_length + p.least - 1) / p.least;
+  p.splits = (int)(want < most ? want : most);
+  p.splits = p.splits < 1 ? 1 : p.splits > 64 ? 64 : p.splits;
+  return p;
+}
+template <typename T, int DB>
+int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
+  const dim3 grid((uint32_t)(a.n_seqs * a.kv_heads * p.splits * p.blocks));
+  if (p.own) tree_own_kernel<T, DB><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least);
+  else tree_tile_kernel<T, DB><<<grid, 64 * TREE_WAVES, 0, s>>>(a, p.splits, p.least);
+  if (p.splits > 1) tree_join_kernel<T><<<dim3((uint32_t)((a.nodes * a.q_heads + 3) / 4)), 256, 0, s>>>(a, p.splits, p.least);
+  return (int)hipGetLastError();
+}
+template <typename T>
+int launch_tree_tiles(const fi_tree_attention_args& a, hipStream_t s) {
+  const TreePlan p = plan_tree(a);
+  switch (blocks_of(a.head_dim)) {
+    case 2: return launch_tree_db<T, 2>(a, p, s);
+    case 3: return launch_tree_db<T, 3>(a, p, s);
+    case 4: return launch_tree_db<T, 4>(a, p, s);
+    default: return launch_tree_db<T, 8>(a, p, s);
+  }
+}
+
 }  // namespace
 
 int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (prompt_on_tiles(a)) return a.dtype == FI_F32 ? launch_prompt_tiles<float>(a, s) : launch_prompt_tiles<bf16_t>(a, s);
   const dim3 grid((uint32_t)a.q_tokens, (uint32_t)a.q_heads);
   if (a.dtype == FI_F32) prompt_row_kernel<float><<<grid, 64, 0, s>>>(a);
   else prompt_row_kernel<bf16_t><<<grid, 64, 0, s>>>(a);
   return (int)hipGetLastError();
 }
 
-uint64_t tree_workspace(const fi_tree_attention_args&) { return 0; }
+uint64_t tree_workspace(const fi_tree_attention_args& a) {
+  const TreePlan p = plan_tree(a);
+  return p.splits > 1 ? (uint64_t)a.nodes * a.q_heads * p.splits * (a.head_dim + 2) * 4 : 0;
+}
 
 int launch_tree_attention(const fi_tree_attention_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (tree_on_tiles(a)) return a.dtype == FI_F32 ? launch_tree_tiles<float>(a, s) : launch_tree_tiles<bf16_t>(a, s);
   const dim3 grid((uint32_t)a.nodes, (uint32_t)a.q_heads);
   if (a.dtype == FI_F32) tree_row_kernel<float><<<grid, 64, 0, s>>>(a);
   else tree_row_kernel<bf16_t><<<grid, 64, 0, s>>>(a);
