@@ -566,8 +566,12 @@ fi_status fi_tree_attention_workspace(const fi_tree_attention_args* args, uint64
 fi_status fi_tree_attention(const fi_tree_attention_args* args, void* hip_stream);
 
 /* y[m][n] = sum over groups g of scales[n][g] * sum over k in g of (w[n][k] - zeros[n][g]) * x[m][k]: a few rows times a
- * matrix of 4-bit weights, read once per 64 rows.  w holds two weights in [0, 15] per byte, the even one in the low half;
- * a group is `group` consecutive inputs.  The weights enter the products exactly, scales are applied to fp32 sums. */
+ * matrix of 4-bit weights, read once per 32 rows.  w holds two weights in [0, 15] per byte, the even one in the low half;
+ * a group is `group` consecutive inputs.  The weights enter the products exactly, scales are applied to fp32 sums; a row
+ * that holds an infinity or a NaN yields NaN.
+ * With more than a few rows the inputs are shared out over workgroups, whose sums a second launch adds, always in the same
+ * order; they are kept in `workspace` meanwhile, the caller's, of at least fi_q4_matmul_workspace bytes (0: may be NULL).
+ * Calls that overlap in time need a workspace each. */
 typedef struct {
   int32_t dtype;                 /* of x and out */
   int32_t rows, inputs, outputs;
@@ -578,8 +582,12 @@ typedef struct {
   const float* scales;           /* [outputs, inputs / group] */
   const uint8_t* zeros;          /* [outputs, inputs / group], values in [0, 15]; NULL = 8 */
   void* out;                     /* [rows, outputs] */
+  void* workspace;               /* 16-byte aligned */
+  uint64_t workspace_bytes;
   int64_t x_stride, w_stride, scales_stride, zeros_stride, out_stride; /* between rows */
 } fi_q4_matmul_args;
+/* Bytes of workspace that fi_q4_matmul needs for these sizes (pointers and strides are not looked at). */
+fi_status fi_q4_matmul_workspace(const fi_q4_matmul_args* args, uint64_t* bytes);
 fi_status fi_q4_matmul(const fi_q4_matmul_args* args, void* hip_stream);
 
 const char* fi_last_error(void); /* thread-local, valid until the next call on this thread */

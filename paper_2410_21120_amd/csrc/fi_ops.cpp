@@ -71,6 +71,21 @@ fi_status check_tree_sizes(const fi_tree_attention_args& a) {
   return FI_OK;
 }
 
+fi_status check_q4_sizes(const fi_q4_matmul_args& a) {
+  if (!good_dtype(a.dtype)) return FI_EINVAL;
+  if (a.rows < 0 || a.inputs < 0 || a.outputs < 0 || a.group < 1 || a.inputs % a.group) { set_error("%d x %d x %d in groups of %d", a.rows, a.outputs, a.inputs, a.group); return FI_EINVAL; }
+  if (a.group != 32 && a.group != 64 && a.group % 128) { set_error("groups of %d: 32, 64 and multiples of 128 are covered", a.group); return FI_EUNSUPPORTED; }
+  if (a.rows > 1 << 19 || a.inputs > 1 << 24 || a.outputs > 1 << 24) { set_error("%d x %d x %d: too many", a.rows, a.outputs, a.inputs); return FI_EUNSUPPORTED; }
+  return FI_OK;
+}
+
+bool good_workspace(const void* p, uint64_t bytes, uint64_t need) {
+  if (!need) return true;
+  if (!good(p, 16, "workspace")) return false;
+  if (bytes < need) { set_error("the workspace has %llu bytes, %llu are needed", (unsigned long long)bytes, (unsigned long long)need); return false; }
+  return true;
+}
+
 }  // namespace
 }  // namespace fi
 
@@ -161,26 +176,28 @@ fi_status fi_tree_attention(const fi_tree_attention_args* args, void* hip_stream
   if (!good_strides(a.q_strides, 2, "q") || !good_strides(a.k_strides, 3, "k_cache") || !good_strides(a.v_strides, 3, "v_cache") || !good_strides(a.out_strides, 2, "out") ||
       !good_strides(&a.table_stride, 1, "block_table")) return FI_EINVAL;
   if (!apart(a.out_strides[0], a.nodes, a.head_dim, "out") || !apart(a.out_strides[1], a.q_heads, a.head_dim, "out")) return FI_EINVAL;
-  const uint64_t need = tree_workspace(a);
-  if (need) {
-    if (!good(a.workspace, 16, "workspace")) return FI_EINVAL;
-    if (a.workspace_bytes < need) { set_error("the workspace has %llu bytes, %llu are needed", (unsigned long long)a.workspace_bytes, (unsigned long long)need); return FI_EINVAL; }
-  }
+  if (!good_workspace(a.workspace, a.workspace_bytes, tree_workspace(a))) return FI_EINVAL;
   return done(launch_tree_attention(a, hip_stream), "fi_tree_attention");
+}
+
+fi_status fi_q4_matmul_workspace(const fi_q4_matmul_args* args, uint64_t* bytes) {
+  if (!args || !bytes) { set_error("null argument"); return FI_EINVAL; }
+  if (fi_status st = check_q4_sizes(*args)) return st;
+  *bytes = q4_workspace(*args);
+  return FI_OK;
 }
 
 fi_status fi_q4_matmul(const fi_q4_matmul_args* args, void* hip_stream) {
   if (!args) { set_error("null argument"); return FI_EINVAL; }
   const fi_q4_matmul_args& a = *args;
-  if (!good_dtype(a.dtype)) return FI_EINVAL;
-  if (a.rows < 0 || a.inputs < 0 || a.outputs < 0 || a.group < 1 || a.inputs % a.group) { set_error("%d x %d x %d in groups of %d", a.rows, a.outputs, a.inputs, a.group); return FI_EINVAL; }
-  if (a.group != 32 && a.group != 64 && a.group % 128) { set_error("groups of %d: 32, 64 and multiples of 128 are covered", a.group); return FI_EUNSUPPORTED; }
+  if (fi_status st = check_q4_sizes(a)) return st;
   if (a.rows == 0 || a.outputs == 0) return FI_OK;
   const int es = elem_size(a.dtype);
   if (!good(a.out, es, "out")) return FI_EINVAL;
   if (a.inputs && (!good(a.x, es, "x") || !good(a.w, 1, "w") || !good(a.scales, 4, "scales"))) return FI_EINVAL;
   const int64_t strides[5] = {a.x_stride, a.w_stride, a.scales_stride, a.zeros ? a.zeros_stride : 0, a.out_stride};
   if (!good_strides(strides, 5, "x, w, scales, zeros or out") || !apart(a.out_stride, a.rows, a.outputs, "out")) return FI_EINVAL;
+  if (!good_workspace(a.workspace, a.workspace_bytes, q4_workspace(a))) return FI_EINVAL;
   return done(launch_q4_matmul(a, hip_stream), "fi_q4_matmul");
 }
 

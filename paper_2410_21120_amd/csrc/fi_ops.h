@@ -12,6 +12,7 @@ int launch_qk_norm_rope(const fi_qk_norm_rope_args& a, void* stream);
 int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream);
 int launch_tree_attention(const fi_tree_attention_args& a, void* stream);
 int launch_q4_matmul(const fi_q4_matmul_args& a, void* stream);
+uint64_t q4_workspace(const fi_q4_matmul_args& a);
 uint64_t tree_workspace(const fi_tree_attention_args& a);
 
 }  // namespace fi

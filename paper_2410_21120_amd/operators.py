@@ -42,7 +42,7 @@ class fi_tree_attention_args(C.Structure):
 
 
 class fi_q4_matmul_args(C.Structure):
-    _fields_ = _fields("i:dtype i:rows i:inputs i:outputs i:group i:reserved p:x p:w p:scales p:zeros p:out "
+    _fields_ = _fields("i:dtype i:rows i:inputs i:outputs i:group i:reserved p:x p:w p:scales p:zeros p:out p:workspace u:workspace_bytes "
                        "l:x_stride l:w_stride l:scales_stride l:zeros_stride l:out_stride")
 
 
@@ -63,6 +63,12 @@ def fi_tree_attention_workspace(args: fi_tree_attention_args) -> int:
 
 def fi_tree_attention(args: fi_tree_attention_args, stream_ptr=0) -> None:
     _b._check(_b.lib().fi_tree_attention(C.byref(args), stream_ptr), "fi_tree_attention")
+
+
+def fi_q4_matmul_workspace(args: fi_q4_matmul_args) -> int:
+    n = C.c_uint64(0)
+    _b._check(_b.lib().fi_q4_matmul_workspace(C.byref(args), C.byref(n)), "fi_q4_matmul_workspace")
+    return n.value
 
 
 def fi_q4_matmul(args: fi_q4_matmul_args, stream_ptr=0) -> None:
@@ -115,6 +121,21 @@ def _call(entry, args, like, stream):
             entry(args, cuda.current_stream().cuda_stream if stream is None else stream)
     else:
         entry(args, cuda.current_stream().cuda_stream if stream is None else stream)
+
+
+def _workspace(args, needed, workspace, like, stream):
+    """Puts the caller's workspace, or one made here, into args.  Returns what has to live until the call is made."""
+    if workspace is None:
+        need = needed(args)
+        if not need:
+            return None
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=like.device)
+        if stream is not None:   # the memory may be handed out again only after that stream is done with it
+            workspace.record_stream(_torch.cuda.ExternalStream(stream, device=like.device))
+    elif workspace.dtype != _torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous uint8 on {like.device} is wanted")
+    args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    return workspace
 
 
 def qk_norm_rope(q, k, v, positions, inv_freq, *, q_weight=None, k_weight=None, eps=1e-6, sections=None, interleaved=False, slots=None,
@@ -218,23 +239,15 @@ def tree_attention(q, k_cache, v_cache, block_table, cached, cu_nodes, mask=None
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), _plain(cached, "cached", i32, (seqs,), q),
         _plain(cu_nodes, "cu_nodes", i32, (seqs + 1,), q), mask_ptr, out.data_ptr(), 0, 0,
         qs[0], qs[1], os[0], os[1], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], block_table.stride(0))
-    if workspace is None:
-        need = fi_tree_attention_workspace(args)
-        if need:
-            workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
-            if stream is not None:   # the memory may be handed out again only after that stream is done with it
-                workspace.record_stream(_torch.cuda.ExternalStream(stream, device=q.device))
-    elif workspace.dtype != _torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
-        raise ValueError("workspace: contiguous uint8 on the device of q is wanted")
-    if workspace is not None:
-        args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    workspace = _workspace(args, fi_tree_attention_workspace, workspace, q, stream)
     _call(fi_tree_attention, args, q, stream)
     return out
 
 
-def q4_matmul(x, w, scales, zeros=None, *, group=None, out=None, stream=None):
+def q4_matmul(x, w, scales, zeros=None, *, group=None, out=None, workspace=None, stream=None):
     """x [rows, inputs] times 4-bit weights: w uint8 [outputs, inputs / 2], two weights per byte, the even one in the low half; scales fp32 and
-    zeros uint8 (8 where None) [outputs, inputs / group].  Returns out [rows, outputs] in x's type."""
+    zeros uint8 (8 where None) [outputs, inputs / group].  workspace: uint8, fi_q4_matmul_workspace bytes; made here if None.  Returns out [rows,
+    outputs] in x's type."""
     kind = _kind(x, "x")
     if x.dim() != 2 or w.dim() != 2 or scales.dim() != 2:
         raise ValueError("x is [rows, inputs], w [outputs, inputs / 2], scales [outputs, groups]")
@@ -251,6 +264,7 @@ def q4_matmul(x, w, scales, zeros=None, *, group=None, out=None, stream=None):
     out = _torch.empty((rows, outputs), dtype=x.dtype, device=x.device) if out is None else out
     xs, os = _rows(x, "x", (rows, inputs), x), _rows(out, "out", (rows, outputs), x)
     args = fi_q4_matmul_args(kind, rows, inputs, outputs, group, 0, x.data_ptr(), w.data_ptr(), scales.data_ptr(), zeros.data_ptr() if zeros is not None else 0,
-                             out.data_ptr(), xs[0], w.stride(0), scales.stride(0), zeros.stride(0) if zeros is not None else 0, os[0])
+                             out.data_ptr(), 0, 0, xs[0], w.stride(0), scales.stride(0), zeros.stride(0) if zeros is not None else 0, os[0])
+    workspace = _workspace(args, fi_q4_matmul_workspace, workspace, x, stream)
     _call(fi_q4_matmul, args, x, stream)
     return out
