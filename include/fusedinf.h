@@ -522,7 +522,7 @@ typedef struct {
   int32_t causal;                /* 0 / 1 */
   float scale;                   /* finite, > 0 */
   int32_t reserved;
-  int64_t q_tokens, k_tokens;    /* rows of q and out, of k and v; below 2^31 */
+  int64_t q_tokens, k_tokens;    /* rows of q and out, of k and v; below 2^31 - 1024 */
   const void *q, *k, *v;         /* [tokens, heads, head_dim] */
   const int32_t *cu_q, *cu_k;    /* [n_seqs + 1], ascending from 0 to q_tokens / k_tokens */
   void* out;                     /* [q_tokens, q_heads, head_dim] */
@@ -543,12 +543,12 @@ typedef struct {
   int32_t dtype;
   int32_t n_seqs, q_heads, kv_heads, head_dim;
   int32_t page_size, n_pages;    /* tokens per page, pages of the caches */
-  int32_t table_columns;         /* pages that a row of block_table names; page_size * table_columns below 2^31 */
+  int32_t table_columns;         /* pages that a row of block_table names; page_size * table_columns below 2^31 - 1024 */
   int32_t mask_words;            /* 64-bit words per node; a sequence has at most 64 * mask_words nodes (later ones are not seen).  0 without a mask */
   int32_t max_nodes;             /* most nodes of a sequence: later ones are not computed */
   int32_t max_length;            /* most committed tokens and nodes of a sequence together; only guides how the work is shared out */
   float scale;                   /* finite, > 0 */
-  int64_t nodes;                 /* rows of q and out, of all sequences; below 2^31 */
+  int64_t nodes;                 /* rows of q and out, of all sequences; nodes * q_heads below 2^31 - 1024 */
   const void *q, *k_cache, *v_cache; /* [nodes, q_heads, head_dim], [n_pages, page_size, kv_heads, head_dim] */
   const int32_t* block_table;    /* [n_seqs, table_columns], rows table_stride apart */
   const int32_t* cached;         /* [n_seqs] */

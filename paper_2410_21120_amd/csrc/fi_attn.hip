@@ -1,6 +1,8 @@
 // Attention over whole prompts (packed sequences) and of drafted trees over a paged cache.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "fi_device.h"
 #include "fi_ops.h"
 
@@ -122,6 +124,15 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
+// One direct load: the active lanes' N bytes at `from` go to at + N * lane (at: the same for the wave).  In assembler, which has no output register: the
+// compiler knows nothing of the load, so it puts no wait of its own before the transposed reads of other tiles; every wait is written out below.
+template <int N>
+__device__ __forceinline__ void load_lds_from(const void* from, uint8_t* at) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)at);
+  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
+}
+
 template <typename T, int DB_>   // DB: blocks of 32 values of a head
 struct Tile {
   static constexpr bool F32 = sizeof(T) == 4;
@@ -160,6 +171,12 @@ struct Tile {
     }
   }
 
+  // Waits for the queries here: a wait that the compiler puts before their first use would stand in the loop over the tiles and hold up its loads.
+  static __device__ __forceinline__ void have_q(u32x4 (&q)[KS]) {
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(q[kk]));
+  }
+
   // Rows [0, 32 KB) of a tile, instruction by instruction: `waves` waves share them, this is number `wave`.  rows(r): where key r's row begins, in pieces.
   template <int KB, int WAVES, typename Rows>
   static __device__ __forceinline__ void load_tile(const T* k, const T* v, uint8_t* tile, int wave, int D, Rows rows) {
@@ -174,8 +191,8 @@ struct Tile {
       rows(u, row, ko, vo);
       const int pk = pos ^ swizzle_k(row), pv = pos ^ swizzle_v(row);
       uint8_t* const at = tile + i * 1024;
-      if (pk * EP < D) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k + ((uint64_t)ko + pk) * EP), (lds_void*)at, 16, 0, 0);
-      if (pv * EP < D) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + ((uint64_t)vo + pv) * EP), (lds_void*)(at + KB * 32 * PB), 16, 0, 0);
+      if (pk * EP < D) load_lds_from<16>(k + ((uint64_t)ko + pk) * EP, at);
+      if (pv * EP < D) load_lds_from<16>(v + ((uint64_t)vo + pv) * EP, at + KB * 32 * PB);
     }
   }
 
@@ -251,10 +268,10 @@ struct Tile {
     }
   }
 
-  // One tile of 32 KB keys.  c: scale * log2(e).  MASKED: bit 8 g + 4 half + i of visible(kb) (half: this lane's) tells whether the lane's query sees key
-  // 32 kb + 8 g + 4 half + i.
-  template <int KB, bool MASKED, typename Visible>
-  static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, Visible visible) {
+  // One tile of 32 KB keys.  c: scale * log2(e).  masked (the same for the wave): bit 8 g + 4 half + i of visible(kb) (half: this lane's) tells whether the
+  // lane's query sees key 32 kb + 8 g + 4 half + i.
+  template <int KB, typename Visible>
+  static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, bool masked, Visible visible) {
     const int half = (threadIdx.x & 63) >> 5;
     f32x16 s[KB];
 #pragma unroll
@@ -265,7 +282,7 @@ struct Tile {
       for (int kk = 0; kk < KS; ++kk)
         s[kb] = product(*reinterpret_cast<const u32x4*>(tile + at.k[kk & 7] + (kk >> 3) * 256 + kb * 32 * PB), q[kk], s[kb]);
     }
-    if constexpr (MASKED) {
+    if (masked) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const uint32_t bits = visible(kb) >> (4 * half);
@@ -359,6 +376,13 @@ __device__ __forceinline__ void meet() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// The same, with the `LATER` last loads still in flight.
+template <int LATER>
+__device__ __forceinline__ void meet_but() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 // The same for what the waves wrote to LDS themselves; loads stay in flight.
 __device__ __forceinline__ void meet_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -422,6 +446,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_til
       vo = key * vs;
     });
   };
+  TL::have_q(q);
   if (tiles > 0) load(0);
   for (int t = 0; t < tiles; ++t) {
     meet();
@@ -431,8 +456,8 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_til
       if (TL::template take_out<KB>(tile, threadIdx.x, 64 * PROMPT_WAVES)) *strange = 1;
       meet_lds();
     }
-    if (t * KEYS + KEYS - 1 <= wave_least) TL::template attend<KB, false>(st, q, tile, at, c, [](int) { return ~0u; });
-    else if (t * KEYS <= wave_most) TL::template attend<KB, true>(st, q, tile, at, c, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
+    if (t * KEYS <= wave_most)
+      TL::template attend<KB>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
   }
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
@@ -479,13 +504,32 @@ __device__ __forceinline__ uint32_t tree_visible(const fi_tree_attention_args& a
   return bits & low_bits(w.keys - key);
 }
 
-// Where key `key` of the sequence is, in pieces from the caches' beginnings (the key head's).
-__device__ __forceinline__ void tree_row(const fi_tree_attention_args& a, const int32_t* table, int key, int ep, uint32_t& ko, uint32_t& vo) {
-  const int column = key / a.page_size, place = key - column * a.page_size;
-  const int page = clamp_int(table[column], 0, a.n_pages - 1);
-  ko = (uint32_t)((page * a.k_strides[0] + place * a.k_strides[1]) / ep);
-  vo = (uint32_t)((page * a.v_strides[0] + place * a.v_strides[1]) / ep);
-}
+// Where keys of a sequence are: page and place by a reciprocal of the page size (floor(2^32 / size): the quotient is right or one too small), offsets in
+// pieces of 16 bytes from the key head's part of the caches (below 2^32: checked on the host).
+struct Pages {
+  const int32_t* table;
+  uint32_t size, inv, most, kp, kt, vp, vt;
+  __device__ __forceinline__ Pages(const fi_tree_attention_args& a, int b, int ep)
+      : table(a.block_table + b * a.table_stride), size(a.page_size), inv(a.page_size == 1 ? ~0u : (uint32_t)((1ull << 32) / (uint32_t)a.page_size)), most(a.n_pages - 1),
+        kp((uint32_t)(a.k_strides[0] / ep)), kt((uint32_t)(a.k_strides[1] / ep)), vp((uint32_t)(a.v_strides[0] / ep)), vt((uint32_t)(a.v_strides[1] / ep)) {}
+  __device__ __forceinline__ uint32_t column(int key, uint32_t& row) const {
+    uint32_t c = __umulhi((uint32_t)key, inv);
+    row = (uint32_t)key - c * size;
+    if (row >= size) { ++c; row -= size; }
+    return c;
+  }
+  struct Place { int32_t page; uint32_t row; };
+  __device__ __forceinline__ Place find(int key) const {   // issues the table's load
+    uint32_t row;
+    const uint32_t c = column(key, row);
+    return Place{table[c], row};
+  }
+  __device__ __forceinline__ void offsets(const Place& p, uint32_t& ko, uint32_t& vo) const {
+    const uint32_t page = p.page < 0 ? 0u : (uint32_t)p.page > most ? most : (uint32_t)p.page;
+    ko = page * kp + p.row * kt;
+    vo = page * vp + p.row * vt;
+  }
+};
 
 // Parts of a row (node, head) in the workspace: `splits` times head_dim sums, then for all rows the maximum and the weights' sum of each.
 __device__ __forceinline__ float* part_sums(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
@@ -497,13 +541,13 @@ __device__ __forceinline__ float* part_stats(const fi_tree_attention_args& a, in
 
 // TL::add_strange for the keys [from, to) of a tree: of those only the tiles that were masked.
 template <typename TL, typename T>
-__device__ __forceinline__ void tree_strange(const fi_tree_attention_args& a, const TreeWork& w, typename TL::State& st, const T* v, const int32_t* table, const uint64_t* words,
+__device__ __forceinline__ void tree_strange(const fi_tree_attention_args& a, const TreeWork& w, typename TL::State& st, const T* v, const Pages& pages, const uint64_t* words,
                                              int node, int from, int to, int tile) {
   const int masked = w.cached / tile * tile;
   TL::add_strange(st, a.head_dim, from > masked ? from : masked, to < w.keys ? to : w.keys,
                   [&](int key) {
                     uint32_t ko, vo;
-                    tree_row(a, table, key, TL::EP, ko, vo);
+                    pages.offsets(pages.find(key), ko, vo);
                     return v + (uint64_t)vo * TL::EP;
                   },
                   [&](int key) { return (tree_visible(a, w, node, words, key) & 1) != 0; });
@@ -529,29 +573,54 @@ __device__ __forceinline__ void finish(const fi_tree_attention_args& a, const Tr
   if (half == 0) *reinterpret_cast<float2*>(part_stats(a, row, splits, w.split)) = make_float2(st.top, total);
 }
 
-constexpr int TREE_WAVES = 4;
-
-// Many rows: the waves have 32 rows each and share the tiles, as for a prompt.
-template <typename T, int DB>
-__global__ void __launch_bounds__(64 * TREE_WAVES, DB <= 4 ? 2 : 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least) {
+// Many rows: the waves have 32 rows each and share the tiles, as for a prompt, but few workgroups are there to hide each other's waiting: three tiles
+// are on their way while one is multiplied, and the pages are asked for (into a ring in LDS, by the same kind of load) three tiles earlier still.
+// A wave's loads come back in order, so its waits count them: L loads a tile and one page request, which comes first.
+template <typename T, int DB, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least) {
   using TL = Tile<T, DB>;
   constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
-  int* const strange = reinterpret_cast<int*>(smem + 2 * BYTES);
+  constexpr int AHEAD = BYTES <= 32768 ? 3 : 1, BUFS = AHEAD + 1, L = 2 * (KEYS / TL::RPI) / WAVES, RING = 8;
+  static_assert(KEYS / TL::RPI % WAVES == 0 && 2 * AHEAD + 2 <= RING, "every wave issues L loads a tile; a ring slot is free again");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[BUFS * BYTES + WAVES * RING * 256 + 16];
+  int* const strange = reinterpret_cast<int*>(smem + BUFS * BYTES + WAVES * RING * 256);
   if (threadIdx.x == 0) *strange = 0;
   const int D = a.head_dim, group = a.q_heads / a.kv_heads;
   const int units = a.n_seqs * a.kv_heads * splits, block = blockIdx.x / units;
   const TreeWork w = tree_work(a, blockIdx.x % units, splits, least);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = w.nodes * group, first = block * 32 * TREE_WAVES;
+  const int rows = w.nodes * group, first = block * 32 * WAVES;
   if (first >= rows || w.split >= w.splits) return;
   const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
   const int all = (w.keys + KEYS - 1) / KEYS, t0 = (int)((int64_t)all * w.split / w.splits), t1 = (int)((int64_t)all * (w.split + 1) / w.splits);
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
   const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
-  const int32_t* const table = a.block_table + w.b * a.table_stride;
+  const Pages pages(a, w.b, TL::EP);
   const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
-  clear_pads<TL, 2 * BYTES>(smem, D, 64 * TREE_WAVES);
+  uint8_t* const ring = smem + BUFS * BYTES + wave * RING * 256;
+  // lane r is asked where row r of a tile is
+  auto key_of = [&](int t) { return t * KEYS + (lane & (KEYS - 1)) < w.keys ? t * KEYS + (lane & (KEYS - 1)) : w.keys - 1; };
+  auto ask = [&](int t) {
+    uint32_t at_row;
+    const int32_t* const entry = pages.table + pages.column(key_of(t < t1 ? t : t1 - 1), at_row);
+    load_lds_from<4>(entry, ring + (t & (RING - 1)) * 256);
+  };
+  auto load = [&](int t) {
+    uint32_t mk, mv;
+    typename Pages::Place place;
+    pages.column(key_of(t), place.row);
+    place.page = *reinterpret_cast<const int32_t*>(ring + (t & (RING - 1)) * 256 + lane * 4);
+    pages.offsets(place, mk, mv);
+    TL::template load_tile<KB, WAVES>(k, v, smem + (t & (BUFS - 1)) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+      ko = __shfl(mk, r);
+      vo = __shfl(mv, r);
+    });
+  };
+  if (t0 < t1) {
+#pragma unroll
+    for (int u = 0; u <= 2 * AHEAD; ++u) ask(t0 + u);
+  }
+  clear_pads<TL, BUFS * BYTES>(smem, D, 64 * WAVES);
   u32x4 q[TL::KS];
   TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, q);
   typename TL::Addr at;
@@ -559,25 +628,28 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, DB <= 4 ? 2 : 1) tree_tile_ke
   typename TL::State st;
   TL::clear(st);
   const float c = a.scale * 1.44269504f;
-  auto load = [&](int t) {
-    TL::template load_tile<KB, TREE_WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
-      tree_row(a, table, t * KEYS + r < w.keys ? t * KEYS + r : w.keys - 1, TL::EP, ko, vo);
-    });
-  };
-  if (t0 < t1) load(t0);
+  arrived();
+  TL::have_q(q);
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (t0 + u < t1) load(t0 + u);
   for (int t = t0; t < t1; ++t) {
-    meet();
-    if (t + 1 < t1) load(t + 1);
-    uint8_t* const tile = smem + (t & 1) * BYTES;
+    ask(t + 2 * AHEAD + 1);
+    // behind tile t: the loads of up to AHEAD - 1 tiles and at least this page request
+    if (AHEAD > 1 && t + 2 < t1) meet_but<(AHEAD - 1) * L + 1>();
+    else if (AHEAD > 1 && t + 1 < t1) meet_but<L + 1>();
+    else meet_but<1>();
+    if (t + AHEAD < t1) load(t + AHEAD);
+    uint8_t* const tile = smem + (t & (BUFS - 1)) * BYTES;
     if ((t + 1) * KEYS > w.cached) {
-      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * TREE_WAVES)) *strange = 1;
+      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * WAVES)) *strange = 1;
       meet_lds();
     }
     if (first + 32 * wave >= rows) continue;
-    if ((t + 1) * KEYS <= w.cached) TL::template attend<KB, false>(st, q, tile, at, c, [](int) { return ~0u; });
-    else TL::template attend<KB, true>(st, q, tile, at, c, [&](int kb) { return tree_visible(a, w, node, words, t * KEYS + 32 * kb); });
+    TL::template attend<KB>(st, q, tile, at, c, (t + 1) * KEYS > w.cached, [&](int kb) { return tree_visible(a, w, node, words, t * KEYS + 32 * kb); });
   }
-  if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, table, words, node, t0 * KEYS, t1 * KEYS, KEYS);
+  arrived();   // (page requests past the end)
+  if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * KEYS, t1 * KEYS, KEYS);
   finish<TL, T>(a, w, splits, st, both_halves(st.total), row < rows, node, head);
 }
 
@@ -604,7 +676,7 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(f
   const int t0 = (int)((int64_t)all * share / total_shares), t1 = (int)((int64_t)all * (share + 1) / total_shares);
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
   const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
-  const int32_t* const table = a.block_table + w.b * a.table_stride;
+  const Pages pages(a, w.b, TL::EP);
   const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
   uint8_t* const tiles = smem + wave * 2 * BYTES;
   clear_pads<TL, 2 * BYTES * WAVES>(smem, D, 64 * WAVES);
@@ -615,26 +687,29 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(f
   typename TL::State st;
   TL::clear(st);
   const float c = a.scale * 1.44269504f;
-  auto load = [&](int t) {   // lane r finds row r, the lanes that load it ask for it
-    const int key = t * 32 + (lane & 31);
+  auto find = [&](int t) { return pages.find(t * 32 + (lane & 31) < w.keys ? t * 32 + (lane & 31) : w.keys - 1); };
+  typename Pages::Place place{0, 0};
+  auto load = [&](int t) {
     uint32_t mk, mv;
-    tree_row(a, table, key < w.keys ? key : w.keys - 1, TL::EP, mk, mv);
+    pages.offsets(place, mk, mv);
     TL::template load_tile<1, 1>(k, v, tiles + (t & 1) * BYTES, 0, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
       ko = __shfl(mk, r);
       vo = __shfl(mv, r);
     });
+    if (t + 1 < t1) place = find(t + 1);
   };
   bool strange = false;
+  if (t0 < t1) place = find(t0);
+  TL::have_q(q);
   if (t0 < t1) load(t0);
   for (int t = t0; t < t1; ++t) {
     arrived();
     if (t + 1 < t1) load(t + 1);
     uint8_t* const tile = tiles + (t & 1) * BYTES;
     if ((t + 1) * 32 > w.cached) strange |= __any(TL::template take_out<1>(tile, lane, 64)) != 0;
-    if ((t + 1) * 32 <= w.cached) TL::template attend<1, false>(st, q, tile, at, c, [](int) { return ~0u; });
-    else TL::template attend<1, true>(st, q, tile, at, c, [&](int) { return tree_visible(a, w, node, words, t * 32); });
+    TL::template attend<1>(st, q, tile, at, c, (t + 1) * 32 > w.cached, [&](int) { return tree_visible(a, w, node, words, t * 32); });
   }
-  if (strange) tree_strange<TL, T>(a, w, st, v, table, words, node, t0 * 32, t1 * 32, 32);
+  if (strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * 32, t1 * 32, 32);
   float total = both_halves(st.total);
   if constexpr (WAVES > 1) {
     // the waves' sums against the largest maximum, added in the order of the waves by wave 0
@@ -675,34 +750,62 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(f
   finish<TL, T>(a, w, splits, st, total, row < rows, node, head);
 }
 
-// Joins the parts of a row, in their order: one wave per (node, head).
-template <typename T>
+// Joins the parts of a row (node, head), in their order and all in flight at once (they come from other dies: a load takes microseconds).  Up to 16
+// parts: a wave per row.  WIDE: a workgroup per row, its waves add a quarter of the parts each, then the waves' sums are added.
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) tree_join_kernel(fi_tree_attention_args a, int splits, int least) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ float sums[3][FI_MAX_HEAD_DIM];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (row >= a.nodes * a.q_heads) return;
-  const int node = (int)(row / a.q_heads), head = (int)(row - (int64_t)node * a.q_heads), lane = threadIdx.x & 63;
+  const int node = (int)(row / a.q_heads), head = (int)(row - (int64_t)node * a.q_heads);
   const int b = find_seq(a.cu_nodes, a.n_seqs, node);
   const TreeWork w = tree_work(a, b * a.kv_heads * splits, splits, least);
   if (w.splits == 1 || node < w.n0 || node - w.n0 >= w.nodes) return;
   const float c = a.scale * 1.44269504f;
-  const float2* const stats = reinterpret_cast<const float2*>(part_stats(a, row, splits, 0));
-  const float* const sums = part_sums(a, row, splits, 0);
-  float top = -INFINITY;
-  for (int s = 0; s < w.splits; ++s) top = fmaxf(top, stats[s].x);
-  const float base = top == -INFINITY ? 0.0f : top;
-  float total = 0.0f, acc[RUN] = {};
-  for (int s = 0; s < w.splits; ++s) {
-    const float f = __builtin_amdgcn_exp2f((stats[s].x - base) * c);
-    total += stats[s].y * f;
+  const float* const parts = part_sums(a, row, splits, 0);
+  // lane s has part s (64 at most): the weights of all parts at once
+  const float2 mine = lane < w.splits ? *reinterpret_cast<const float2*>(part_stats(a, row, splits, lane)) : make_float2(-INFINITY, 0.0f);
+  const int each = WIDE ? (w.splits + 3) / 4 : w.splits, s0 = WIDE ? wave * each : 0;
+  float acc[RUN] = {};
+  auto add = [&](auto many, int from, float weight) {
+    constexpr int N = decltype(many)::value;
+    float x[N][RUN];
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const bool there = s < each && from + s < w.splits && lane + 64 * i < a.head_dim;
+        x[s][i] = there ? parts[(int64_t)(from + s) * a.head_dim + lane + 64 * i] : 0.0f;
+      }
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      const float f = __shfl(weight, from + s < 64 ? from + s : 63);
+#pragma unroll
+      for (int i = 0; i < RUN; ++i)
+        if (s < each && from + s < w.splits) acc[i] += x[s][i] * f;
+    }
+  };
+  const float top = wave_max(mine.x), base = top == -INFINITY ? 0.0f : top;
+  const float weight = lane < w.splits ? __builtin_amdgcn_exp2f((mine.x - base) * c) : 0.0f, total = wave_sum(lane < w.splits ? mine.y * weight : 0.0f);
+  if (each <= 4) add(std::integral_constant<int, 4>{}, s0, weight);
+  else add(std::integral_constant<int, 16>{}, s0, weight);
+  if constexpr (WIDE) {
 #pragma unroll
     for (int i = 0; i < RUN; ++i)
-      if (lane + 64 * i < a.head_dim) acc[i] += sums[(int64_t)s * a.head_dim + lane + 64 * i] * f;
+      if (wave && lane + 64 * i < a.head_dim) sums[wave - 1][lane + 64 * i] = acc[i];
+    __syncthreads();
+    if (wave) return;
   }
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   T* const out = static_cast<T*>(a.out) + node * a.out_strides[0] + head * a.out_strides[1];
 #pragma unroll
-  for (int i = 0; i < RUN; ++i)
-    if (lane + 64 * i < a.head_dim) st(out + lane + 64 * i, acc[i] * inv);
+  for (int i = 0; i < RUN; ++i) {
+    const int d = lane + 64 * i;
+    if (d >= a.head_dim) continue;
+    if constexpr (WIDE) acc[i] = acc[i] + sums[0][d] + sums[1][d] + sums[2][d];
+    st(out + d, acc[i] * inv);
+  }
 }
 
 // Whether every row of a tensor starts on 16 bytes and its last one, counted in 16-byte pieces, has a 32-bit offset.
@@ -750,14 +853,17 @@ bool tree_on_tiles(const fi_tree_attention_args& a) {
 
 // How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 that share
 // them; parts of every sequence's keys, and the least keys of a part.
-struct TreePlan { bool own; int blocks, splits, least; };
+struct TreePlan { bool own; int waves, blocks, splits, least; };
 TreePlan plan_tree(const fi_tree_attention_args& a) {
   TreePlan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
   p.own = rows <= 32;
-  p.blocks = (int)((rows + (p.own ? 31 : 127)) / (p.own ? 32 : 128));
-  p.least = p.own ? 256 : 512;
-  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, want = units > 0 ? (512 + units - 1) / units : 1;
+  p.waves = rows <= 128 || a.head_dim > 128 ? 4 : 8;
+  const int64_t per_block = p.own ? 32 : 32 * p.waves;
+  p.blocks = (int)((rows + per_block - 1) / per_block);
+  p.least = p.own ? 128 : 512;
+  // Histories differ: enough parts that the longest is no more than a quarter of a compute unit's share were all as long.
+  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, want = units > 0 ? (1024 + units - 1) / units : 1;
   const int64_t most = ((int64_t)a.max_length + p.least - 1) / p.least;
   p.splits = (int)(want < most ? want : most);
   p.splits = p.splits < 1 ? 1 : p.splits > 64 ? 64 : p.splits;
@@ -765,10 +871,13 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
 }
 template <typename T, int DB>
 int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
-  const dim3 grid((uint32_t)(a.n_seqs * a.kv_heads * p.splits * p.blocks));
+  const dim3 grid((uint32_t)((int64_t)a.n_seqs * a.kv_heads * p.splits * p.blocks));
   if (p.own) tree_own_kernel<T, DB><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least);
-  else tree_tile_kernel<T, DB><<<grid, 64 * TREE_WAVES, 0, s>>>(a, p.splits, p.least);
-  if (p.splits > 1) tree_join_kernel<T><<<dim3((uint32_t)((a.nodes * a.q_heads + 3) / 4)), 256, 0, s>>>(a, p.splits, p.least);
+  else if (p.waves == 4) tree_tile_kernel<T, DB, 4><<<grid, 256, 0, s>>>(a, p.splits, p.least);
+  else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8><<<grid, 512, 0, s>>>(a, p.splits, p.least);
+  const int64_t all_rows = a.nodes * a.q_heads;
+  if (p.splits > 16) tree_join_kernel<T, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, p.splits, p.least);
+  else if (p.splits > 1) tree_join_kernel<T, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, p.splits, p.least);
   return (int)hipGetLastError();
 }
 template <typename T>

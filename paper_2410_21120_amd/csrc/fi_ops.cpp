@@ -9,7 +9,7 @@
 namespace fi {
 namespace {
 
-constexpr int64_t kRows = 1ll << 31;   // row indices are 32 bits
+constexpr int64_t kRows = (1ll << 31) - 1024;   // row indices are 32 bits, a tile past the last row included
 constexpr int64_t kStride = 1ll << 40; // elements: products of strides and indices stay below 2^63
 
 fi_status done(int e, const char* where) {
