@@ -19,7 +19,7 @@ def stale() -> bool:
     if not os.path.exists(OUT):
         return True
     t = os.path.getmtime(OUT)
-    deps = sources() + [os.path.join(CSRC, "fi_internal.h"), os.path.join(CSRC, "fi_device.h"), os.path.join(CSRC, "fi_ops.h"), os.path.join(HERE, "..", "include", "fusedinf.h")]
+    deps = sources() + [os.path.join(CSRC, "fi_internal.h"), os.path.join(CSRC, "fi_device.h"), os.path.join(CSRC, "fi_ops.h"), os.path.join(CSRC, "fi_ops_device.h"), os.path.join(HERE, "..", "include", "fusedinf.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

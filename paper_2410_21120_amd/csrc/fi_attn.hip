@@ -5,6 +5,7 @@
 
 #include "fi_device.h"
 #include "fi_ops.h"
+#include "fi_ops_device.h"
 
 namespace fi {
 namespace {
@@ -123,15 +124,6 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
 // transposed (16 lanes get columns of 4 x 16 elements), fp32 ones column by column.
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
-
-// One direct load: the active lanes' N bytes at `from` go to at + N * lane (at: the same for the wave).  In assembler, which has no output register: the
-// compiler knows nothing of the load, so it puts no wait of its own before the transposed reads of other tiles; every wait is written out below.
-template <int N>
-__device__ __forceinline__ void load_lds_from(const void* from, uint8_t* at) {
-  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)at);
-  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
-}
 
 template <typename T, int DB_>   // DB: blocks of 32 values of a head
 struct Tile {
@@ -369,26 +361,6 @@ __device__ __forceinline__ float both_halves(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
-// This wave's direct loads have arrived and its reads are done; behind the barrier that holds for all waves.
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void meet() {
-  arrived();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-// The same, with the `LATER` last loads still in flight.
-template <int LATER>
-__device__ __forceinline__ void meet_but() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-// The same for what the waves wrote to LDS themselves; loads stay in flight.
-__device__ __forceinline__ void meet_lds() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 template <typename TL, int BYTES>
 __device__ __forceinline__ void clear_pads(uint8_t* smem, int D, int threads) {   // pieces past D are never loaded: zeros
   if (D == TL::PB / TL::ES) return;

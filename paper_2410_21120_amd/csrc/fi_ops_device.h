@@ -1,0 +1,40 @@
+// Device-side helpers that the decoder operators' kernels share: direct loads to LDS, and the waits for them.
+#pragma once
+
+#include "fi_device.h"
+
+namespace fi {
+
+// One direct load: the active lanes' N bytes (1: a byte, as a dword) at `from` go to at + max(N, 4) * lane (at: the same for the wave).  In assembler, which has
+// no output register: the compiler knows nothing of the load, so it puts no wait of its own before other reads of LDS (it does before transposed ones,
+// whose tile it cannot tell from the one under way); every wait is written out in the kernels.
+template <int N>
+__device__ __forceinline__ void load_lds_from(const void* from, uint8_t* at) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)at);
+  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
+  else if constexpr (N == 4) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(m0), "v"(from) : "memory", "m0");
+}
+
+// This wave's direct loads have arrived and its reads are done; behind the barrier that holds for all waves.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void meet() {
+  arrived();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// The same, with the `LATER` last loads still in flight.
+template <int LATER>
+__device__ __forceinline__ void meet_but() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// The same for what the waves wrote to LDS themselves; loads stay in flight.
+__device__ __forceinline__ void meet_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+}  // namespace fi

@@ -7,8 +7,11 @@
 // (24 bits), so that they enter exactly, too.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "fi_device.h"
 #include "fi_ops.h"
+#include "fi_ops_device.h"
 
 namespace fi {
 namespace {
@@ -104,14 +107,14 @@ struct Run8<float> {
 // A workgroup computes 16 MB rows x 16 NB outputs over a share of the inputs (part `split` of `splits`).  A wave's step is 128 inputs; lane (q, i) = (lane / 16,
 // lane % 16) holds, of output i of a block, VW dwords of weights in each of 4 / VW pieces: inputs 32 VW piece + 8 VW q .. + 8 VW of the step, all in one group,
 // and of row i the same inputs.
-template <typename T, int MB, int NB, int VW>
-__global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_args a, int splits) {
+template <typename T, int NB, int VW>
+__global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_args a, uint32_t inv_group) {
+  constexpr int MB = 1;
   constexpr int PIECES = 4 / VW, TERMS = Run8<T>::TERMS;
   __shared__ f32x4 sums[WAVES][MB * NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i = lane & 15;
-  const int split = blockIdx.x % splits, n0 = (int)(blockIdx.x / splits) * 16 * NB, m0 = blockIdx.y * 16 * MB, K = a.inputs;
-  const int steps = (K + 127) / 128, share = split * WAVES + wave, shares = splits * WAVES;
-  const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
+  const int n0 = (int)blockIdx.x * 16 * NB, m0 = blockIdx.y * 16 * MB, K = a.inputs;
+  const int steps = (K + 127) / 128, s0 = (int)((int64_t)steps * wave / WAVES), s1 = (int)((int64_t)steps * (wave + 1) / WAVES);
   struct Step {
     uint32_t w[NB][PIECES][VW];
     float scale[NB][PIECES];
@@ -124,12 +127,17 @@ __global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_arg
   for (int b = 0; b < NB; ++b) n[b] = n0 + 16 * b + i < a.outputs ? n0 + 16 * b + i : a.outputs - 1;   // (past the last: once more, not stored)
 #pragma unroll
   for (int b = 0; b < MB; ++b) x[b] = static_cast<const T*>(a.x) + (int64_t)(m0 + 16 * b + i) * a.x_stride;
+  // k / group by a reciprocal (floor(2^32 / group): the quotient is right or one too small)
+  auto group_of = [&](int k) {
+    const uint32_t g = __umulhi((uint32_t)k, inv_group);
+    return (int)(g + ((uint32_t)k - g * (uint32_t)a.group >= (uint32_t)a.group ? 1u : 0u));
+  };
   auto load = [&](Step& s, int step) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int k = step * 128 + p * 32 * VW;
       const bool inside = k < K;   // (a step at the end may be short by whole pieces)
-      const int g = inside ? k / a.group : 0;
+      const int g = inside ? group_of(k) : 0;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const uint8_t* const at = a.w + (int64_t)n[b] * a.w_stride + (inside ? (k >> 1) + 4 * VW * q : 0);
@@ -208,10 +216,144 @@ __global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_arg
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (row + e >= a.rows) continue;
-      if (splits > 1) static_cast<float*>(a.workspace)[((int64_t)split * a.rows + row + e) * a.outputs + col] = y[e];
-      else st(static_cast<T*>(a.out) + (row + e) * a.out_stride + col, y[e]);
+      st(static_cast<T*>(a.out) + (row + e) * a.out_stride + col, y[e]);
     }
   }
+}
+
+// More rows (bf16): a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, BUFS - 1 steps
+// ahead: each wave's weights (32 outputs) and their scales and zero points for itself, the rows for all.  Bound by HBM and about as much by the vector unit
+// (a wave's step: 64 operations to unpack 2 KB of weights, 32 to weave the rows, 32 for each group's scale).
+// GP: groups in a step (1: groups of 128 inputs and multiples).  Scales and zero points come in chunks of CS steps, so that a load takes whole pieces of rows
+// (two values of 32 rows at a time cost 7 of 37 us): every step brings S of the instructions that fill the chunk after its own.
+template <int MB, int GP>
+struct Wide {
+  static constexpr int S = GP == 4 ? 2 : 1, CS = GP == 4 ? 2 : 4, GC = GP * CS;         // (a chunk's groups: 8, of single ones 4)
+  static constexpr int W = 0, X = WAVES * 2048, BYTES = X + MB * 4096;                   // a step's slot: weights, rows
+  static constexpr int CHUNK = 32 * GC * 4, CHUNKS = GP == 4 ? 4 : 3;                    // of a wave: as much for scales as for zero points
+  static constexpr int LEFT = 160 * 1024 - CHUNKS * WAVES * 2 * CHUNK;
+  static constexpr int BUFS = LEFT / BYTES < 5 ? LEFT / BYTES : 5, L = 3 + 2 * S;        // L: loads of a wave in a step
+  static_assert(BUFS >= 4 && (BUFS - 2) * L < 64 && (CS - 1 + BUFS - 1) / CS + 1 < CHUNKS, "waits can be counted; the chunk in use is not loaded over");
+};
+template <int MB, int GP>
+__global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_args a, int splits, int per_group) {
+  using Z = Wide<MB, GP>;
+  constexpr int AHEAD = Z::BUFS - 1;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Z::BUFS * Z::BYTES + Z::CHUNKS * WAVES * 2 * Z::CHUNK];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i = lane & 15, K = a.inputs;
+  const int split = blockIdx.x % splits, n0 = (int)(blockIdx.x / splits) * 32 * WAVES + 32 * wave, m0 = blockIdx.y * 16 * MB;
+  const int steps = (K + 127) / 128, s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
+  const int last = a.outputs - 1, groups = K / a.group;
+  // what this lane loads: weights of two outputs (rows past the last: the last once more, not stored), a piece of a row, a scale or two
+  const int piece_w = (lane & 3) ^ (q & 3), row_x = 4 * (wave & (4 * MB - 1)) + q, piece_x = i ^ (row_x & 15);
+  const uint8_t* w[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int n = n0 + 16 * b + (lane >> 2);
+    w[b] = a.w + (int64_t)(n < last ? n : last) * a.w_stride;
+  }
+  const int m = m0 + row_x;
+  const bf16_t* const x = static_cast<const bf16_t*>(a.x) + (int64_t)(m < a.rows ? m : a.rows - 1) * a.x_stride;
+  uint8_t* const own = smem + Z::BUFS * Z::BYTES + wave * Z::CHUNKS * 2 * Z::CHUNK;   // the wave's chunks
+  // instruction `part` of a chunk (64 / GC rows of it), into buffer `to`
+  constexpr int PARTS = Z::GC / 2;
+  auto load_scales = [&](int chunk, int part, int to) {
+    const int n = n0 + part * (64 / Z::GC) + lane / Z::GC, there = n < last ? n : last;
+    const int first = GP > 1 ? chunk * Z::GC : chunk * Z::CS / per_group, g = first + lane % Z::GC < groups ? first + lane % Z::GC : groups - 1;
+    uint8_t* const at = own + to * 2 * Z::CHUNK + part * 256;
+    load_lds_from<4>(a.scales + (int64_t)there * a.scales_stride + g, at);
+    // (without zero points: anything, not looked at)
+    load_lds_from<1>(a.zeros ? a.zeros + (int64_t)there * a.zeros_stride + g : reinterpret_cast<const uint8_t*>(a.scales), at + Z::CHUNK);
+  };
+  int slot = 0, to = (s0 / Z::CS + 1) % Z::CHUNKS;   // of the next step to load: its slot, the buffer of the chunk after its own
+  auto load = [&](int step) {
+    uint8_t* const at = smem + slot * Z::BYTES;
+    const int k = step * 128;   // pieces past the end of the inputs: the step's first once more, not multiplied
+    const int kw = k + 32 * piece_w < K ? k + 32 * piece_w : k, kx = k + 8 * piece_x < K ? k + 8 * piece_x : k;
+#pragma unroll
+    for (int u = 0; u < Z::S; ++u) load_scales(step / Z::CS + 1, (step % Z::CS * Z::S + u) % PARTS, to);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) load_lds_from<16>(w[b] + (kw >> 1), at + Z::W + wave * 2048 + b * 1024);
+    load_lds_from<16>(x + kx, at + Z::X + (wave & (4 * MB - 1)) * 1024);
+    slot = slot + 1 < Z::BUFS ? slot + 1 : 0;
+    if ((step + 1) % Z::CS == 0) to = to + 1 < Z::CHUNKS ? to + 1 : 0;
+  };
+  f32x4 acc[MB][2], dot[MB][2], all[MB];
+#pragma unroll
+  for (int r = 0; r < MB; ++r)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) acc[r][b] = f32x4{0, 0, 0, 0};
+  // the first chunk, and what the steps before the first one of its chunk would have brought of the next
+#pragma unroll
+  for (int u = 0; u < PARTS; ++u) load_scales(s0 / Z::CS, u, s0 / Z::CS % Z::CHUNKS);
+  for (int u = 0; u < s0 % Z::CS * Z::S; ++u) load_scales(s0 / Z::CS + 1, u % PARTS, to);
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (s0 + u < s1) load(s0 + u);
+  int now = 0, from = s0 / Z::CS % Z::CHUNKS;
+  for (int step = s0; step < s1; ++step) {
+    if (step + AHEAD <= s1) meet_but<(AHEAD - 1) * Z::L>();
+    else meet();
+    if (step + AHEAD < s1) load(step + AHEAD);   // into the slot that all waves have read
+    const uint8_t* const at = smem + now * Z::BYTES;
+    now = now + 1 < Z::BUFS ? now + 1 : 0;
+    // the step's first group in its chunk
+    const uint8_t* const scales = own + from * 2 * Z::CHUNK + 4 * (GP > 1 ? step % Z::CS * GP : step / per_group - step / Z::CS * Z::CS / per_group);
+    if ((step + 1) % Z::CS == 0) from = from + 1 < Z::CHUNKS ? from + 1 : 0;
+    auto run = [&](auto which) {   // 32 inputs
+      constexpr int r = decltype(which)::value, per = 4 / GP;   // (groups of 128 and more make whole steps)
+      constexpr bool begins = r % per == 0, ends = r % per == per - 1;
+      const f32x4 none = {0, 0, 0, 0};
+      u32x4 v[MB];
+#pragma unroll
+      for (int t = 0; t < MB; ++t) {
+        v[t] = weave(*reinterpret_cast<const u32x4*>(at + Z::X + (16 * t + i) * 256 + (((4 * r + q) ^ i) << 4)));
+        all[t] = mfma16(v[t], u32x4{ONES, ONES, ONES, ONES}, begins ? none : all[t]);
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t d = *reinterpret_cast<const uint32_t*>(at + Z::W + wave * 2048 + b * 1024 + i * 64 + ((r ^ (i >> 2)) << 4) + q * 4);
+        const u32x4 f = {(d << 3 & 0x00780078u) | 0x41804180u, (d >> 1 & 0x00780078u) | 0x41804180u, (d >> 5 & 0x00780078u) | 0x41804180u, (d >> 9 & 0x00780078u) | 0x41804180u};
+#pragma unroll
+        for (int t = 0; t < MB; ++t) dot[t][b] = mfma16(v[t], f, begins ? none : dot[t][b]);
+      }
+      if constexpr (ends) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint8_t* const entry = scales + ((16 * b + i) * Z::GC + r / per) * 4;
+          const float scale = *reinterpret_cast<const float*>(entry);
+          const float zero = 16.0f + (a.zeros ? (float)*reinterpret_cast<const uint32_t*>(entry + Z::CHUNK) : 8.0f);
+#pragma unroll
+          for (int t = 0; t < MB; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][b][e] += scale * (dot[t][b][e] - zero * all[t][e]);
+        }
+      }
+    };
+    const int left = K - step * 128;   // a last step may be short by whole groups
+    run(std::integral_constant<int, 0>{});
+    if (GP == 1 || left >= 128) {
+      run(std::integral_constant<int, 1>{});
+      run(std::integral_constant<int, 2>{});
+      run(std::integral_constant<int, 3>{});
+    } else {
+      if (left > 32) run(std::integral_constant<int, 1>{});
+      if (left > 64) run(std::integral_constant<int, 2>{});
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < MB; ++t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int col = n0 + 16 * b + i, row = m0 + 16 * t + 4 * q;
+      if (col > last) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (row + e >= a.rows) continue;
+        if (splits > 1) static_cast<float*>(a.workspace)[((int64_t)split * a.rows + row + e) * a.outputs + col] = acc[t][b][e];
+        else st(static_cast<bf16_t*>(a.out) + (row + e) * a.out_stride + col, acc[t][b][e]);
+      }
+    }
 }
 
 // Adds the parts of every result, in their order.
@@ -226,21 +368,25 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
   st(static_cast<T*>(a.out) + row * a.out_stride + (at - (int64_t)row * a.outputs), y);
 }
 
-// Blocks of 16 rows and of 16 outputs that a workgroup computes, parts of the inputs.
-struct Plan { int mb, nb, splits; };
+// How a call is shared out, from its sizes alone (the workspace goes by it): blocks of 16 rows and of 16 outputs that a workgroup computes, parts of the inputs.
+struct Plan { bool wide; int mb, nb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
   Plan p;
-  p.mb = a.rows <= 16 ? 1 : 2;
-  const int64_t blocks = ((int64_t)a.outputs + 15) / 16, passes = ((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb);
-  // A workgroup reads its rows' inputs beside its weights: from a few rows on more outputs share them, and parts of the inputs fill the chip.
-  p.nb = a.rows > 8 || blocks >= 1024 ? 4 : 1;
-  const int64_t groups = (blocks + p.nb - 1) / p.nb * passes, steps = ((int64_t)a.inputs + 127) / 128;
-  int64_t splits = groups > 0 && p.nb > 1 ? (256 + groups - 1) / groups : 1;
-  if (splits > steps / (2 * WAVES)) splits = steps / (2 * WAVES);
-  p.splits = splits < 1 ? 1 : splits > 16 ? 16 : (int)splits;
+  const int64_t blocks = ((int64_t)a.outputs + 15) / 16, steps = ((int64_t)a.inputs + 127) / 128;
+  p.wide = a.dtype == FI_BF16 && a.rows > 8;
+  p.mb = p.wide && a.rows > 16 ? 2 : 1;
+  p.nb = p.wide ? 2 * WAVES : blocks >= 1024 ? 4 : 1;
+  p.splits = 1;
+  if (p.wide) {
+    const int64_t groups = (blocks + p.nb - 1) / p.nb * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
+    int64_t splits = groups > 0 ? (256 + groups - 1) / groups : 1;
+    if (splits > steps / 4) splits = steps / 4;   // (a join costs about as much as four steps)
+    p.splits = splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
+  }
   return p;
 }
 
+// The rows start on 16 bytes, weights on the VW dwords that a lane of the tile kernel takes at once.
 bool on_tiles(const fi_q4_matmul_args& a, int& vw) {
   const int es = elem_size(a.dtype);
   if (reinterpret_cast<uintptr_t>(a.x) % 16 || a.x_stride * es % 16) return false;
@@ -249,25 +395,38 @@ bool on_tiles(const fi_q4_matmul_args& a, int& vw) {
   return w % 4 == 0;
 }
 
-template <typename T, int MB, int NB>
-void launch_tiles(const fi_q4_matmul_args& a, const Plan& p, int vw, hipStream_t s) {
-  const dim3 grid((uint32_t)((((int64_t)a.outputs + 16 * NB - 1) / (16 * NB)) * p.splits), (uint32_t)(((int64_t)a.rows + 16 * MB - 1) / (16 * MB)));
-  if (vw == 4) q4_tile_kernel<T, MB, NB, 4><<<grid, 64 * WAVES, 0, s>>>(a, p.splits);
-  else if (vw == 2) q4_tile_kernel<T, MB, NB, 2><<<grid, 64 * WAVES, 0, s>>>(a, p.splits);
-  else q4_tile_kernel<T, MB, NB, 1><<<grid, 64 * WAVES, 0, s>>>(a, p.splits);
+template <typename T, int NB>
+void launch_tiles(const fi_q4_matmul_args& a, int vw, hipStream_t s) {
+  const dim3 grid((uint32_t)(((int64_t)a.outputs + 16 * NB - 1) / (16 * NB)), (uint32_t)(((int64_t)a.rows + 15) / 16));
+  const uint32_t inv = (uint32_t)((1ull << 32) / (uint32_t)a.group);
+  if (vw == 4) q4_tile_kernel<T, NB, 4><<<grid, 64 * WAVES, 0, s>>>(a, inv);
+  else if (vw == 2) q4_tile_kernel<T, NB, 2><<<grid, 64 * WAVES, 0, s>>>(a, inv);
+  else q4_tile_kernel<T, NB, 1><<<grid, 64 * WAVES, 0, s>>>(a, inv);
+}
+template <int MB>
+void launch_wide(const fi_q4_matmul_args& a, const Plan& p, hipStream_t s) {
+  const dim3 grid((uint32_t)(((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES) * p.splits), (uint32_t)(((int64_t)a.rows + 16 * MB - 1) / (16 * MB)));
+  if (a.group == 32) q4_wide_kernel<MB, 4><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
+  else if (a.group == 64) q4_wide_kernel<MB, 2><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
+  else q4_wide_kernel<MB, 1><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, a.group / 128);
 }
 template <typename T>
 int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
   int vw;
-  if (!on_tiles(a, vw)) {
+  if (a.inputs == 0 || !on_tiles(a, vw)) {
     q4_row_kernel<T><<<dim3((uint32_t)(((int64_t)a.outputs + 3) / 4)), 256, 0, s>>>(a);
     return (int)hipGetLastError();
   }
   const Plan p = plan(a);
-  if (p.nb == 1) launch_tiles<T, 1, 1>(a, p, vw, s);
-  else if (p.mb == 1) launch_tiles<T, 1, 4>(a, p, vw, s);
-  else launch_tiles<T, 2, 4>(a, p, vw, s);
-  if (p.splits > 1) q4_join_kernel<T><<<dim3((uint32_t)(((int64_t)a.rows * a.outputs + 255) / 256)), 256, 0, s>>>(a, p.splits);
+  if (p.wide && (reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.w_stride) % 16 == 0) {
+    if (p.mb == 1) launch_wide<1>(a, p, s);
+    else launch_wide<2>(a, p, s);
+    if (p.splits > 1) q4_join_kernel<T><<<dim3((uint32_t)(((int64_t)a.rows * a.outputs + 255) / 256)), 256, 0, s>>>(a, p.splits);
+  } else if (p.nb == 1) {
+    launch_tiles<T, 1>(a, vw, s);
+  } else {
+    launch_tiles<T, 4>(a, vw, s);
+  }
   return (int)hipGetLastError();
 }
 
