@@ -107,8 +107,8 @@ struct Run8<float> {
 // A workgroup computes 16 MB rows x 16 NB outputs over a share of the inputs (part `split` of `splits`).  A wave's step is 128 inputs; lane (q, i) = (lane / 16,
 // lane % 16) holds, of output i of a block, VW dwords of weights in each of 4 / VW pieces: inputs 32 VW piece + 8 VW q .. + 8 VW of the step, all in one group,
 // and of row i the same inputs.
-template <typename T, int NB, int VW>
-__global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_args a, uint32_t inv_group) {
+template <typename T, int NB, int VW, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES / 4) q4_tile_kernel(fi_q4_matmul_args a, uint32_t inv_group) {
   constexpr int MB = 1;
   constexpr int PIECES = 4 / VW, TERMS = Run8<T>::TERMS;
   __shared__ f32x4 sums[WAVES][MB * NB][64];
@@ -219,6 +219,162 @@ __global__ void __launch_bounds__(64 * WAVES, 2) q4_tile_kernel(fi_q4_matmul_arg
       st(static_cast<T*>(a.out) + (row + e) * a.out_stride + col, y[e]);
     }
   }
+}
+
+// Few rows: the vector unit.  A lane has 32 inputs at a time, 16 bytes of weights of each of OUTS outputs, all in one group; M rows.  The rows' inputs come
+// through LDS, in the order in which the lanes want them, together with their sums (a lane's own 64 bytes of a row, loaded as they lie, touch a
+// line per lane and load: twice the time).  bf16 weights come two by two as above and are multiplied two by two (v_dot2); fp32 rows
+// take them as numbers.  WK waves share an output's inputs, each 2048 of a chunk.
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false); }
+template <typename T, int M, int OUTS, int WK>
+__global__ void __launch_bounds__(256) q4_few_kernel(fi_q4_matmul_args a, uint32_t inv_group) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int NX = F32 ? 2 : 1, CHUNK = WK * 2048;   // 16-byte pieces of eight inputs; inputs of a chunk
+  __shared__ u32x4 xs[M * WK * 4 * NX * 64];           // [row][part][eighth d of a lane's 32][half of it][lane]
+  __shared__ float sums[M * WK * 64];                  // [row][part][lane]
+  __shared__ float parts[4][OUTS * M];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m0 = blockIdx.y * M, K = a.inputs;
+  const int n0 = ((int)blockIdx.x * (4 / WK) + wave / WK) * OUTS, part = wave % WK;
+  const uint8_t* w[OUTS];
+  const float* scales[OUTS];
+  const uint8_t* zeros[OUTS];
+#pragma unroll
+  for (int o = 0; o < OUTS; ++o) {
+    const int64_t n = n0 + o < a.outputs ? n0 + o : a.outputs - 1;   // (past the last: once more, not stored)
+    w[o] = a.w + n * a.w_stride;
+    scales[o] = a.scales + n * a.scales_stride;
+    zeros[o] = a.zeros ? a.zeros + n * a.zeros_stride : nullptr;
+  }
+  const T* x[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) x[m] = static_cast<const T*>(a.x) + (int64_t)(m0 + m < a.rows ? m0 + m : a.rows - 1) * a.x_stride;
+  struct Chunk {
+    u32x4 q[OUTS], x[M][WK][NX];
+    float scale[OUTS];
+    uint32_t zero[OUTS];
+  };
+  auto load = [&](Chunk& c, int from) {   // inputs past the end: zeros, times the row's first weights
+    const int mine = from + (part * 64 + lane) * 32, k = mine < K ? mine : 0;
+    uint32_t g = __umulhi((uint32_t)k, inv_group);   // k / group: right or one too small
+    g += (uint32_t)k - g * (uint32_t)a.group >= (uint32_t)a.group ? 1u : 0u;
+#pragma unroll
+    for (int o = 0; o < OUTS; ++o) {
+      c.q[o] = *reinterpret_cast<const u32x4*>(w[o] + (k >> 1));
+      c.scale[o] = scales[o][g];
+      c.zero[o] = zeros[o] ? zeros[o][g] : 8u;
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int j = 0; j < WK; ++j) {
+        const int kx = from + j * 2048 + tid * 8;
+#pragma unroll
+        for (int u = 0; u < NX; ++u) c.x[m][j][u] = kx < K ? reinterpret_cast<const u32x4*>(x[m] + kx)[u] : u32x4{0, 0, 0, 0};
+      }
+  };
+  float acc[OUTS][M];
+#pragma unroll
+  for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+    for (int m = 0; m < M; ++m) acc[o][m] = 0.0f;
+  Chunk c;
+  load(c, 0);
+  for (int from = 0; from < K; from += CHUNK) {
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int j = 0; j < WK; ++j) {   // thread t has piece t % 4 of lane t / 4
+        float sum = 0.0f;
+        u32x4* const at = xs + (((m * WK + j) * 4 + (tid & 3)) * NX) * 64 + (tid >> 2);
+        if constexpr (F32) {
+#pragma unroll
+          for (int t = 0; t < 8; ++t) sum += __uint_as_float(c.x[m][j][t / 4][t % 4]);
+          at[0] = c.x[m][j][0];
+          at[64] = c.x[m][j][1];
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) sum = dot2(c.x[m][j][0][t], ONES, sum);
+          at[0] = weave(c.x[m][j][0]);
+        }
+        sum += __shfl_xor(sum, 1);
+        sum += __shfl_xor(sum, 2);
+        if ((tid & 3) == 0) sums[(m * WK + j) * 64 + (tid >> 2)] = sum;
+      }
+    __syncthreads();
+    u32x4 q[OUTS];
+    float scale[OUTS], zero[OUTS], dot[OUTS][M];
+#pragma unroll
+    for (int o = 0; o < OUTS; ++o) {
+      q[o] = c.q[o];
+      scale[o] = c.scale[o];
+      zero[o] = (F32 ? 0.0f : 16.0f) + (float)c.zero[o];
+#pragma unroll
+      for (int m = 0; m < M; ++m) dot[o][m] = 0.0f;
+    }
+    if (from + CHUNK < K) load(c, from + CHUNK);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      u32x4 v[M][NX];
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int u = 0; u < NX; ++u) v[m][u] = xs[(((m * WK + part) * 4 + d) * NX + u) * 64 + lane];
+#pragma unroll
+      for (int o = 0; o < OUTS; ++o) {
+        if constexpr (F32) {
+          const uint32_t low = q[o][d] & 0x0F0F0F0Fu, high = q[o][d] >> 4 & 0x0F0F0F0Fu;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const float f = (float)(((t & 1 ? high : low) >> (8 * (t >> 1))) & 255u);
+#pragma unroll
+            for (int m = 0; m < M; ++m) dot[o][m] = __builtin_fmaf(f, __uint_as_float(v[m][t / 4][t % 4]), dot[o][m]);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t f = ((t == 0 ? q[o][d] << 3 : q[o][d] >> (4 * t - 3)) & 0x00780078u) | 0x41804180u;
+#pragma unroll
+            for (int m = 0; m < M; ++m) dot[o][m] = dot2(v[m][0][t], f, dot[o][m]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const float all = sums[(m * WK + part) * 64 + lane];
+#pragma unroll
+      for (int o = 0; o < OUTS; ++o) acc[o][m] += scale[o] * (dot[o][m] - zero[o] * all);
+    }
+    __syncthreads();
+  }
+  // Sums over the lanes: at every step a lane hands half of its values to the lane opposite and takes that one's other half, until it has one.
+  constexpr int V = OUTS * M;
+  float v[V];
+#pragma unroll
+  for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+    for (int m = 0; m < M; ++m) v[o * M + m] = acc[o][m];
+  int h = 32;
+#pragma unroll
+  for (int left = V / 2; left >= 1; left /= 2, h /= 2) {
+    const bool upper = (lane & h) != 0;
+#pragma unroll
+    for (int u = 0; u < left; ++u) {
+      const float keep = upper ? v[u + left] : v[u], give = upper ? v[u] : v[u + left];
+      v[u] = keep + __shfl_xor(give, h);
+    }
+  }
+  for (; h; h /= 2) v[0] += __shfl_xor(v[0], h);
+  if (lane % (64 / V) == 0) parts[wave][lane / (64 / V)] = v[0];
+  __syncthreads();
+  // the WK waves' sums, in their order
+  if (part || lane >= V) return;
+  float y = parts[wave][lane];
+#pragma unroll
+  for (int v = 1; v < WK; ++v) y += parts[wave + v][lane];
+  const int n = n0 + lane / M, m = m0 + lane % M;
+  if (n < a.outputs && m < a.rows) st(static_cast<T*>(a.out) + m * a.out_stride + n, y);
 }
 
 // More rows (bf16): a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, BUFS - 1 steps
@@ -368,19 +524,24 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
   st(static_cast<T*>(a.out) + row * a.out_stride + (at - (int64_t)row * a.outputs), y);
 }
 
-// How a call is shared out, from its sizes alone (the workspace goes by it): blocks of 16 rows and of 16 outputs that a workgroup computes, parts of the inputs.
-struct Plan { bool wide; int mb, nb, splits; };
+// Which kernel takes a call, from its sizes and type alone (the workspace goes by it), where the addresses allow all of them.
+//  FEW:  reads 2048 inputs a step; its time grows with rows x outputs (us, few / tile: 4096 x 1000 inputs x outputs, 1 row 3.2 / 8.4, 4 rows 5.2 / 9.1, 16 rows 7.9 / 11.3;
+//        4096 x 4096, 4 rows 7.8 / 10.0, 8 rows 10.9 / 10.8; 1024 x 16384, 2 rows 8.2 / 8.2, 4 rows 12.6 / 8.4; 512 x 8192, 1 row 4.2 / 3.6).
+//  WIDE: has two launches and about 9 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 14.0 / 11.9, 20 rows 15.4 / 19.4;
+//        1024 x 16384, 8 rows 11.3 / 8.5, 20 rows 13.9 / 15.3; 4096 x 16384, 8 rows 19.4 / 27.4; 16384 x 4096, 16 rows 23 / 38; few there 4 rows 19.6).
+enum Kernel { FEW, TILE, WIDE };
+struct Plan { Kernel kernel; int mb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
-  Plan p;
-  const int64_t blocks = ((int64_t)a.outputs + 15) / 16, steps = ((int64_t)a.inputs + 127) / 128;
-  p.wide = a.dtype == FI_BF16 && a.rows > 8;
-  p.mb = p.wide && a.rows > 16 ? 2 : 1;
-  p.nb = p.wide ? 2 * WAVES : blocks >= 1024 ? 4 : 1;
-  p.splits = 1;
-  if (p.wide) {
-    const int64_t groups = (blocks + p.nb - 1) / p.nb * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
-    int64_t splits = groups > 0 ? (256 + groups - 1) / groups : 1;
-    if (splits > steps / 4) splits = steps / 4;   // (a join costs about as much as four steps)
+  Plan p = {TILE, 1, 1};
+  const int64_t weights = (int64_t)a.inputs * a.outputs, blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
+  if ((a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && (a.rows <= 4 || (a.rows <= 16 && a.outputs < 2048)))) {
+    p.kernel = FEW;
+  } else if (a.dtype == FI_BF16 && a.rows > 4 && weights * ((a.rows + 15) / 16) >= 3 << 23) {
+    p.kernel = WIDE;
+    p.mb = a.rows > 16 ? 2 : 1;
+    const int64_t groups = blocks * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
+    int64_t splits = groups > 0 ? (256 + groups - 1) / groups : 1;   // a workgroup per compute unit
+    if (splits > steps / 4) splits = steps / 4;                       // (a join costs about as much as four steps)
     p.splits = splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
   }
   return p;
@@ -395,13 +556,23 @@ bool on_tiles(const fi_q4_matmul_args& a, int& vw) {
   return w % 4 == 0;
 }
 
-template <typename T, int NB>
+template <typename T, int NB, int W>
 void launch_tiles(const fi_q4_matmul_args& a, int vw, hipStream_t s) {
   const dim3 grid((uint32_t)(((int64_t)a.outputs + 16 * NB - 1) / (16 * NB)), (uint32_t)(((int64_t)a.rows + 15) / 16));
   const uint32_t inv = (uint32_t)((1ull << 32) / (uint32_t)a.group);
-  if (vw == 4) q4_tile_kernel<T, NB, 4><<<grid, 64 * WAVES, 0, s>>>(a, inv);
-  else if (vw == 2) q4_tile_kernel<T, NB, 2><<<grid, 64 * WAVES, 0, s>>>(a, inv);
-  else q4_tile_kernel<T, NB, 1><<<grid, 64 * WAVES, 0, s>>>(a, inv);
+  if (vw == 4) q4_tile_kernel<T, NB, 4, W><<<grid, 64 * W, 0, s>>>(a, inv);
+  else if (vw == 2) q4_tile_kernel<T, NB, 2, W><<<grid, 64 * W, 0, s>>>(a, inv);
+  else q4_tile_kernel<T, NB, 1, W><<<grid, 64 * W, 0, s>>>(a, inv);
+}
+template <typename T, int M>
+void launch_few(const fi_q4_matmul_args& a, hipStream_t s) {
+  const uint32_t inv = (uint32_t)((1ull << 32) / (uint32_t)a.group);
+  const uint32_t passes = (uint32_t)((a.rows + M - 1) / M);
+  auto grid = [&](int outs, int wk) { return dim3((uint32_t)(((int64_t)a.outputs + outs * (4 / wk) - 1) / (outs * (4 / wk))), passes); };
+  // two outputs share what is read of the rows, once that leaves enough waves (4096 x 1000, 4 rows: one 5.2 us, two 6.0; 8 rows, two passes: 7.2, 6.2; 4096 x 4096, 4 rows: 11.9, 7.8)
+  if ((int64_t)a.outputs * passes >= 1536) q4_few_kernel<T, M, 2, 1><<<grid(2, 1), 256, 0, s>>>(a, inv);
+  else if (a.inputs > 2048) q4_few_kernel<T, M, 1, 2><<<grid(1, 2), 256, 0, s>>>(a, inv);
+  else q4_few_kernel<T, M, 1, 1><<<grid(1, 1), 256, 0, s>>>(a, inv);
 }
 template <int MB>
 void launch_wide(const fi_q4_matmul_args& a, const Plan& p, hipStream_t s) {
@@ -418,14 +589,21 @@ int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
     return (int)hipGetLastError();
   }
   const Plan p = plan(a);
-  if (p.wide && (reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.w_stride) % 16 == 0) {
+  const bool aligned = (reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.w_stride) % 16 == 0;
+  if (p.kernel == FEW && aligned) {
+    if (a.rows == 1) launch_few<T, 1>(a, s);
+    else if (a.rows == 2) launch_few<T, 2>(a, s);
+    else launch_few<T, 4>(a, s);
+  } else if (p.kernel == WIDE && aligned) {
     if (p.mb == 1) launch_wide<1>(a, p, s);
     else launch_wide<2>(a, p, s);
     if (p.splits > 1) q4_join_kernel<T><<<dim3((uint32_t)(((int64_t)a.rows * a.outputs + 255) / 256)), 256, 0, s>>>(a, p.splits);
-  } else if (p.nb == 1) {
-    launch_tiles<T, 1>(a, vw, s);
+  } else if (a.outputs >= 16384) {   // (four blocks of outputs share the rows' inputs; fewer leave compute units without work)
+    launch_tiles<T, 4, 8>(a, vw, s);
+  } else if (a.inputs >= 2048) {
+    launch_tiles<T, 1, 16>(a, vw, s);
   } else {
-    launch_tiles<T, 4>(a, vw, s);
+    launch_tiles<T, 1, 8>(a, vw, s);
   }
   return (int)hipGetLastError();
 }
