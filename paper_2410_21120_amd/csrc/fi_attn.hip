@@ -368,11 +368,10 @@ __device__ __forceinline__ void clear_pads(uint8_t* smem, int D, int threads) { 
   __syncthreads();
 }
 
-constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
-
-// A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS.
-template <typename T, int DB>
-__global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_tile_kernel(fi_prompt_attention_args a) {
+// A workgroup has 32 WAVES queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS.
+template <typename T, int DB, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
+  constexpr int ROWS = 32 * WAVES;
   using TL = Tile<T, DB>;
   constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
@@ -382,27 +381,27 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_til
   const int hq = a.q_heads, tile_id = (int)(gridDim.x / hq) - 1 - (int)(blockIdx.x / hq);
   int h = blockIdx.x % hq;
   if (hq % NXCD == 0) h = h % NXCD * (hq / NXCD) + h / NXCD;
-  // sequence b has the tiles from cu_q[b] / 128 + b on: enough for its rows wherever they start
+  // sequence b has the tiles from cu_q[b] / ROWS + b on: enough for its rows wherever they start
   int lo = 0, hi = a.n_seqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (a.cu_q[mid] / PROMPT_ROWS + mid <= tile_id) lo = mid;
+    if (a.cu_q[mid] / ROWS + mid <= tile_id) lo = mid;
     else hi = mid - 1;
   }
   const int b = lo, nq = (int)a.q_tokens, nk = (int)a.k_tokens;
   const int q0 = clamp_int(a.cu_q[b], 0, nq), q1 = clamp_int(a.cu_q[b + 1], q0, nq), k0 = clamp_int(a.cu_k[b], 0, nk), k1 = clamp_int(a.cu_k[b + 1], k0, nk);
-  const int first = (tile_id - (q0 / PROMPT_ROWS + b)) * PROMPT_ROWS, rows = q1 - q0, keys = k1 - k0;
+  const int first = (tile_id - (q0 / ROWS + b)) * ROWS, rows = q1 - q0, keys = k1 - k0;
   if (first < 0 || first >= rows) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1;
   // the last key that a query sees (-1: none), of this lane's, of the wave's first and last, of the workgroup's last
   auto last_of = [&](int r) { return a.causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; };
-  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + PROMPT_ROWS - 1);
+  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + ROWS - 1);
   const int hk = h / (hq / a.kv_heads), D = a.head_dim;
   const T* const k = static_cast<const T*>(a.k) + k0 * a.k_strides[0] + hk * a.k_strides[1];
   const T* const v = static_cast<const T*>(a.v) + k0 * a.v_strides[0] + hk * a.v_strides[1];
   const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
-  clear_pads<TL, 2 * BYTES>(smem, D, 64 * PROMPT_WAVES);
+  clear_pads<TL, 2 * BYTES>(smem, D, 64 * WAVES);
   u32x4 q[TL::KS];
   TL::load_q(static_cast<const T*>(a.q) + (int64_t)(q0 + mine) * a.q_strides[0] + h * a.q_strides[1], D, q);
   typename TL::Addr at;
@@ -412,7 +411,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_til
   const float c = a.scale * 1.44269504f;
   const int tiles = (most + KEYS) / KEYS;   // 0 where nobody sees a key
   auto load = [&](int t) {
-    TL::template load_tile<KB, PROMPT_WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+    TL::template load_tile<KB, WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
       const uint32_t key = (uint32_t)(t * KEYS + r < keys ? t * KEYS + r : keys - 1);   // (rows past the end: the last key once more, unseen)
       ko = key * ks;
       vo = key * vs;
@@ -425,7 +424,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB <= 4 ? 2 : 1) prompt_til
     if (t + 1 < tiles) load(t + 1);
     uint8_t* const tile = smem + (t & 1) * BYTES;
     if (t * KEYS + KEYS - 1 > least) {
-      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * PROMPT_WAVES)) *strange = 1;
+      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * WAVES)) *strange = 1;
       meet_lds();
     }
     if (t * KEYS <= wave_most)
@@ -804,16 +803,21 @@ bool prompt_on_tiles(const fi_prompt_attention_args& a) {
   return a.head_dim * es % 16 == 0 && starts(a.q, a.q_strides, 2, es, 16) && starts(a.out, a.out_strides, 2, es, 4 * es) && pieces(a.k, a.k_strides, n, 2, es) &&
          pieces(a.v, a.v_strides, n, 2, es);
 }
-template <typename T>
-int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
+constexpr int64_t PROMPT_FEW = 1024;
+template <typename T, int WAVES>
+int launch_prompt_waves(const fi_prompt_attention_args& a, hipStream_t s) {
+  const dim3 grid((uint32_t)((a.q_tokens / (32 * WAVES) + a.n_seqs) * a.q_heads));
   switch (blocks_of(a.head_dim)) {
-    case 2: prompt_tile_kernel<T, 2><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    case 3: prompt_tile_kernel<T, 3><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    case 4: prompt_tile_kernel<T, 4><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    default: prompt_tile_kernel<T, 8><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a);
+    case 2: prompt_tile_kernel<T, 2, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
+    case 3: prompt_tile_kernel<T, 3, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
+    case 4: prompt_tile_kernel<T, 4, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
+    default: prompt_tile_kernel<T, 8, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   return (int)hipGetLastError();
+}
+template <typename T>
+int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
+  return (a.q_tokens / 128 + a.n_seqs) * a.q_heads < PROMPT_FEW ? launch_prompt_waves<T, 2>(a, s) : launch_prompt_waves<T, 4>(a, s);
 }
 
 bool tree_on_tiles(const fi_tree_attention_args& a) {

@@ -1,9 +1,10 @@
 // Norms of queries and keys for every head, the position rotation and the write into the paged cache, in one launch.
 //
-// y = rotate(x * w / sqrt(mean(x^2) + eps)).  Every value is read once and written once, so HBM bounds it.  A head's row is held by
-// a group of lanes, in registers from the load to the store: a lane has NP pairs (both halves of each, whichever way pairs are formed) or
-// 2 NP of the values behind the rotated part, so a rotation needs no neighbour and the mean one reduction over the group.  The lane keeps
-// its pairs from head to head of a token: sines and cosines are computed once per token and lane.
+// y = rotate(x * w / sqrt(mean(x^2) + eps)).  Every value is read once and written once, so HBM bounds it, if the vector unit is kept from doing so.  A head's
+// row is held by a group of lanes, in registers from the load to the store: a lane has NP pairs (both halves of each, whichever way pairs are
+// formed) or 2 NP of the values behind the rotated part, so a rotation needs no neighbour, and the mean is one reduction over the group (in the
+// registers' own rotations: 4 additions for 16 lanes).  The lane keeps its pairs from head to head of a token: a wave computes each sine once (one per lane,
+// handed out through LDS), and weight, cosine and sine become two factors per value before the first head.
 #include <hip/hip_runtime.h>
 
 #include "fi_device.h"
@@ -12,56 +13,94 @@
 namespace fi {
 namespace {
 
-constexpr int HEADS = 4;   // rows that a group has in flight
+constexpr int64_t FEWEST_WAVES = 4096;   // waves of a call, where it has rows for them (2187 tokens of 48 fp32 heads of 72: 2048 18 us, 4096 17, 8192 20)
+constexpr int HEADS = 4;                 // rows that a group has in flight (16384 tokens of 48 bf16 heads of 128: one 101 us, two 95, three 88, four 88)
 
 template <typename T, int N>
 struct alignas(sizeof(T) * N) Run { T v[N]; };
 
-// NP pairs per lane; ITEMS runs of them per lane (2: one pair at a time, rows that are not a whole number of longer runs).
-// lanes: lanes of a group, a power of two.  waves: waves that share a token.
-template <typename T, int NP, int ITEMS>
-__global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int lanes, int waves) {
-  const int lane = threadIdx.x & 63, D = a.head_dim, half = a.rot_dim / 2;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int token = (int)(wave / waves), part = (int)(wave - (int64_t)token * waves);
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {   // the value of another lane of the same 16
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+// The sum over aligned groups of `lanes` lanes (a power of two, the same for the wave), in all of them.  Groups of fewer than 16 do not take whole rows of
+// lanes: they exchange.
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+  if (lanes >= 16) {
+    v += rotated<0x128>(v);   // row_ror:8, 4, 2, 1
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    v += rotated<0x121>(v);
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
+  }
+  for (int o = lanes >> 1; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// NP pairs per lane; ITEMS runs of them per lane (2: one pair at a time, rows that are not a whole number of longer runs).  INTER: pair t of a run is its values
+// 2 t and 2 t + 1, else value t of each half.  lanes: of a group, 1 << wave_bits: waves that share a token.
+template <typename T, int NP, int ITEMS, bool INTER>
+__global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int lanes, int wave_bits) {
+  __shared__ float2 turns[4][FI_MAX_HEAD_DIM / 2];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, D = a.head_dim, half = a.rot_dim / 2;
+  const uint32_t wave = blockIdx.x * 4 + w;
+  const int token = (int)(wave >> wave_bits), part = (int)(wave & ((1u << wave_bits) - 1u));
   if (token >= a.tokens) return;
-  const int per_wave = 64 / lanes, group = part * per_wave + lane / lanes, groups = waves * per_wave;
+  const int shift = __builtin_ctz(lanes), group = (part << (6 - shift)) + (lane >> shift), groups = 64 >> shift << wave_bits, in_group = lane & (lanes - 1);
   const int turned = half / NP;                                       // runs of the rotated part
   const int items = turned + (D - a.rot_dim + 2 * NP - 1) / (2 * NP); // and of the whole row
+  for (int pair = lane; pair < half; pair += 64) {
+    int axis = 0, end = a.sections[0];
+#pragma unroll
+    for (int x = 1; x < FI_MAX_AXES; ++x)
+      if (x < a.n_axes) { axis += pair >= end ? 1 : 0; end += a.sections[x]; }
+    // the angle is one fp32 product, as models form it when they are trained
+    float2 t;
+    sincosf((float)a.positions[(int64_t)token * a.n_axes + axis] * a.inv_freq[pair], &t.y, &t.x);
+    turns[w][pair] = t;
+  }
+  asm volatile("" ::: "memory");   // (a wave's writes and reads of LDS are done in order)
 
   int first[ITEMS], second[ITEMS];   // where the lane's values stand in a row; an absent value: -1
-  float c[ITEMS][NP], s[ITEMS][NP], wq[ITEMS][2 * NP], wk[ITEMS][2 * NP];
+  bool turn[ITEMS];
+  // value t of a run becomes r * (own[t] * it + other[t] * its partner), r = 1 / sqrt(..)
+  float own[2][ITEMS][2 * NP], other[2][ITEMS][2 * NP];   // [queries, keys]
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u) {
-    const int item = (lane & (lanes - 1)) + u * lanes;
+    const int item = in_group + u * lanes;
     first[u] = second[u] = -1;
-#pragma unroll
-    for (int t = 0; t < NP; ++t) c[u][t] = 1.0f, s[u][t] = 0.0f;
-    if (item < turned) {
-      first[u] = a.interleaved ? item * 2 * NP : item * NP;
-      second[u] = a.interleaved ? first[u] + NP : half + first[u];
-#pragma unroll
-      for (int t = 0; t < NP; ++t) {
-        const int pair = item * NP + t;
-        int axis = 0, end = a.sections[0];
-#pragma unroll
-        for (int x = 1; x < FI_MAX_AXES; ++x)
-          if (x < a.n_axes) { axis += pair >= end ? 1 : 0; end += a.sections[x]; }
-        // the angle is one fp32 product, as models form it when they are trained
-        sincosf((float)a.positions[(int64_t)token * a.n_axes + axis] * a.inv_freq[pair], &s[u][t], &c[u][t]);
-      }
+    turn[u] = item < turned;
+    if (turn[u]) {
+      first[u] = INTER ? item * 2 * NP : item * NP;
+      second[u] = INTER ? first[u] + NP : half + first[u];
     } else if (item < items) {
       first[u] = a.rot_dim + (item - turned) * 2 * NP;
       second[u] = first[u] + NP < D ? first[u] + NP : -1;   // (an odd row's last value, one pair at a time)
     }
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t) {
-      const int at = (t < NP ? first[u] : second[u]) + t % NP;
-      const bool there = t < NP ? first[u] >= 0 : second[u] >= 0;
-      wq[u][t] = there && a.q_weight ? a.q_weight[at] : 1.0f;
-      wk[u][t] = there && a.k_weight ? a.k_weight[at] : 1.0f;
+    for (int x = 0; x < 2; ++x) {
+      const float* const weight = x ? a.k_weight : a.q_weight;
+      float wt[2 * NP];
+#pragma unroll
+      for (int t = 0; t < 2 * NP; ++t) {
+        const int at = (t < NP ? first[u] : second[u]) + t % NP;
+        const bool there = t < NP ? first[u] >= 0 : second[u] >= 0;
+        wt[t] = there && weight ? weight[at] : 1.0f;
+      }
+#pragma unroll
+      for (int t = 0; t < NP; ++t) {
+        const float2 cs = turn[u] ? turns[w][item * NP + t] : make_float2(1.0f, 0.0f);
+        const int i = INTER ? 2 * t : t, j = INTER ? 2 * t + 1 : NP + t;
+        own[x][u][i] = wt[i] * cs.x;
+        other[x][u][i] = -wt[j] * cs.y;
+        own[x][u][j] = wt[j] * cs.x;
+        other[x][u][j] = wt[i] * cs.y;
+      }
     }
   }
+  const bool rest = a.rot_dim < D;   // some lanes' values are not rotated
   const float inv_d = 1.0f / (float)D;
   // where the token's keys and values go
   int64_t page = 0, place = token;
@@ -69,11 +108,14 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
   if (a.slots) {
     const int64_t slot = a.slots[token];
     keep = slot >= 0 && slot < a.n_slots;
-    page = slot / a.page_size;
-    place = slot - page * a.page_size;
+    if ((uint64_t)slot >> 32 == 0) {
+      page = (uint32_t)slot / (uint32_t)a.page_size;
+      place = (uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size;
+    } else {
+      page = slot / a.page_size;
+      place = slot - page * a.page_size;
+    }
   }
-  // The interleaved order of a run: values 2t, 2t + 1 are pair t; first / second hold its two halves in memory order.
-  const bool inter = a.interleaved != 0;
   const int heads = a.q_heads + a.kv_heads + (a.v ? a.kv_heads : 0);
   for (int h0 = group; h0 < heads; h0 += groups * HEADS) {
     Run<T, NP> x0[HEADS][ITEMS], x1[HEADS][ITEMS];
@@ -101,7 +143,6 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
       T* const row = hk < 0   ? static_cast<T*>(a.q_out) + token * a.q_out_strides[0] + h * a.q_out_strides[1]
                      : hv < 0 ? static_cast<T*>(a.k_out) + page * a.k_out_strides[0] + place * a.k_out_strides[1] + hk * a.k_out_strides[2]
                               : static_cast<T*>(a.v_out) + page * a.v_out_strides[0] + place * a.v_out_strides[1] + hv * a.v_out_strides[2];
-      const bool store = hk < 0 || keep;
       if (hv < 0) {
         float v[ITEMS][2 * NP], sum = 0.0f;
 #pragma unroll
@@ -109,29 +150,34 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
 #pragma unroll
           for (int t = 0; t < 2 * NP; ++t) {
             v[u][t] = ld(t < NP ? &x0[j][u].v[t % NP] : &x1[j][u].v[t % NP]);
-            sum += v[u][t] * v[u][t];
+            sum = __builtin_fmaf(v[u][t], v[u][t], sum);
           }
-        for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor(sum, o);
-        const float r = 1.0f / sqrtf(sum * inv_d + a.eps);
+        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(group_sum(sum, lanes), inv_d, a.eps));
 #pragma unroll
         for (int u = 0; u < ITEMS; ++u) {
           float y[2 * NP];
 #pragma unroll
-          for (int t = 0; t < 2 * NP; ++t) v[u][t] *= r * (hk < 0 ? wq[u][t] : wk[u][t]);
-          const bool turns = (lane & (lanes - 1)) + u * lanes < turned;
-#pragma unroll
-          for (int t = 0; t < NP; ++t) {
-            const int i0 = t, i1 = NP + t, k0 = 2 * t, k1 = 2 * t + 1;
-            const float p = inter ? v[u][k0] : v[u][i0], q = inter ? v[u][k1] : v[u][i1];
-            const float yp = turns ? p * c[u][t] - q * s[u][t] : p, yq = turns ? q * c[u][t] + p * s[u][t] : q;
-            if (inter) { y[k0] = yp; y[k1] = yq; }
-            else { y[i0] = yp; y[i1] = yq; }
+          for (int t = 0; t < 2 * NP; ++t) {
+            const int partner = INTER ? t ^ 1 : (t + NP) % (2 * NP);
+            const float f = hk < 0 ? own[0][u][t] : own[1][u][t], g = hk < 0 ? other[0][u][t] : other[1][u][t];
+            const float mine = v[u][t] * f;
+            y[t] = __builtin_fmaf(v[u][partner], g, mine);
+            if (rest) y[t] = turn[u] ? y[t] : mine;   // (an infinite partner times zero would not vanish)
+            y[t] *= r;
           }
+          if constexpr (sizeof(T) == 2 && NP % 2 == 0) {
 #pragma unroll
-          for (int t = 0; t < 2 * NP; ++t) st(t < NP ? &x0[j][u].v[t % NP] : &x1[j][u].v[t % NP], y[t]);
+            for (int t = 0; t < NP; t += 2) {
+              reinterpret_cast<uint32_t*>(x0[j][u].v)[t / 2] = pack_bf16x2(y[t], y[t + 1]);
+              reinterpret_cast<uint32_t*>(x1[j][u].v)[t / 2] = pack_bf16x2(y[NP + t], y[NP + t + 1]);
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < 2 * NP; ++t) st(t < NP ? &x0[j][u].v[t % NP] : &x1[j][u].v[t % NP], y[t]);
+          }
         }
       }
-      if (!store) continue;
+      if (hk >= 0 && !keep) continue;
 #pragma unroll
       for (int u = 0; u < ITEMS; ++u) {
         if (first[u] >= 0) *reinterpret_cast<Run<T, NP>*>(row + first[u]) = x0[j][u];
@@ -155,12 +201,13 @@ int launch_np(const fi_qk_norm_rope_args& a, hipStream_t s) {
   const int items = a.rot_dim / 2 / NP + (a.head_dim - a.rot_dim + 2 * NP - 1) / (2 * NP);
   int lanes = 1;
   while (lanes * ITEMS < items) lanes *= 2;
-  // A wave per token computes the fewest sines; with few tokens more waves share one, down to a row per group.
+  // A wave per token does the fewest preparations; with few tokens more waves share one, down to a row per group.
   const int heads = a.q_heads + a.kv_heads * (a.v ? 2 : 1), most = (heads + 64 / lanes - 1) / (64 / lanes);
-  int waves = 1;
-  while (waves < most && (int64_t)a.tokens * waves < 8192) waves *= 2;
-  const int64_t blocks = ((int64_t)a.tokens * waves + 3) / 4;
-  rope_kernel<T, NP, ITEMS><<<dim3((uint32_t)blocks), 256, 0, s>>>(a, lanes, waves);
+  int bits = 0;
+  while (1 << bits < most && ((int64_t)a.tokens << bits) < FEWEST_WAVES) ++bits;
+  const dim3 grid((uint32_t)((((int64_t)a.tokens << bits) + 3) / 4));
+  if (a.interleaved) rope_kernel<T, NP, ITEMS, true><<<grid, 256, 0, s>>>(a, lanes, bits);
+  else rope_kernel<T, NP, ITEMS, false><<<grid, 256, 0, s>>>(a, lanes, bits);
   return (int)hipGetLastError();
 }
 
