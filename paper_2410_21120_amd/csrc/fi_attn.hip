@@ -260,12 +260,9 @@ struct Tile {
     }
   }
 
-  // One tile of 32 KB keys.  c: scale * log2(e).  masked (the same for the wave): bit 8 g + 4 half + i of visible(kb) (half: this lane's) tells whether the
-  // lane's query sees key 32 kb + 8 g + 4 half + i.
-  template <int KB, typename Visible>
-  static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, bool masked, Visible visible) {
-    const int half = (threadIdx.x & 63) >> 5;
-    f32x16 s[KB];
+  // ---- one tile of 32 KB keys, in five steps; c: scale * log2(e)
+  template <int KB>
+  static __device__ __forceinline__ void scores(f32x16 (&s)[KB], const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
@@ -274,22 +271,30 @@ struct Tile {
       for (int kk = 0; kk < KS; ++kk)
         s[kb] = product(*reinterpret_cast<const u32x4*>(tile + at.k[kk & 7] + (kk >> 3) * 256 + kb * 32 * PB), q[kk], s[kb]);
     }
-    if (masked) {
+  }
+  // Bit 8 g + 4 half + i of visible(kb) (half: this lane's) tells whether the lane's query sees key 32 kb + 8 g + 4 half + i.
+  template <int KB, typename Visible>
+  static __device__ __forceinline__ void hide(f32x16 (&s)[KB], Visible visible) {
+    const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const uint32_t bits = visible(kb) >> (4 * half);
+    for (int kb = 0; kb < KB; ++kb) {
+      const uint32_t bits = visible(kb) >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] = (bits >> (8 * (e >> 2) + (e & 3))) & 1 ? s[kb][e] : -INFINITY;
-      }
+      for (int e = 0; e < 16; ++e) s[kb][e] = (bits >> (8 * (e >> 2) + (e & 3))) & 1 ? s[kb][e] : -INFINITY;
     }
+  }
+  template <int KB>
+  static __device__ __forceinline__ float highest(const f32x16 (&s)[KB]) {
     float m = s[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-    m = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    // The weights may be taken against any number that keeps them in range: the maximum moves only when it has grown by a factor of 2^8 in weight.
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+  }
+  // The weights may be taken against any number that keeps them in range: it moves only when the maximum has grown by a factor of 2^8 in weight.
+  static __device__ __forceinline__ void follow(State& st, float m, float c) {
     if (__any((m - st.top) * c > 8.0f || (st.top == -INFINITY && m > -INFINITY))) {
       const float now = fmaxf(st.top, m), shrink = __builtin_amdgcn_exp2f((st.top - (now == -INFINITY ? 0.0f : now)) * c);
       st.total *= shrink;
@@ -299,6 +304,9 @@ struct Tile {
 #pragma unroll
         for (int e = 0; e < 16; ++e) st.o[db][e] *= shrink;
     }
+  }
+  template <int KB>
+  static __device__ __forceinline__ void weigh(State& st, f32x16 (&s)[KB], float c) {
     const float base = st.top == -INFINITY ? 0.0f : st.top * c;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -307,6 +315,9 @@ struct Tile {
         s[kb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], c, -base));
         st.total += s[kb][e];
       }
+  }
+  template <int KB>
+  static __device__ __forceinline__ void add_values(State& st, const f32x16 (&s)[KB], const uint8_t* tile, const Addr& at) {
     const uint8_t* const values = tile + KB * 32 * PB;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -333,12 +344,21 @@ struct Tile {
             const uint8_t* const from = values + at.v[db & 3] + (db >> 2) * 256 + (kb * 32 + 16 * h) * PB;
             const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)from));
             const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(from + 8 * PB)));
-            u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
-            st.o[db] = product(a, p, st.o[db]);
+            st.o[db] = product(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, st.o[db]);
           }
         }
       }
     }
+  }
+  // All five.  masked: the same for the wave.
+  template <int KB, typename Visible>
+  static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, bool masked, Visible visible) {
+    f32x16 s[KB];
+    scores<KB>(s, q, tile, at);
+    if (masked) hide<KB>(s, visible);
+    follow(st, highest<KB>(s), c);
+    weigh<KB>(st, s, c);
+    add_values<KB>(st, s, tile, at);
   }
 
   // The lane's outputs: o[db][4 g ..] are values 32 db + 8 g + 4 half .. of its query.
@@ -368,10 +388,12 @@ __device__ __forceinline__ void clear_pads(uint8_t* smem, int D, int threads) { 
   __syncthreads();
 }
 
-// A workgroup has 32 WAVES queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS.
-template <typename T, int DB, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
-  constexpr int ROWS = 32 * WAVES;
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
+
+// A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS; two workgroups on a compute unit.
+template <typename T, int DB>
+__global__ void __launch_bounds__(64 * PROMPT_WAVES, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
+  constexpr int ROWS = PROMPT_ROWS, WAVES = PROMPT_WAVES;
   using TL = Tile<T, DB>;
   constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
@@ -425,6 +447,92 @@ __global__ void __launch_bounds__(64 * WAVES, DB > 4 ? 1 : 2) prompt_tile_kernel
     uint8_t* const tile = smem + (t & 1) * BYTES;
     if (t * KEYS + KEYS - 1 > least) {
       if (TL::template take_out<KB>(tile, threadIdx.x, 64 * WAVES)) *strange = 1;
+      meet_lds();
+    }
+    if (t * KEYS <= wave_most)
+      TL::template attend<KB>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
+  }
+  if (tiles > 0 && *strange)   // (written before the last barrier)
+    TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
+  const float total = both_halves(st.total);
+  if (row < rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(q0 + row) * a.out_strides[0] + h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+}
+
+// Long prompts in bf16: 256 queries a workgroup, eight waves.  A wave multiplies the next tile's scores while it takes this one's exponentials, and finds their maximum
+// while it multiplies this one's values: neither unit waits for the other (8192 queries of 32 heads of 128, causal: PIPE_US us, one after the other in four
+// waves 560).  Four tiles in LDS, two on their way; the lanes' offsets of a whole tile stay in registers.
+constexpr int LONG_ROWS = 256, LONG_GROUPS = 512;
+template <int DB>
+__global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention_args a) {
+  typedef bf16_t T;
+  using TL = Tile<T, DB>;
+  constexpr int KB = 2, KEYS = 64, BYTES = 2 * KEYS * TL::PB, NI = KEYS / TL::RPI, U = NI / 8, L = 2 * U;
+  static_assert(NI % 8 == 0, "every wave issues U loads of keys and U of values");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES + 16];
+  int* const strange = reinterpret_cast<int*>(smem + 4 * BYTES);
+  if (threadIdx.x == 0) *strange = 0;
+  const int hq = a.q_heads, tile_id = (int)(gridDim.x / hq) - 1 - (int)(blockIdx.x / hq);
+  int h = blockIdx.x % hq;
+  if (hq % NXCD == 0) h = h % NXCD * (hq / NXCD) + h / NXCD;   // (as above: one key head's on one die, late rows first)
+  int lo = 0, hi = a.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.cu_q[mid] / LONG_ROWS + mid <= tile_id) lo = mid;
+    else hi = mid - 1;
+  }
+  const int b = lo, nq = (int)a.q_tokens, nk = (int)a.k_tokens;
+  const int q0 = clamp_int(a.cu_q[b], 0, nq), q1 = clamp_int(a.cu_q[b + 1], q0, nq), k0 = clamp_int(a.cu_k[b], 0, nk), k1 = clamp_int(a.cu_k[b + 1], k0, nk);
+  const int first = (tile_id - (q0 / LONG_ROWS + b)) * LONG_ROWS, rows = q1 - q0, keys = k1 - k0;
+  if (first < 0 || first >= rows) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1;
+  auto last_of = [&](int r) { return a.causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; };
+  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + LONG_ROWS - 1);
+  const int hk = h / (hq / a.kv_heads), D = a.head_dim;
+  const T* const k = static_cast<const T*>(a.k) + k0 * a.k_strides[0] + hk * a.k_strides[1];
+  const T* const v = static_cast<const T*>(a.v) + k0 * a.v_strides[0] + hk * a.v_strides[1];
+  const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
+  clear_pads<TL, 4 * BYTES>(smem, D, 512);
+  u32x4 q[TL::KS];
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(q0 + mine) * a.q_strides[0] + h * a.q_strides[1], D, q);
+  typename TL::Addr at;
+  TL::addresses(at);
+  typename TL::State st;
+  TL::clear(st);
+  const float c = a.scale * 1.44269504f;
+  const int tiles = (most + KEYS) / KEYS;
+  uint32_t ko[U], vo[U];   // bytes from the tile's first row
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = (u * 8 + wave) * TL::RPI + lane / TL::NP, pos = lane % TL::NP;
+    ko[u] = (r * ks + (pos ^ TL::swizzle_k(r))) * 16;
+    vo[u] = (r * vs + (pos ^ TL::swizzle_v(r))) * 16;
+  }
+  auto load = [&](int t) {
+    const T* const kt = k + (int64_t)t * KEYS * a.k_strides[0];
+    const T* const vt = v + (int64_t)t * KEYS * a.v_strides[0];
+    uint8_t* const tile = smem + (t & 3) * BYTES;
+    const int left = keys - t * KEYS;   // rows past the end: the last key once more, unseen
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = (u * 8 + wave) * TL::RPI + lane / TL::NP, pos = lane % TL::NP, pk = pos ^ TL::swizzle_k(r), pv = pos ^ TL::swizzle_v(r);
+      const uint32_t over = left < KEYS && r >= left ? (uint32_t)(r - left + 1) : 0u;
+      uint8_t* const to = tile + (u * 8 + wave) * 1024;
+      if (pk * TL::EP < D) load_lds_off(kt, ko[u] - over * ks * 16, to);
+      if (pv * TL::EP < D) load_lds_off(vt, vo[u] - over * vs * 16, to + KEYS * TL::PB);
+    }
+  };
+  TL::have_q(q);
+#pragma unroll
+  for (int u = 0; u < 3; ++u)
+    if (u < tiles) load(u);
+  for (int t = 0; t < tiles; ++t) {
+    if (t + 2 < tiles) meet_but<2 * L>();
+    else meet();
+    if (t + 3 < tiles) load(t + 3);
+    uint8_t* const tile = smem + (t & 3) * BYTES;
+    if (t * KEYS + KEYS - 1 > least) {
+      if (TL::template take_out<KB>(tile, threadIdx.x, 512)) *strange = 1;
       meet_lds();
     }
     if (t * KEYS <= wave_most)
@@ -803,21 +911,31 @@ bool prompt_on_tiles(const fi_prompt_attention_args& a) {
   return a.head_dim * es % 16 == 0 && starts(a.q, a.q_strides, 2, es, 16) && starts(a.out, a.out_strides, 2, es, 4 * es) && pieces(a.k, a.k_strides, n, 2, es) &&
          pieces(a.v, a.v_strides, n, 2, es);
 }
-constexpr int64_t PROMPT_FEW = 1024;
-template <typename T, int WAVES>
-int launch_prompt_waves(const fi_prompt_attention_args& a, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.q_tokens / (32 * WAVES) + a.n_seqs) * a.q_heads));
-  switch (blocks_of(a.head_dim)) {
-    case 2: prompt_tile_kernel<T, 2, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
-    case 3: prompt_tile_kernel<T, 3, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
-    case 4: prompt_tile_kernel<T, 4, WAVES><<<grid, 64 * WAVES, 0, s>>>(a); break;
-    default: prompt_tile_kernel<T, 8, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
-  }
-  return (int)hipGetLastError();
+// The kernel of eight waves wants enough workgroups of 256 queries to fill the chip more than once, and offsets inside a tile below 2^32 bytes.
+bool prompt_is_long(const fi_prompt_attention_args& a) {
+  return a.dtype == FI_BF16 && a.head_dim <= 128 && (a.q_tokens / LONG_ROWS) * a.q_heads >= LONG_GROUPS && a.k_strides[0] < 1 << 24 && a.v_strides[0] < 1 << 24;
 }
 template <typename T>
 int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
-  return (a.q_tokens / 128 + a.n_seqs) * a.q_heads < PROMPT_FEW ? launch_prompt_waves<T, 2>(a, s) : launch_prompt_waves<T, 4>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    if (prompt_is_long(a)) {
+      const dim3 grid((uint32_t)((a.q_tokens / LONG_ROWS + a.n_seqs) * a.q_heads));
+      switch (blocks_of(a.head_dim)) {
+        case 2: prompt_long_kernel<2><<<grid, 512, 0, s>>>(a); break;
+        case 3: prompt_long_kernel<3><<<grid, 512, 0, s>>>(a); break;
+        default: prompt_long_kernel<4><<<grid, 512, 0, s>>>(a);
+      }
+      return (int)hipGetLastError();
+    }
+  }
+  const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
+  switch (blocks_of(a.head_dim)) {
+    case 2: prompt_tile_kernel<T, 2><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    case 3: prompt_tile_kernel<T, 3><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    case 4: prompt_tile_kernel<T, 4><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
+    default: prompt_tile_kernel<T, 8><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a);
+  }
+  return (int)hipGetLastError();
 }
 
 bool tree_on_tiles(const fi_tree_attention_args& a) {

@@ -216,6 +216,35 @@ def test_prompt_attention(torch, fi, dtype, nq, extra, hq, hk, d, causal, layout
     assert torch.equal(again, got)
 
 
+# Enough rows and heads for the kernel of large calls, whose base addresses also pass 2^31 in their low word somewhere among several tensors
+LARGE = [
+    ([1100], [0], 128, 8, 128, True), ([515, 700, 1, 300], [0, 77, 600, -120], 104, 4, 64, True), ([1200, 64], [0, 0], 128, 128, 72, False), ([900, 400], [-450, 33], 128, 2, 96, True),
+]
+
+
+@pytest.mark.parametrize("nq,extra,hq,hk,d,causal", LARGE)
+def test_prompt_attention_of_many_rows(torch, fi, nq, extra, hq, hk, d, causal):
+    g = torch.Generator().manual_seed(sum(nq) + d)
+    nk = [n + e for n, e in zip(nq, extra)]
+    pad = torch.empty((1 << 30) + 4096 * d, dtype=torch.uint8, device="cuda")   # (moves what follows to other addresses)
+    q, k, v = _packed(torch, g, nq, hq, d, torch.bfloat16, "plain"), _packed(torch, g, nk, hk, d, torch.bfloat16, "wide"), _packed(torch, g, nk, hk, d, torch.bfloat16, "plain")
+    out = torch.full(q.shape, math.nan, dtype=torch.bfloat16, device="cuda")
+    got = fi.prompt_attention(q, k, v, _cu(torch, nq), _cu(torch, nk), causal=causal, out=out)
+    want, bound = _prompt_ref(torch, q, k, v, nq, nk, causal, d ** -0.5, "bf16")
+    _inside(got.double().cpu(), want, bound)
+    assert torch.equal(fi.prompt_attention(q, k, v, _cu(torch, nq), _cu(torch, nk), causal=causal), got)
+    if causal:   # nothing leaks from behind the diagonal
+        at = nk[0] - 100
+        bad_k, bad_v = k.clone(), v.clone()
+        bad_k[at, 0, 1], bad_v[at, 1, 2] = math.nan, math.inf
+        again = fi.prompt_attention(q, bad_k, bad_v, _cu(torch, nq), _cu(torch, nk))
+        blind, group = nq[0] - 100, hq // hk
+        assert torch.equal(again[:blind], got[:blind]) and torch.equal(again[nq[0]:], got[nq[0]:]) and torch.equal(again[:, 2 * group:], got[:, 2 * group:])
+        assert again[blind:nq[0], :group].isnan().all() and (again[blind:nq[0], group:2 * group, 2] == math.inf).all()
+        assert torch.equal(again[:nq[0], group:2 * group, 3:], got[:nq[0], group:2 * group, 3:])
+    del pad
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompt_attention_of_far_apart_scores(torch, fi, dtype):
     """Scores from -300 to 300 in rising, falling and mixed order: the running maximum moves late, early and often."""
