@@ -544,28 +544,109 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
   if (row < rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(q0 + row) * a.out_strides[0] + h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
-// What a workgroup of the tree kernels works on: the rows (node, head) of one key head of one sequence, and a share of its keys.
+// What a workgroup of the tree kernels works on: a block of rows (node, head) of one key head of one sequence, and a share of its keys.
 struct TreeWork {
-  int b, hk, cached, keys, n0, nodes, split, splits;
+  int b, hk, cached, keys, n0, nodes, block, split, splits;
 };
 
-// Shares of a sequence's keys: as many as there are, but none below `least` keys.
+// A sequence as the kernels see it: its offsets and lengths clamped to the tensors.
+__device__ __forceinline__ void tree_sequence(const fi_tree_attention_args& a, int b, TreeWork& w) {
+  const int total = (int)a.nodes, places = a.n_pages ? a.page_size * a.table_columns : 0;
+  w.b = b;
+  w.n0 = clamp_int(a.cu_nodes[b], 0, total);
+  w.nodes = clamp_int(a.cu_nodes[b + 1], w.n0, total) - w.n0;
+  if (w.nodes > a.max_nodes) w.nodes = a.max_nodes;
+  w.cached = clamp_int(a.cached[b], 0, places);
+  w.keys = w.nodes < places - w.cached ? w.cached + w.nodes : places;
+}
+// Shares of a sequence's keys: `splits` at most, of `least` keys or more.
 __device__ __forceinline__ int shares(int keys, int splits, int least) { return clamp_int((keys + least - 1) / least, 1, splits); }
 
-__device__ __forceinline__ TreeWork tree_work(const fi_tree_attention_args& a, int id, int splits, int least) {
-  TreeWork w;
-  w.split = id % splits;
-  id /= splits;
-  w.hk = id % a.kv_heads;
-  w.b = id / a.kv_heads;
-  const int total = (int)a.nodes, places = a.n_pages ? a.page_size * a.table_columns : 0;
-  w.n0 = clamp_int(a.cu_nodes[w.b], 0, total);
-  w.nodes = clamp_int(a.cu_nodes[w.b + 1], w.n0, total) - w.n0;
-  if (w.nodes > a.max_nodes) w.nodes = a.max_nodes;
-  w.cached = clamp_int(a.cached[w.b], 0, places);
-  w.keys = w.nodes < places - w.cached ? w.cached + w.nodes : places;
+// The work of a call goes to the workgroups in one of two ways.
+//  Direct: a workgroup for every part that a sequence can have; parts that a shorter one has not end at once, but wait for a compute unit to themselves first.
+//  Counted (few sequences that may have many parts): as many workgroups as run at a time; the first wave of each counts the parts of all sequences and
+//  the parts, of about equal size, are dealt out in turn.  12 sequences, three of them long: direct 43 us, counted 38; one sequence of 1004 keys: 16, 19.
+constexpr int SEQS = 512;   // most sequences that are counted
+struct TreeItems {
+  int ends[SEQS];   // parts of the sequences up to this one
+  int n0[SEQS], nodes[SEQS], cached[SEQS], keys[SEQS];
+  int least, total;
+};
+__device__ __forceinline__ void count_items(const fi_tree_attention_args& a, TreeItems& items, int rows_per_block, int splits, int least, int parts) {
+  const int group = a.q_heads / a.kv_heads, n = a.n_seqs;
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    auto blocks_of = [&](int nodes) { return (nodes * group + rows_per_block - 1) / rows_per_block * a.kv_heads; };
+    float work = 0.0f;
+    for (int b = lane; b < n; b += 64) {
+      TreeWork w;
+      tree_sequence(a, b, w);
+      items.n0[b] = w.n0;
+      items.nodes[b] = w.nodes;
+      items.cached[b] = w.cached;
+      items.keys[b] = w.keys;
+      work += (float)w.keys * (float)blocks_of(w.nodes);
+    }
+    int size = least, total = 0;
+    if (splits > 1) {   // about as many parts as there are workgroups at a time, rather fewer than more
+      const float even = wave_sum(work) / (float)parts;
+      if (even > (float)least) size = even < 1e9f ? ((int)even + 64) / 64 * 64 : 1 << 30;
+      for (int tries = 0; tries < 4; ++tries) {
+        float count = 0.0f;
+        for (int b = lane; b < n; b += 64) count += (float)(blocks_of(items.nodes[b]) * shares(items.keys[b], splits, size));
+        if (wave_sum(count) <= (float)parts || size >= 1 << 29) break;
+        size = (size + size / 4 + 63) / 64 * 64;
+      }
+    }
+    for (int c = 0; c < n; c += 64) {
+      const int b = c + lane;
+      int upto = b < n ? blocks_of(items.nodes[b]) * shares(items.keys[b], splits, size) : 0;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(upto, o);
+        if (lane >= o) upto += up;
+      }
+      if (b < n) items.ends[b] = total + upto;
+      total += __shfl(upto, 63);
+    }
+    if (lane == 0) {
+      items.least = size;
+      items.total = total;
+      if (splits > 1 && blockIdx.x == 0) *static_cast<int*>(a.workspace) = size;   // (for the join)
+    }
+  }
+  __syncthreads();
+}
+// Item number `item`; false behind the last one.
+__device__ __forceinline__ bool tree_item(const fi_tree_attention_args& a, const TreeItems& items, int item, int splits, TreeWork& w) {
+  if (item >= items.total) return false;
+  int lo = 0, hi = a.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (items.ends[mid] > item) hi = mid;
+    else lo = mid + 1;
+  }
+  w.b = lo;
+  w.n0 = items.n0[lo];
+  w.nodes = items.nodes[lo];
+  w.cached = items.cached[lo];
+  w.keys = items.keys[lo];
+  w.splits = shares(w.keys, splits, items.least);
+  int r = lo > 0 ? item - items.ends[lo - 1] : item;
+  w.split = r % w.splits;
+  r /= w.splits;
+  w.hk = r % a.kv_heads;
+  w.block = r / a.kv_heads;
+  return true;
+}
+// Direct: the grid is sequences and blocks, key heads, parts.
+__device__ __forceinline__ bool tree_direct(const fi_tree_attention_args& a, int splits, int least, int blocks, TreeWork& w) {
+  const int b = blocks == 1 ? blockIdx.x : blockIdx.x / blocks;
+  tree_sequence(a, b, w);
+  w.block = blockIdx.x - b * blocks;
+  w.hk = blockIdx.y;
+  w.split = blockIdx.z;
   w.splits = shares(w.keys, splits, least);
-  return w;
+  return w.split < w.splits;
 }
 
 // Which of the 32 keys from `key` on a node (place `node` in its tree, mask row `words`) sees.
@@ -610,12 +691,13 @@ struct Pages {
   }
 };
 
-// Parts of a row (node, head) in the workspace: `splits` times head_dim sums, then for all rows the maximum and the weights' sum of each.
+// The workspace: 16 bytes (the least keys of a part), then parts of a row (node, head): `splits` times head_dim sums, then for all rows the maximum and the
+// weights' sum of each.
 __device__ __forceinline__ float* part_sums(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
-  return static_cast<float*>(a.workspace) + (row * splits + split) * a.head_dim;
+  return static_cast<float*>(a.workspace) + 4 + (row * splits + split) * a.head_dim;
 }
 __device__ __forceinline__ float* part_stats(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
-  return static_cast<float*>(a.workspace) + a.nodes * a.q_heads * splits * a.head_dim + (row * splits + split) * 2;
+  return static_cast<float*>(a.workspace) + 4 + a.nodes * a.q_heads * splits * a.head_dim + (row * splits + split) * 2;
 }
 
 // TL::add_strange for the keys [from, to) of a tree: of those only the tiles that were masked.
@@ -656,20 +738,23 @@ __device__ __forceinline__ void finish(const fi_tree_attention_args& a, const Tr
 // are on their way while one is multiplied, and the pages are asked for (into a ring in LDS, by the same kind of load) three tiles earlier still.
 // A wave's loads come back in order, so its waits count them: L loads a tile and one page request, which comes first.
 template <typename T, int DB, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least) {
+struct Shared {
   using TL = Tile<T, DB>;
-  constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
-  constexpr int AHEAD = BYTES <= 32768 ? 3 : 1, BUFS = AHEAD + 1, L = 2 * (KEYS / TL::RPI) / WAVES, RING = 8;
+  static constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
+  static constexpr int AHEAD = BYTES <= 32768 ? 3 : 1, BUFS = AHEAD + 1, L = 2 * (KEYS / TL::RPI) / WAVES, RING = 8, LDS = BUFS * BYTES + WAVES * RING * 256 + 16;
   static_assert(KEYS / TL::RPI % WAVES == 0 && 2 * AHEAD + 2 <= RING, "every wave issues L loads a tile; a ring slot is free again");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[BUFS * BYTES + WAVES * RING * 256 + 16];
+};
+template <typename T, int DB, int WAVES>
+__device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, const TreeWork& w, int splits, uint8_t* smem) {
+  using TL = Tile<T, DB>;
+  using SH = Shared<T, DB, WAVES>;
+  constexpr int KB = SH::KB, KEYS = SH::KEYS, BYTES = SH::BYTES, AHEAD = SH::AHEAD, BUFS = SH::BUFS, L = SH::L, RING = SH::RING;
   int* const strange = reinterpret_cast<int*>(smem + BUFS * BYTES + WAVES * RING * 256);
   if (threadIdx.x == 0) *strange = 0;
   const int D = a.head_dim, group = a.q_heads / a.kv_heads;
-  const int units = a.n_seqs * a.kv_heads * splits, block = blockIdx.x / units;
-  const TreeWork w = tree_work(a, blockIdx.x % units, splits, least);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = w.nodes * group, first = block * 32 * WAVES;
-  if (first >= rows || w.split >= w.splits) return;
+  const int rows = w.nodes * group, first = w.block * 32 * WAVES;
+  if (first >= rows) return;
   const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
   const int all = (w.keys + KEYS - 1) / KEYS, t0 = (int)((int64_t)all * w.split / w.splits), t1 = (int)((int64_t)all * (w.split + 1) / w.splits);
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
@@ -731,6 +816,21 @@ __global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attent
   if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * KEYS, t1 * KEYS, KEYS);
   finish<TL, T>(a, w, splits, st, both_halves(st.total), row < rows, node, head);
 }
+template <typename T, int DB, int WAVES, bool COUNTED>
+__global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least, int blocks) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Shared<T, DB, WAVES>::LDS];
+  TreeWork w;
+  if constexpr (COUNTED) {
+    __shared__ TreeItems items;
+    count_items(a, items, 32 * WAVES, splits, least, gridDim.x);
+    for (int item = blockIdx.x; tree_item(a, items, item, splits, w); item += gridDim.x) {
+      meet();   // (the item before has been read to the end)
+      tree_tile_work<T, DB, WAVES>(a, w, splits, smem);
+    }
+  } else if (tree_direct(a, splits, least, blocks, w)) {
+    tree_tile_work<T, DB, WAVES>(a, w, splits, smem);
+  }
+}
 
 // Few rows: every wave has the same 32 rows and keys of its own, 32 at a time, loaded by itself (no barriers); joined in LDS at the end.
 template <typename T, int DB>
@@ -738,18 +838,16 @@ struct Own {
   using TL = Tile<T, DB>;
   static constexpr int BYTES = 2 * 32 * TL::PB;                                        // a tile
   static constexpr int WAVES = TL::PB <= 256 ? 4 : TL::PB == 512 ? 2 : 1;              // 128 KB of tiles at most
+  static constexpr int LDS = 2 * BYTES * WAVES + WAVES * 512;
 };
 template <typename T, int DB>
-__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, int splits, int least) {
+__device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, const TreeWork& w, int splits, uint8_t* smem) {
   using TL = Tile<T, DB>;
   constexpr int BYTES = Own<T, DB>::BYTES, WAVES = Own<T, DB>::WAVES;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES * WAVES + WAVES * 512];
   const int D = a.head_dim, group = a.q_heads / a.kv_heads;
-  const int units = a.n_seqs * a.kv_heads * splits, block = blockIdx.x / units;
-  const TreeWork w = tree_work(a, blockIdx.x % units, splits, least);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = w.nodes * group, first = block * 32;
-  if (first >= rows || w.split >= w.splits) return;
+  const int rows = w.nodes * group, first = w.block * 32;
+  if (first >= rows) return;
   const int row = first + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
   const int all = (w.keys + 31) / 32, share = w.split * WAVES + wave, total_shares = w.splits * WAVES;
   const int t0 = (int)((int64_t)all * share / total_shares), t1 = (int)((int64_t)all * (share + 1) / total_shares);
@@ -828,6 +926,21 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(f
   }
   finish<TL, T>(a, w, splits, st, total, row < rows, node, head);
 }
+template <typename T, int DB, bool COUNTED>
+__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, int splits, int least, int blocks) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Own<T, DB>::LDS];
+  TreeWork w;
+  if constexpr (COUNTED) {
+    __shared__ TreeItems items;
+    count_items(a, items, 32, splits, least, gridDim.x);
+    for (int item = blockIdx.x; tree_item(a, items, item, splits, w); item += gridDim.x) {
+      __syncthreads();   // (the item before has been read to the end)
+      tree_own_work<T, DB>(a, w, splits, smem);
+    }
+  } else if (tree_direct(a, splits, least, blocks, w)) {
+    tree_own_work<T, DB>(a, w, splits, smem);
+  }
+}
 
 // Joins the parts of a row (node, head), in their order and all in flight at once (they come from other dies: a load takes microseconds).  Up to 16
 // parts: a wave per row.  WIDE: a workgroup per row, its waves add a quarter of the parts each, then the waves' sums are added.
@@ -839,7 +952,9 @@ __global__ void __launch_bounds__(256) tree_join_kernel(fi_tree_attention_args a
   if (row >= a.nodes * a.q_heads) return;
   const int node = (int)(row / a.q_heads), head = (int)(row - (int64_t)node * a.q_heads);
   const int b = find_seq(a.cu_nodes, a.n_seqs, node);
-  const TreeWork w = tree_work(a, b * a.kv_heads * splits, splits, least);
+  TreeWork w;
+  tree_sequence(a, b, w);
+  w.splits = shares(w.keys, splits, least > 0 ? least : *static_cast<const int*>(a.workspace));
   if (w.splits == 1 || node < w.n0 || node - w.n0 >= w.nodes) return;
   const float c = a.scale * 1.44269504f;
   const float* const parts = part_sums(a, row, splits, 0);
@@ -947,7 +1062,7 @@ bool tree_on_tiles(const fi_tree_attention_args& a) {
 
 // How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 that share
 // them; parts of every sequence's keys, and the least keys of a part.
-struct TreePlan { bool own; int waves, blocks, splits, least; };
+struct TreePlan { bool own, counted; int waves, blocks, splits, least; };
 TreePlan plan_tree(const fi_tree_attention_args& a) {
   TreePlan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
@@ -956,22 +1071,35 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   const int64_t per_block = p.own ? 32 : 32 * p.waves;
   p.blocks = (int)((rows + per_block - 1) / per_block);
   p.least = p.own ? 128 : 512;
-  // Histories differ: enough parts that the longest is no more than a quarter of a compute unit's share were all as long.
-  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, want = units > 0 ? (1024 + units - 1) / units : 1;
-  const int64_t most = ((int64_t)a.max_length + p.least - 1) / p.least;
-  p.splits = (int)(want < most ? want : most);
-  p.splits = p.splits < 1 ? 1 : p.splits > 64 ? 64 : p.splits;
+  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, most = ((int64_t)a.max_length + p.least - 1) / p.least;
+  p.counted = a.n_seqs > 4 && a.n_seqs <= SEQS && units < 512 && most > 1;
+  // Counted: parts enough that one long history among short ones fills the chip, as far as the workspace stays below 64 MB.  Direct: four rounds of workgroups
+  // (4 x 131072 keys: one round 398 us, four 383: the hardware hands them out as units come free).
+  const int64_t room = (64ll << 20) / ((int64_t)a.nodes * a.q_heads * (a.head_dim + 2) * 4 + 1);
+  int64_t splits = units > 0 ? ((p.counted ? 2048 : 1024) + units - 1) / units : 1;
+  if (splits > most) splits = most;
+  if (splits > room && splits * units > 512) splits = room * units > 512 ? room : (512 + units - 1) / units;
+  p.splits = splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
   return p;
 }
 template <typename T, int DB>
 int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)a.n_seqs * a.kv_heads * p.splits * p.blocks));
-  if (p.own) tree_own_kernel<T, DB><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least);
-  else if (p.waves == 4) tree_tile_kernel<T, DB, 4><<<grid, 256, 0, s>>>(a, p.splits, p.least);
-  else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8><<<grid, 512, 0, s>>>(a, p.splits, p.least);
+  using TL = Tile<T, DB>;
+  if (p.counted) {   // as many workgroups as run at a time: by LDS one on a compute unit, of the smallest heads two
+    const dim3 grid(TL::PB == 128 && (p.own || p.waves == 4) ? 512 : 256);
+    if (p.own) tree_own_kernel<T, DB, true><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least, p.blocks);
+    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, true><<<grid, 256, 0, s>>>(a, p.splits, p.least, p.blocks);
+    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, true><<<grid, 512, 0, s>>>(a, p.splits, p.least, p.blocks);
+  } else {
+    const dim3 grid((uint32_t)(a.n_seqs * p.blocks), (uint32_t)a.kv_heads, (uint32_t)p.splits);
+    if (p.own) tree_own_kernel<T, DB, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least, p.blocks);
+    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, false><<<grid, 256, 0, s>>>(a, p.splits, p.least, p.blocks);
+    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, false><<<grid, 512, 0, s>>>(a, p.splits, p.least, p.blocks);
+  }
   const int64_t all_rows = a.nodes * a.q_heads;
-  if (p.splits > 16) tree_join_kernel<T, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, p.splits, p.least);
-  else if (p.splits > 1) tree_join_kernel<T, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, p.splits, p.least);
+  const int least = p.counted ? 0 : p.least;
+  if (p.splits > 16) tree_join_kernel<T, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, p.splits, least);
+  else if (p.splits > 1) tree_join_kernel<T, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, p.splits, least);
   return (int)hipGetLastError();
 }
 template <typename T>
@@ -998,7 +1126,7 @@ int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream) {
 
 uint64_t tree_workspace(const fi_tree_attention_args& a) {
   const TreePlan p = plan_tree(a);
-  return p.splits > 1 ? (uint64_t)a.nodes * a.q_heads * p.splits * (a.head_dim + 2) * 4 : 0;
+  return p.splits > 1 ? (uint64_t)a.nodes * a.q_heads * p.splits * (a.head_dim + 2) * 4 + 16 : 0;
 }
 
 int launch_tree_attention(const fi_tree_attention_args& a, void* stream) {

@@ -310,6 +310,9 @@ TREES = [
     ([5000, 17, 2100], [2, 1, 3], 16, 16, 2, 128, "plain", "tree"),
     ([3000], [100], 32, 8, 8, 64, "plain", None),
     ([40], [9], 8, 6, 3, 21, "odd", "tree"),
+    ([7 * i % 50 for i in range(530)], [i % 3 for i in range(530)], 16, 4, 2, 64, "plain", "tree"),     # more sequences than a workgroup counts
+    ([1500 if i == 40 else i % 9 for i in range(90)], [1 + i % 2 for i in range(90)], 16, 8, 1, 128, "plain", "tree"),   # one long among many short ones
+    ([2500, 3, 0, 700], [40, 33, 1, 2], 16, 8, 1, 128, "plain", "tree"),
 ]
 
 
