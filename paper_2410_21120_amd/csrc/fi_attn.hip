@@ -125,12 +125,12 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
-template <typename T, int DB_>   // DB: blocks of 32 values of a head
+template <typename T, int DB_, int DQ = DB_ * 32>   // DB: blocks of 32 values of a head; DQ: values that its scores are summed over
 struct Tile {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int DB = DB_, ES = sizeof(T), EP = 16 / ES;                          // bytes of an element, elements of a piece
   static constexpr int PB = (DB <= 2 ? 64 : DB <= 4 ? 128 : 256) * ES, NP = PB / 16;    // bytes and pieces of a row in LDS
-  static constexpr int KS = DB * 32 / (2 * EP);                                         // steps of two pieces in a score's sum
+  static constexpr int KS = DQ / (2 * EP);                                             // steps of two pieces in a score's sum
   static constexpr int RPI = 1024 / PB;                                                 // rows that one load instruction brings
   static constexpr int FV = F32 ? 2 : 4;                                                // values' addresses that differ by more than a constant
 
@@ -388,21 +388,21 @@ __device__ __forceinline__ void clear_pads(uint8_t* smem, int D, int threads) { 
   __syncthreads();
 }
 
-constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
-
-// A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS; two workgroups on a compute unit.
-template <typename T, int DB>
-__global__ void __launch_bounds__(64 * PROMPT_WAVES, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
-  constexpr int ROWS = PROMPT_ROWS, WAVES = PROMPT_WAVES;
-  using TL = Tile<T, DB>;
-  constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * BYTES + 16];
-  int* const strange = reinterpret_cast<int*>(smem + 2 * BYTES);   // a masked tile held values that are no finite numbers
-  if (threadIdx.x == 0) *strange = 0;
+// What a workgroup of the prompt kernels works on: ROWS queries of a head.
+struct PromptWork {
+  int h, hk, q0, k0, rows, keys, first;   // the sequence's first query and key, how many it has; the workgroup's first query among them
+  bool causal;
+  // the last key that query r of the sequence sees (-1: none); past the last query: as it
+  __device__ __forceinline__ int last(int r) const { return causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; }
+};
+template <int ROWS>
+__device__ __forceinline__ bool prompt_work(const fi_prompt_attention_args& a, PromptWork& w) {
   // heads of one key head on one die (workgroups go to the eight dies in turn), late rows first: they see most keys
   const int hq = a.q_heads, tile_id = (int)(gridDim.x / hq) - 1 - (int)(blockIdx.x / hq);
-  int h = blockIdx.x % hq;
-  if (hq % NXCD == 0) h = h % NXCD * (hq / NXCD) + h / NXCD;
+  w.h = blockIdx.x % hq;
+  if (hq % NXCD == 0) w.h = w.h % NXCD * (hq / NXCD) + w.h / NXCD;
+  w.hk = w.h / (hq / a.kv_heads);
+  w.causal = a.causal != 0;
   // sequence b has the tiles from cu_q[b] / ROWS + b on: enough for its rows wherever they start
   int lo = 0, hi = a.n_seqs - 1;
   while (lo < hi) {
@@ -410,91 +410,126 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, DB > 4 ? 1 : 2) prompt_tile
     if (a.cu_q[mid] / ROWS + mid <= tile_id) lo = mid;
     else hi = mid - 1;
   }
-  const int b = lo, nq = (int)a.q_tokens, nk = (int)a.k_tokens;
-  const int q0 = clamp_int(a.cu_q[b], 0, nq), q1 = clamp_int(a.cu_q[b + 1], q0, nq), k0 = clamp_int(a.cu_k[b], 0, nk), k1 = clamp_int(a.cu_k[b + 1], k0, nk);
-  const int first = (tile_id - (q0 / ROWS + b)) * ROWS, rows = q1 - q0, keys = k1 - k0;
-  if (first < 0 || first >= rows) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1;
-  // the last key that a query sees (-1: none), of this lane's, of the wave's first and last, of the workgroup's last
-  auto last_of = [&](int r) { return a.causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; };
-  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + ROWS - 1);
-  const int hk = h / (hq / a.kv_heads), D = a.head_dim;
-  const T* const k = static_cast<const T*>(a.k) + k0 * a.k_strides[0] + hk * a.k_strides[1];
-  const T* const v = static_cast<const T*>(a.v) + k0 * a.v_strides[0] + hk * a.v_strides[1];
+  const int nq = (int)a.q_tokens, nk = (int)a.k_tokens;
+  w.q0 = clamp_int(a.cu_q[lo], 0, nq);
+  w.rows = clamp_int(a.cu_q[lo + 1], w.q0, nq) - w.q0;
+  w.k0 = clamp_int(a.cu_k[lo], 0, nk);
+  w.keys = clamp_int(a.cu_k[lo + 1], w.k0, nk) - w.k0;
+  w.first = (tile_id - (w.q0 / ROWS + lo)) * ROWS;
+  return w.first >= 0 && w.first < w.rows;
+}
+
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
+
+// A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS; two workgroups on a compute unit.  GROUPS 2, for calls that
+// do not fill the chip: two groups of four waves have the same queries, one the even tiles, one the odd, joined in LDS at the end (bf16, causal, us with one / two:
+// 512 tokens of 8 heads of 64 12.2 / 10.9, 2048 33 / 25; heads of 128: 512 16.4 / 16.4, 2048 47 / 43; fp32 is bound by its products, 91 / 94).
+template <typename T, int DB, int GROUPS, int DQ>
+__global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
+  constexpr int WAVES = PROMPT_WAVES;
+  using TL = Tile<T, DB, DQ>;
+  constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[GROUPS * 2 * BYTES + 16];
+  int* const strange = reinterpret_cast<int*>(smem + GROUPS * 2 * BYTES);   // a masked tile held values that are no finite numbers
+  if (threadIdx.x == 0) *strange = 0;
+  PromptWork w;
+  if (!prompt_work<PROMPT_ROWS>(a, w)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & (WAVES - 1), group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES;
+  const int row = w.first + 32 * wave + (lane & 31), mine = row < w.rows ? row : w.rows - 1;
+  const int last = w.last(mine), wave_least = w.last(w.first + 32 * wave), least = w.last(w.first), most = w.last(w.first + PROMPT_ROWS - 1);
+  const int wave_most = w.first + 32 * wave < w.rows ? w.last(w.first + 32 * wave + 31) : -1;   // (a wave without queries does nothing)
+  const int D = a.head_dim, keys = w.keys;
+  const T* const k = static_cast<const T*>(a.k) + w.k0 * a.k_strides[0] + w.hk * a.k_strides[1];
+  const T* const v = static_cast<const T*>(a.v) + w.k0 * a.v_strides[0] + w.hk * a.v_strides[1];
   const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
-  clear_pads<TL, 2 * BYTES>(smem, D, 64 * WAVES);
+  clear_pads<TL, GROUPS * 2 * BYTES>(smem, D, 64 * WAVES * GROUPS);
+  uint8_t* const tiles_at = smem + group * 2 * BYTES;
   u32x4 q[TL::KS];
-  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(q0 + mine) * a.q_strides[0] + h * a.q_strides[1], D, q);
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.q0 + mine) * a.q_strides[0] + w.h * a.q_strides[1], D, q);
   typename TL::Addr at;
   TL::addresses(at);
   typename TL::State st;
   TL::clear(st);
   const float c = a.scale * 1.44269504f;
-  const int tiles = (most + KEYS) / KEYS;   // 0 where nobody sees a key
-  auto load = [&](int t) {
-    TL::template load_tile<KB, WAVES>(k, v, smem + (t & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+  const int tiles = (most + KEYS) / KEYS, turns = (tiles + GROUPS - 1) / GROUPS;   // 0 where nobody sees a key
+  auto load = [&](int turn) {
+    const int t = turn * GROUPS + group;
+    if (t >= tiles) return;
+    TL::template load_tile<KB, WAVES>(k, v, tiles_at + (turn & 1) * BYTES, wave, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
       const uint32_t key = (uint32_t)(t * KEYS + r < keys ? t * KEYS + r : keys - 1);   // (rows past the end: the last key once more, unseen)
       ko = key * ks;
       vo = key * vs;
     });
   };
   TL::have_q(q);
-  if (tiles > 0) load(0);
-  for (int t = 0; t < tiles; ++t) {
+  load(0);
+  for (int turn = 0; turn < turns; ++turn) {
     meet();
-    if (t + 1 < tiles) load(t + 1);
-    uint8_t* const tile = smem + (t & 1) * BYTES;
-    if (t * KEYS + KEYS - 1 > least) {
-      if (TL::template take_out<KB>(tile, threadIdx.x, 64 * WAVES)) *strange = 1;
+    if (turn + 1 < turns) load(turn + 1);
+    const int t = turn * GROUPS + group;
+    uint8_t* const tile = tiles_at + (turn & 1) * BYTES;
+    if ((turn + 1) * GROUPS * KEYS - 1 > least) {   // (of the groups' tiles at least one is masked)
+      if (t < tiles && t * KEYS + KEYS - 1 > least && TL::template take_out<KB>(tile, threadIdx.x & (64 * WAVES - 1), 64 * WAVES)) *strange = 1;
       meet_lds();
     }
     if (t * KEYS <= wave_most)
       TL::template attend<KB>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
   }
+  float total = both_halves(st.total);
+  if constexpr (GROUPS == 2) {
+    static_assert(WAVES * DB * 4096 + WAVES * 512 <= 4 * BYTES, "the second group's sums fit the tiles");
+    float* const sums = reinterpret_cast<float*>(smem + wave * DB * 4096) + lane;
+    float2* const stats = reinterpret_cast<float2*>(smem + WAVES * DB * 4096 + wave * 512) + lane;
+    meet();
+    if (group == 1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[(db * 16 + e) * 64] = st.o[db][e];
+      *stats = make_float2(st.top, total);
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float top = fmaxf(st.top, stats->x), base = top == -INFINITY ? 0.0f : top;
+    const float f0 = __builtin_amdgcn_exp2f((st.top - base) * c), f1 = __builtin_amdgcn_exp2f((stats->x - base) * c);
+    total = total * f0 + stats->y * f1;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st.o[db][e] = st.o[db][e] * f0 + sums[(db * 16 + e) * 64] * f1;
+  }
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
-  const float total = both_halves(st.total);
-  if (row < rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(q0 + row) * a.out_strides[0] + h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+  if (row < w.rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
-// Long prompts in bf16: 256 queries a workgroup, eight waves.  A wave multiplies the next tile's scores while it takes this one's exponentials, and finds their maximum
-// while it multiplies this one's values: neither unit waits for the other (8192 queries of 32 heads of 128, causal: PIPE_US us, one after the other in four
-// waves 560).  Four tiles in LDS, two on their way; the lanes' offsets of a whole tile stay in registers.
+// Long prompts in bf16: 256 queries a workgroup, eight waves, four tiles in LDS of which three are on their way; the lanes' offsets of a whole tile stay in registers.
+// 8192 queries of 32 heads of 128, causal: 529 to 548 us (1.0 PFLOP/s of the seen half, three quarters of what a large library product reaches; with four waves and two
+// tiles 565).  What bounds it: the matrix unit is busy 46 % of the time and the vector unit, with the exponentials, 44 %, and they hardly overlap.
+// Tried: the next block's scores among this one's exponentials in a wave 608; the two waves of a unit half a tile apart by barriers 594; wave priorities 543 to 552.
 constexpr int LONG_ROWS = 256, LONG_GROUPS = 512;
-template <int DB>
+template <int DB, int DQ>
 __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention_args a) {
   typedef bf16_t T;
-  using TL = Tile<T, DB>;
+  using TL = Tile<T, DB, DQ>;
   constexpr int KB = 2, KEYS = 64, BYTES = 2 * KEYS * TL::PB, NI = KEYS / TL::RPI, U = NI / 8, L = 2 * U;
   static_assert(NI % 8 == 0, "every wave issues U loads of keys and U of values");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES + 16];
   int* const strange = reinterpret_cast<int*>(smem + 4 * BYTES);
   if (threadIdx.x == 0) *strange = 0;
-  const int hq = a.q_heads, tile_id = (int)(gridDim.x / hq) - 1 - (int)(blockIdx.x / hq);
-  int h = blockIdx.x % hq;
-  if (hq % NXCD == 0) h = h % NXCD * (hq / NXCD) + h / NXCD;   // (as above: one key head's on one die, late rows first)
-  int lo = 0, hi = a.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.cu_q[mid] / LONG_ROWS + mid <= tile_id) lo = mid;
-    else hi = mid - 1;
-  }
-  const int b = lo, nq = (int)a.q_tokens, nk = (int)a.k_tokens;
-  const int q0 = clamp_int(a.cu_q[b], 0, nq), q1 = clamp_int(a.cu_q[b + 1], q0, nq), k0 = clamp_int(a.cu_k[b], 0, nk), k1 = clamp_int(a.cu_k[b + 1], k0, nk);
-  const int first = (tile_id - (q0 / LONG_ROWS + b)) * LONG_ROWS, rows = q1 - q0, keys = k1 - k0;
-  if (first < 0 || first >= rows) return;
+  PromptWork w;
+  if (!prompt_work<LONG_ROWS>(a, w)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1;
-  auto last_of = [&](int r) { return a.causal ? clamp_int(keys - rows + (r < rows ? r : rows - 1), -1, keys - 1) : keys - 1; };
-  const int last = last_of(mine), wave_least = last_of(first + 32 * wave), wave_most = last_of(first + 32 * wave + 31), least = last_of(first), most = last_of(first + LONG_ROWS - 1);
-  const int hk = h / (hq / a.kv_heads), D = a.head_dim;
-  const T* const k = static_cast<const T*>(a.k) + k0 * a.k_strides[0] + hk * a.k_strides[1];
-  const T* const v = static_cast<const T*>(a.v) + k0 * a.v_strides[0] + hk * a.v_strides[1];
+  const int row = w.first + 32 * wave + (lane & 31), mine = row < w.rows ? row : w.rows - 1;
+  const int last = w.last(mine), wave_least = w.last(w.first + 32 * wave), least = w.last(w.first), most = w.last(w.first + LONG_ROWS - 1);
+  const int wave_most = w.first + 32 * wave < w.rows ? w.last(w.first + 32 * wave + 31) : -1;   // (a wave without queries does nothing)
+  const int D = a.head_dim, keys = w.keys;
+  const T* const k = static_cast<const T*>(a.k) + w.k0 * a.k_strides[0] + w.hk * a.k_strides[1];
+  const T* const v = static_cast<const T*>(a.v) + w.k0 * a.v_strides[0] + w.hk * a.v_strides[1];
   const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
   clear_pads<TL, 4 * BYTES>(smem, D, 512);
   u32x4 q[TL::KS];
-  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(q0 + mine) * a.q_strides[0] + h * a.q_strides[1], D, q);
+  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.q0 + mine) * a.q_strides[0] + w.h * a.q_strides[1], D, q);
   typename TL::Addr at;
   TL::addresses(at);
   typename TL::State st;
@@ -541,7 +576,7 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
   const float total = both_halves(st.total);
-  if (row < rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(q0 + row) * a.out_strides[0] + h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+  if (row < w.rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
 // What a workgroup of the tree kernels works on: a block of rows (node, head) of one key head of one sequence, and a share of its keys.
@@ -1030,26 +1065,35 @@ bool prompt_on_tiles(const fi_prompt_attention_args& a) {
 bool prompt_is_long(const fi_prompt_attention_args& a) {
   return a.dtype == FI_BF16 && a.head_dim <= 128 && (a.q_tokens / LONG_ROWS) * a.q_heads >= LONG_GROUPS && a.k_strides[0] < 1 << 24 && a.v_strides[0] < 1 << 24;
 }
+template <typename T, int DB, int DQ>
+void prompt_waves(const fi_prompt_attention_args& a, dim3 grid, bool two, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && DB <= 4) {
+    if (two) return (void)(prompt_tile_kernel<T, DB, 2, DQ><<<grid, 128 * PROMPT_WAVES, 0, s>>>(a));
+  }
+  prompt_tile_kernel<T, DB, 1, DQ><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a);
+}
+// (heads of 65 to 80 values: scores without the steps that heads of 96 take; 4 images of up to 729 fp32 queries, 16 heads of 72: 91 us, 82)
 template <typename T>
 int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
+  const int db = blocks_of(a.head_dim);
   if constexpr (sizeof(T) == 2) {
     if (prompt_is_long(a)) {
       const dim3 grid((uint32_t)((a.q_tokens / LONG_ROWS + a.n_seqs) * a.q_heads));
-      switch (blocks_of(a.head_dim)) {
-        case 2: prompt_long_kernel<2><<<grid, 512, 0, s>>>(a); break;
-        case 3: prompt_long_kernel<3><<<grid, 512, 0, s>>>(a); break;
-        default: prompt_long_kernel<4><<<grid, 512, 0, s>>>(a);
-      }
+      if (db == 2) prompt_long_kernel<2, 64><<<grid, 512, 0, s>>>(a);
+      else if (db == 3 && a.head_dim <= 80) prompt_long_kernel<3, 80><<<grid, 512, 0, s>>>(a);
+      else if (db == 3) prompt_long_kernel<3, 96><<<grid, 512, 0, s>>>(a);
+      else prompt_long_kernel<4, 128><<<grid, 512, 0, s>>>(a);
       return (int)hipGetLastError();
     }
   }
+  // two groups where there is a workgroup or so per compute unit, and a walk is long
   const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
-  switch (blocks_of(a.head_dim)) {
-    case 2: prompt_tile_kernel<T, 2><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    case 3: prompt_tile_kernel<T, 3><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    case 4: prompt_tile_kernel<T, 4><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a); break;
-    default: prompt_tile_kernel<T, 8><<<grid, 64 * PROMPT_WAVES, 0, s>>>(a);
-  }
+  const bool two = (int64_t)grid.x < 512 && a.k_tokens >= 512 * (int64_t)a.n_seqs;
+  if (db == 2) prompt_waves<T, 2, 64>(a, grid, two, s);
+  else if (db == 3 && a.head_dim <= 80) prompt_waves<T, 3, 80>(a, grid, two, s);
+  else if (db == 3) prompt_waves<T, 3, 96>(a, grid, two, s);
+  else if (db == 4) prompt_waves<T, 4, 128>(a, grid, two, s);
+  else prompt_waves<T, 8, 256>(a, grid, two, s);
   return (int)hipGetLastError();
 }
 
