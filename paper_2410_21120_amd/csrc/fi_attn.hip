@@ -553,8 +553,8 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
       const int r = (u * 8 + wave) * TL::RPI + lane / TL::NP, pos = lane % TL::NP, pk = pos ^ TL::swizzle_k(r), pv = pos ^ TL::swizzle_v(r);
       const uint32_t over = left < KEYS && r >= left ? (uint32_t)(r - left + 1) : 0u;
       uint8_t* const to = tile + (u * 8 + wave) * 1024;
-      if (pk * TL::EP < D) load_lds_off(kt, ko[u] - over * ks * 16, to);
-      if (pv * TL::EP < D) load_lds_off(vt, vo[u] - over * vs * 16, to + KEYS * TL::PB);
+      if (pk * TL::EP < D) load_lds_off<16>(kt, ko[u] - over * ks * 16, to);
+      if (pv * TL::EP < D) load_lds_off<16>(vt, vo[u] - over * vs * 16, to + KEYS * TL::PB);
     }
   };
   TL::have_q(q);

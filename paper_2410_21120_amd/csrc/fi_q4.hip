@@ -377,151 +377,230 @@ __global__ void __launch_bounds__(256) q4_few_kernel(fi_q4_matmul_args a, uint32
   if (n < a.outputs && m < a.rows) st(static_cast<T*>(a.out) + m * a.out_stride + n, y);
 }
 
-// More rows (bf16): a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, BUFS - 1 steps
-// ahead: each wave's weights (32 outputs) and their scales and zero points for itself, the rows for all.  Bound by HBM and about as much by the vector unit
-// (a wave's step: 64 operations to unpack 2 KB of weights, 32 to weave the rows, 32 for each group's scale).
-// GP: groups in a step (1: groups of 128 inputs and multiples).  Scales and zero points come in chunks of CS steps, so that a load takes whole pieces of rows
+// More rows (bf16): a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, AHEAD
+// steps ahead: each wave's weights (32 outputs) and their scales and zero points for itself, of the rows a share each, which it weaves and sums by groups a step
+// before they are used.  What the zero points take off, scale * (16 + zero) * (sum of the group's x), is a product of its own over the groups: an fp32 matrix
+// instruction takes four of them, once a chunk.  The vector unit bounds it about as much as HBM (64 operations a step to unpack 2 KB of weights, 16 MB for the groups' scales).
+// GP: groups in a step (1: groups of 128 inputs and multiples).  Scales and zero points come in chunks of CS steps, so that a load takes pieces of rows
 // (two values of 32 rows at a time cost 7 of 37 us): every step brings S of the instructions that fill the chunk after its own.
 template <int MB, int GP>
 struct Wide {
-  static constexpr int S = GP == 4 ? 2 : 1, CS = GP == 4 ? 2 : 4, GC = GP * CS;         // (a chunk's groups: 8, of single ones 4)
-  static constexpr int W = 0, X = WAVES * 2048, BYTES = X + MB * 4096;                   // a step's slot: weights, rows
-  static constexpr int CHUNK = 32 * GC * 4, CHUNKS = GP == 4 ? 4 : 3;                    // of a wave: as much for scales as for zero points
-  static constexpr int LEFT = 160 * 1024 - CHUNKS * WAVES * 2 * CHUNK;
-  static constexpr int BUFS = LEFT / BYTES < 5 ? LEFT / BYTES : 5, L = 3 + 2 * S;        // L: loads of a wave in a step
-  static_assert(BUFS >= 4 && (BUFS - 2) * L < 64 && (CS - 1 + BUFS - 1) / CS + 1 < CHUNKS, "waits can be counted; the chunk in use is not loaded over");
+  static constexpr int S = GP == 4 ? 2 : 1, CS = GP == 4 ? 1 : 4, GC = GP * CS;            // (a chunk's groups: 8 of 64 inputs, else 4)
+  static constexpr int CHUNK = 32 * GC * 4, CHUNKS = GP == 4 ? 6 : 3;                       // of a wave: as much for scales as for zero points
+  static constexpr int WSTEP = WAVES * 2048, XSTEP = MB * 4096, SUMS = GC * 16 * MB * 4;    // a step's weights, its rows; a chunk's sums of the rows
+  static constexpr int LEFT = 160 * 1024 - CHUNKS * WAVES * 2 * CHUNK - 2 * XSTEP - 2 * SUMS + XSTEP, MOST = LEFT / (WSTEP + XSTEP);
+  static constexpr int BUFS = MOST < 5 ? MOST : 5, AHEAD = BUFS - 1, L = 3 + 2 * S;         // L: loads of a wave in a step, its rows' first
+  // in LDS: AHEAD + 1 steps of weights, AHEAD of rows as they come, two of woven rows, two chunks' sums, the waves' chunks
+  static constexpr int X = BUFS * WSTEP, WOVEN = X + AHEAD * XSTEP, ALL = WOVEN + 2 * XSTEP, SCALES = ALL + 2 * SUMS, BYTES = SCALES + CHUNKS * WAVES * 2 * CHUNK;
+  static_assert(BUFS >= 4 && AHEAD * L < 64 && (CS - 1 + AHEAD) / CS + 1 < CHUNKS, "waits can be counted; the chunk in use is not loaded over");
 };
+template <int CTRL>
+__device__ __forceinline__ float swapped(float v) {   // of another lane of the row of 16
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
 template <int MB, int GP>
 __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_args a, int splits, int per_group) {
   using Z = Wide<MB, GP>;
-  constexpr int AHEAD = Z::BUFS - 1;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[Z::BUFS * Z::BYTES + Z::CHUNKS * WAVES * 2 * Z::CHUNK];
+  constexpr int AHEAD = Z::AHEAD, GC = Z::GC, CS = Z::CS;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Z::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i = lane & 15, K = a.inputs;
   const int split = blockIdx.x % splits, n0 = (int)(blockIdx.x / splits) * 32 * WAVES + 32 * wave, m0 = blockIdx.y * 16 * MB;
-  const int steps = (K + 127) / 128, s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
+  const uint32_t steps = (K + 127) / 128, s0 = (uint32_t)((uint64_t)steps * split / splits), s1 = (uint32_t)((uint64_t)steps * (split + 1) / splits);
   const int last = a.outputs - 1, groups = K / a.group;
-  // what this lane loads: weights of two outputs (rows past the last: the last once more, not stored), a piece of a row, a scale or two
-  const int piece_w = (lane & 3) ^ (q & 3), row_x = 4 * (wave & (4 * MB - 1)) + q, piece_x = i ^ (row_x & 15);
-  const uint8_t* w[2];
+  // What this lane loads: weights of two outputs (past the last one: the last once more, not stored), a piece of a row, a scale and a zero point or two.  All
+  // from bases that the wave shares (the strides are below 2^24 elements).
+  const int first_n = n0 < last ? n0 : last, left_n = last - first_n;
+  const int piece_w = (lane & 3) ^ (q & 3), share = wave & (4 * MB - 1), row_x = 4 * share + q, piece_x = i ^ (row_x & 15);
+  const uint8_t* const w = a.w + (int64_t)first_n * a.w_stride;
+  const float* const scale0 = a.scales + (int64_t)first_n * a.scales_stride;
+  const uint8_t* const zero0 = a.zeros ? a.zeros + (int64_t)first_n * a.zeros_stride : nullptr;
+  uint32_t off_w[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    const int n = n0 + 16 * b + (lane >> 2);
-    w[b] = a.w + (int64_t)(n < last ? n : last) * a.w_stride;
+    const int n = 16 * b + (lane >> 2);
+    off_w[b] = (uint32_t)(n < left_n ? n : left_n) * (uint32_t)a.w_stride + 16 * piece_w;
   }
-  const int m = m0 + row_x;
-  const bf16_t* const x = static_cast<const bf16_t*>(a.x) + (int64_t)(m < a.rows ? m : a.rows - 1) * a.x_stride;
-  uint8_t* const own = smem + Z::BUFS * Z::BYTES + wave * Z::CHUNKS * 2 * Z::CHUNK;   // the wave's chunks
+  const int left_m = a.rows - 1 - m0;
+  const bf16_t* const x = static_cast<const bf16_t*>(a.x) + (int64_t)m0 * a.x_stride;
+  const uint32_t off_x = (uint32_t)(row_x < left_m ? row_x : left_m) * (uint32_t)a.x_stride * 2 + 16 * piece_x;
+  uint8_t* const own = smem + Z::SCALES + wave * Z::CHUNKS * 2 * Z::CHUNK;   // the wave's chunks
   // instruction `part` of a chunk (64 / GC rows of it), into buffer `to`
-  constexpr int PARTS = Z::GC / 2;
-  auto load_scales = [&](int chunk, int part, int to) {
-    const int n = n0 + part * (64 / Z::GC) + lane / Z::GC, there = n < last ? n : last;
-    const int first = GP > 1 ? chunk * Z::GC : chunk * Z::CS / per_group, g = first + lane % Z::GC < groups ? first + lane % Z::GC : groups - 1;
+  constexpr int PARTS = GC / 2;
+  auto load_scales = [&](uint32_t chunk, uint32_t part, uint32_t to) {
+    const int row = (int)part * (64 / GC) + lane / GC, n = row < left_n ? row : left_n;
+    const int first = (int)(GP > 1 ? chunk * GC : chunk * CS / (uint32_t)per_group), g = first + lane % GC < groups ? first + lane % GC : groups - 1;
     uint8_t* const at = own + to * 2 * Z::CHUNK + part * 256;
-    load_lds_from<4>(a.scales + (int64_t)there * a.scales_stride + g, at);
-    // (without zero points: anything, not looked at)
-    load_lds_from<1>(a.zeros ? a.zeros + (int64_t)there * a.zeros_stride + g : reinterpret_cast<const uint8_t*>(a.scales), at + Z::CHUNK);
+    load_lds_off<4>(scale0, (__umul24(n, (uint32_t)a.scales_stride) + g) * 4, at);
+    if (zero0) load_lds_off<1>(zero0, __umul24(n, (uint32_t)a.zeros_stride) + g, at + Z::CHUNK);
+    else load_lds_off<1>(scale0, 0, at + Z::CHUNK);   // (not looked at)
   };
-  int slot = 0, to = (s0 / Z::CS + 1) % Z::CHUNKS;   // of the next step to load: its slot, the buffer of the chunk after its own
-  auto load = [&](int step) {
-    uint8_t* const at = smem + slot * Z::BYTES;
-    const int k = step * 128;   // pieces past the end of the inputs: the step's first once more, not multiplied
-    const int kw = k + 32 * piece_w < K ? k + 32 * piece_w : k, kx = k + 8 * piece_x < K ? k + 8 * piece_x : k;
+  uint32_t slot = 0, slot_x = 0, to = (s0 / CS + 1) % Z::CHUNKS;   // of the next step to load: its slots, the buffer of the chunk after its own
+  auto load = [&](uint32_t step) {
+    uint8_t* const at = smem + slot * Z::WSTEP + wave * 2048;
+    uint8_t* const at_x = smem + Z::X + slot_x * Z::XSTEP + share * 1024;
+    const int k = (int)step * 128;
+    if (k + 128 <= K) {
+      load_lds_off<16>(x + k, off_x, at_x);
 #pragma unroll
-    for (int u = 0; u < Z::S; ++u) load_scales(step / Z::CS + 1, (step % Z::CS * Z::S + u) % PARTS, to);
+      for (int b = 0; b < 2; ++b) load_lds_off<16>(w + (k >> 1), off_w[b], at + b * 1024);
+    } else {   // pieces past the end of the inputs: the step's first once more, not multiplied
+      load_lds_off<16>(x + k, off_x - (k + 8 * piece_x < K ? 0 : 16 * piece_x), at_x);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) load_lds_from<16>(w[b] + (kw >> 1), at + Z::W + wave * 2048 + b * 1024);
-    load_lds_from<16>(x + kx, at + Z::X + (wave & (4 * MB - 1)) * 1024);
+      for (int b = 0; b < 2; ++b) load_lds_off<16>(w + (k >> 1), off_w[b] - (k + 32 * piece_w < K ? 0 : 16 * piece_w), at + b * 1024);
+    }
+#pragma unroll
+    for (int u = 0; u < Z::S; ++u) load_scales(step / CS + 1, (step % CS * Z::S + u) % PARTS, to);
     slot = slot + 1 < Z::BUFS ? slot + 1 : 0;
-    if ((step + 1) % Z::CS == 0) to = to + 1 < Z::CHUNKS ? to + 1 : 0;
+    slot_x = slot_x + 1 < AHEAD ? slot_x + 1 : 0;
+    if ((step + 1) % CS == 0) to = to + 1 < Z::CHUNKS ? to + 1 : 0;
   };
-  f32x4 acc[MB][2], dot[MB][2], all[MB];
+  // The wave's own share of a step's rows (which it loaded itself), for all: woven, and summed by groups.
+  uint32_t raw = 0;
+  auto weave_step = [&](uint32_t step) {
+    if (wave < 4 * MB) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(smem + Z::X + raw * Z::XSTEP + share * 1024 + lane * 16);
+      *reinterpret_cast<u32x4*>(smem + Z::WOVEN + (step & 1) * Z::XSTEP + share * 1024 + lane * 16) = weave(v);
+      float sum = dot2(v[0], ONES, dot2(v[1], ONES, 0.0f)) + dot2(v[2], ONES, dot2(v[3], ONES, 0.0f));
+      sum += swapped<0xB1>(sum);                          // lane ^ 1
+      sum += swapped<0x4E>(sum);                          // lane ^ 2
+      if constexpr (GP < 4) sum += swapped<0x141>(sum);   // 7 - lane of eight
+      if constexpr (GP < 2) sum += swapped<0x140>(sum);   // 15 - lane
+      if (i % (16 / GP) == 0) {
+        float* const all = reinterpret_cast<float*>(smem + Z::ALL + (step / CS & 1) * Z::SUMS);
+        all[(step % CS * GP + piece_x / (16 / GP)) * 16 * MB + row_x] = sum;
+      }
+    }
+    raw = raw + 1 < AHEAD ? raw + 1 : 0;
+  };
+  uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+  asm("" : "+v"(mask), "+v"(sixteen));   // (in registers: as literals they take an operation each)
+  f32x4 acc[MB][2];
 #pragma unroll
   for (int r = 0; r < MB; ++r)
 #pragma unroll
     for (int b = 0; b < 2; ++b) acc[r][b] = f32x4{0, 0, 0, 0};
   // the first chunk, and what the steps before the first one of its chunk would have brought of the next
 #pragma unroll
-  for (int u = 0; u < PARTS; ++u) load_scales(s0 / Z::CS, u, s0 / Z::CS % Z::CHUNKS);
-  for (int u = 0; u < s0 % Z::CS * Z::S; ++u) load_scales(s0 / Z::CS + 1, u % PARTS, to);
+  for (int u = 0; u < PARTS; ++u) load_scales(s0 / CS, u, s0 / CS % Z::CHUNKS);
+  for (uint32_t u = 0; u < s0 % CS * Z::S; ++u) load_scales(s0 / CS + 1, u % PARTS, to);
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u)
     if (s0 + u < s1) load(s0 + u);
-  int now = 0, from = s0 / Z::CS % Z::CHUNKS;
-  for (int step = s0; step < s1; ++step) {
-    if (step + AHEAD <= s1) meet_but<(AHEAD - 1) * Z::L>();
+  if (s0 + AHEAD <= s1) arrived_but<AHEAD * Z::L - 1>();   // (the first step's rows)
+  else arrived();
+  weave_step(s0);
+  uint32_t now = 0, from = s0 / CS % Z::CHUNKS;
+  for (uint32_t step = s0; step < s1; ++step) {
+    // this step's weights and the next one's rows are here
+    if (step + AHEAD <= s1) meet_but<(AHEAD - 1) * Z::L - 1>();
     else meet();
-    if (step + AHEAD < s1) load(step + AHEAD);   // into the slot that all waves have read
-    const uint8_t* const at = smem + now * Z::BYTES;
+    if (step + 1 < s1) weave_step(step + 1);
+    if (step + AHEAD < s1) load(step + AHEAD);   // into the slots that this wave has read
+    const uint8_t* const at = smem + now * Z::WSTEP + wave * 2048 + i * 64 + q * 4;
+    const uint8_t* const rows = smem + Z::WOVEN + (step & 1) * Z::XSTEP + i * 256;
     now = now + 1 < Z::BUFS ? now + 1 : 0;
     // the step's first group in its chunk
-    const uint8_t* const scales = own + from * 2 * Z::CHUNK + 4 * (GP > 1 ? step % Z::CS * GP : step / per_group - step / Z::CS * Z::CS / per_group);
-    if ((step + 1) % Z::CS == 0) from = from + 1 < Z::CHUNKS ? from + 1 : 0;
-    auto run = [&](auto which) {   // 32 inputs
-      constexpr int r = decltype(which)::value, per = 4 / GP;   // (groups of 128 and more make whole steps)
-      constexpr bool begins = r % per == 0, ends = r % per == per - 1;
-      const f32x4 none = {0, 0, 0, 0};
-      u32x4 v[MB];
+    const uint8_t* const chunk = own + from * 2 * Z::CHUNK;
+    const uint8_t* const scales = chunk + 4 * (GP > 1 ? step % CS * GP : step / (uint32_t)per_group - step / CS * CS / (uint32_t)per_group);
+    // all that the step multiplies, read at once
+    u32x4 v[4][MB];
+    uint32_t d[4][2];
+    float scale[GP][2];
 #pragma unroll
-      for (int t = 0; t < MB; ++t) {
-        v[t] = weave(*reinterpret_cast<const u32x4*>(at + Z::X + (16 * t + i) * 256 + (((4 * r + q) ^ i) << 4)));
-        all[t] = mfma16(v[t], u32x4{ONES, ONES, ONES, ONES}, begins ? none : all[t]);
-      }
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) d[r][b] = *reinterpret_cast<const uint32_t*>(at + b * 1024 + ((r ^ (i >> 2)) << 4));
+#pragma unroll
+      for (int t = 0; t < MB; ++t) v[r][t] = *reinterpret_cast<const u32x4*>(rows + t * 4096 + (((4 * r + q) ^ i) << 4));
+    }
+#pragma unroll
+    for (int g = 0; g < GP; ++g)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const uint32_t d = *reinterpret_cast<const uint32_t*>(at + Z::W + wave * 2048 + b * 1024 + i * 64 + ((r ^ (i >> 2)) << 4) + q * 4);
-        const u32x4 f = {(d << 3 & 0x00780078u) | 0x41804180u, (d >> 1 & 0x00780078u) | 0x41804180u, (d >> 5 & 0x00780078u) | 0x41804180u, (d >> 9 & 0x00780078u) | 0x41804180u};
-#pragma unroll
-        for (int t = 0; t < MB; ++t) dot[t][b] = mfma16(v[t], f, begins ? none : dot[t][b]);
+        const float f = *reinterpret_cast<const float*>(scales + ((16 * b + i) * GC + g) * 4);
+        scale[g][b] = GP == 1 || (int)step * 128 + g * (128 / GP) < K ? f : 0.0f;   // (a last step may be short by whole groups)
       }
-      if constexpr (ends) {
+#pragma unroll
+    for (int g = 0; g < GP; ++g) {
+      f32x4 dot[MB][2];
+#pragma unroll
+      for (int r = 4 / GP * g; r < 4 / GP * (g + 1); ++r)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const uint8_t* const entry = scales + ((16 * b + i) * Z::GC + r / per) * 4;
-          const float scale = *reinterpret_cast<const float*>(entry);
-          const float zero = 16.0f + (a.zeros ? (float)*reinterpret_cast<const uint32_t*>(entry + Z::CHUNK) : 8.0f);
+          const uint32_t w4 = d[r][b];
+          const u32x4 f = {(w4 << 3 & mask) | sixteen, (w4 >> 1 & mask) | sixteen, (w4 >> 5 & mask) | sixteen, (w4 >> 9 & mask) | sixteen};
 #pragma unroll
-          for (int t = 0; t < MB; ++t)
+          for (int t = 0; t < MB; ++t) dot[t][b] = mfma16(v[r][t], f, r == 4 / GP * g ? f32x4{0, 0, 0, 0} : dot[t][b]);
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[t][b][e] += scale * (dot[t][b][e] - zero * all[t][e]);
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int t = 0; t < MB; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][b][e] += scale[g][b] * dot[t][b][e];
+    }
+    if ((step + 1) % CS == 0 || step + 1 == s1) {   // the chunk's zero points (its groups that lie in this share)
+      const uint32_t c = step / CS;
+      const float* const all = reinterpret_cast<const float*>(smem + Z::ALL + (c & 1) * Z::SUMS);
+#pragma unroll
+      for (int u = 0; u < GC; u += 4) {
+        const uint32_t k = u + q, at_step = c * CS + k / GP;   // this lane's group of the chunk
+        const bool mine = at_step >= s0 && at_step < s1 && (GP == 1 || c * GC + k < (uint32_t)groups);
+        const uint32_t entry = GP > 1 ? k : at_step / (uint32_t)per_group - c * CS / (uint32_t)per_group;
+        float taken[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint8_t* const e = chunk + ((16 * b + i) * GC + entry) * 4;
+          const float zero = 16.0f + (zero0 ? (float)*reinterpret_cast<const uint32_t*>(e + Z::CHUNK) : 8.0f);
+          taken[b] = mine ? -zero * *reinterpret_cast<const float*>(e) : 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < MB; ++t) {
+          const float sum = mine ? all[k * 16 * MB + 16 * t + i] : 0.0f;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum, taken[b], acc[t][b], 0, 0, 0);
         }
       }
-    };
-    const int left = K - step * 128;   // a last step may be short by whole groups
-    run(std::integral_constant<int, 0>{});
-    if (GP == 1 || left >= 128) {
-      run(std::integral_constant<int, 1>{});
-      run(std::integral_constant<int, 2>{});
-      run(std::integral_constant<int, 3>{});
-    } else {
-      if (left > 32) run(std::integral_constant<int, 1>{});
-      if (left > 64) run(std::integral_constant<int, 2>{});
+      from = from + 1 < Z::CHUNKS ? from + 1 : 0;
     }
   }
+  const uint32_t stride = splits > 1 ? (uint32_t)a.outputs : (uint32_t)a.out_stride;
+  float* const part = static_cast<float*>(a.workspace) + ((int64_t)split * a.rows + m0) * a.outputs + n0;
+  bf16_t* const out = static_cast<bf16_t*>(a.out) + (int64_t)m0 * a.out_stride + n0;
 #pragma unroll
   for (int t = 0; t < MB; ++t)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int col = n0 + 16 * b + i, row = m0 + 16 * t + 4 * q;
-      if (col > last) continue;
+    for (int e = 0; e < 4; ++e) {
+      const int row = 16 * t + 4 * q + e;
+      if (m0 + row >= a.rows) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (row + e >= a.rows) continue;
-        if (splits > 1) static_cast<float*>(a.workspace)[((int64_t)split * a.rows + row + e) * a.outputs + col] = acc[t][b][e];
-        else st(static_cast<bf16_t*>(a.out) + (row + e) * a.out_stride + col, acc[t][b][e]);
+      for (int b = 0; b < 2; ++b) {
+        const int col = 16 * b + i;
+        if (n0 + col > last) continue;
+        const uint32_t to = row * stride + col;
+        if (splits > 1) part[to] = acc[t][b][e];
+        else st(out + to, acc[t][b][e]);
       }
     }
 }
 
-// Adds the parts of every result, in their order.
+// Adds the parts of every result, in their order, eight on their way at a time.
 template <typename T>
-__global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int splits) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, size = (int64_t)a.rows * a.outputs;
-  if (at >= size) return;
-  const float* const parts = static_cast<const float*>(a.workspace) + at;
-  float y = parts[0];
-  for (int s = 1; s < splits; ++s) y += parts[s * size];
-  const int row = (int)(at / a.outputs);
-  st(static_cast<T*>(a.out) + row * a.out_stride + (at - (int64_t)row * a.outputs), y);
+__global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int splits, uint32_t blocks) {
+  const uint32_t row = blockIdx.x / blocks, col = blockIdx.x % blocks * 256 + threadIdx.x;
+  if (col >= (uint32_t)a.outputs) return;
+  const int64_t size = (int64_t)a.rows * a.outputs;
+  const float* at = static_cast<const float*>(a.workspace) + (int64_t)row * a.outputs + col;
+  float y = 0.0f;
+  for (int s = 0; s < splits; s += 8) {
+    float part[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) part[u] = s + u < splits ? at[u * size] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) y += part[u];
+    at += 8 * size;
+  }
+  st(static_cast<T*>(a.out) + (int64_t)row * a.out_stride + col, y);
 }
 
 // Which kernel takes a call, from its sizes and type alone (the workspace goes by it), where the addresses allow all of them.
@@ -590,14 +669,16 @@ int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
   }
   const Plan p = plan(a);
   const bool aligned = (reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.w_stride) % 16 == 0;
+  const bool near = a.x_stride < 1 << 24 && a.out_stride < 1 << 24 && a.w_stride < 1 << 24 && a.scales_stride < 1 << 24 && (!a.zeros || a.zeros_stride < 1 << 24);   // (32 rows lie within 2^31 bytes)
   if (p.kernel == FEW && aligned) {
     if (a.rows == 1) launch_few<T, 1>(a, s);
     else if (a.rows == 2) launch_few<T, 2>(a, s);
     else launch_few<T, 4>(a, s);
-  } else if (p.kernel == WIDE && aligned) {
+  } else if (p.kernel == WIDE && aligned && near) {
     if (p.mb == 1) launch_wide<1>(a, p, s);
     else launch_wide<2>(a, p, s);
-    if (p.splits > 1) q4_join_kernel<T><<<dim3((uint32_t)(((int64_t)a.rows * a.outputs + 255) / 256)), 256, 0, s>>>(a, p.splits);
+    const uint32_t blocks = (uint32_t)((a.outputs + 255) / 256);
+    if (p.splits > 1) q4_join_kernel<T><<<dim3(blocks * (uint32_t)a.rows), 256, 0, s>>>(a, p.splits, blocks);
   } else if (a.outputs >= 16384) {   // (four blocks of outputs share the rows' inputs; fewer leave compute units without work)
     launch_tiles<T, 4, 8>(a, vw, s);
   } else if (a.inputs >= 2048) {
