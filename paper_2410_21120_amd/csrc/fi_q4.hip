@@ -606,22 +606,25 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
 // Which kernel takes a call, from its sizes and type alone (the workspace goes by it), where the addresses allow all of them.
 //  FEW:  reads 2048 inputs a step; its time grows with rows x outputs (us, few / tile: 4096 x 1000 inputs x outputs, 1 row 3.2 / 8.4, 4 rows 5.2 / 9.1, 16 rows 7.9 / 11.3;
 //        4096 x 4096, 4 rows 7.8 / 10.0, 8 rows 10.9 / 10.8; 1024 x 16384, 2 rows 8.2 / 8.2, 4 rows 12.6 / 8.4; 512 x 8192, 1 row 4.2 / 3.6).
-//  WIDE: has two launches and about 9 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 14.0 / 11.9, 20 rows 15.4 / 19.4;
-//        1024 x 16384, 8 rows 11.3 / 8.5, 20 rows 13.9 / 15.3; 4096 x 16384, 8 rows 19.4 / 27.4; 16384 x 4096, 16 rows 23 / 38; few there 4 rows 19.6).
+//  WIDE: has two launches and about 8 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 12.0 / 11.8, 20 rows 13.6 / 19.4;
+//        1024 x 16384, 16 rows 12.3 / 8.8, 20 rows 14.1 / 15.4; 4096 x 8192, 8 rows 13.7 / 19.2; 4096 x 300, 20 rows 11.0 / 10.9; 8192 x 300, 20 rows 11.4 / 19.8; wide / few:
+//        8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4).
 enum Kernel { FEW, TILE, WIDE };
 struct Plan { Kernel kernel; int mb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
   Plan p = {TILE, 1, 1};
   const int64_t weights = (int64_t)a.inputs * a.outputs, blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
-  if ((a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && (a.rows <= 4 || (a.rows <= 16 && a.outputs < 2048)))) {
-    p.kernel = FEW;
-  } else if (a.dtype == FI_BF16 && a.rows > 4 && weights * ((a.rows + 15) / 16) >= 3 << 23) {
+  const bool wide = a.dtype == FI_BF16 && a.rows > 4 &&
+                    (weights * ((a.rows + 15) / 16) >= 3 << 23 || a.inputs >= 12288 || (a.inputs >= 8192 && a.rows > 16));
+  if (wide) {
     p.kernel = WIDE;
     p.mb = a.rows > 16 ? 2 : 1;
     const int64_t groups = blocks * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
     int64_t splits = groups > 0 ? (256 + groups - 1) / groups : 1;   // a workgroup per compute unit
     if (splits > steps / 4) splits = steps / 4;                       // (a join costs about as much as four steps)
     p.splits = splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
+  } else if ((a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && (a.rows <= 4 || (a.rows <= 16 && a.outputs < 2048)))) {
+    p.kernel = FEW;
   }
   return p;
 }
