@@ -579,10 +579,13 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
   if (row < w.rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
-// What a workgroup of the tree kernels works on: a block of rows (node, head) of one key head of one sequence, and a share of its keys.
+// What a workgroup of the tree kernels works on: a block of rows (node, head) of one key head of one sequence, and of its keys the tiles [t0, t1).
 struct TreeWork {
-  int b, hk, cached, keys, n0, nodes, block, split, splits;
+  int b, hk, cached, keys, n0, nodes, block, split, splits, t0, t1;
 };
+// How a call is shared out (on the host): parts that a row can have, least tiles of a part, keys of a tile, what a stream costs beside its tiles, in tiles,
+// rows of a block, blocks of a sequence at most, floats before the parts in the workspace.
+struct TreeSplit { int splits, least, unit, over, rows, blocks, header; };
 
 // A sequence as the kernels see it: its offsets and lengths clamped to the tensors.
 __device__ __forceinline__ void tree_sequence(const fi_tree_attention_args& a, int b, TreeWork& w) {
@@ -594,94 +597,125 @@ __device__ __forceinline__ void tree_sequence(const fi_tree_attention_args& a, i
   w.cached = clamp_int(a.cached[b], 0, places);
   w.keys = w.nodes < places - w.cached ? w.cached + w.nodes : places;
 }
-// Shares of a sequence's keys: `splits` at most, of `least` keys or more.
-__device__ __forceinline__ int shares(int keys, int splits, int least) { return clamp_int((keys + least - 1) / least, 1, splits); }
-
 // The work of a call goes to the workgroups in one of two ways.
-//  Direct: a workgroup for every part that a sequence can have; parts that a shorter one has not end at once, but wait for a compute unit to themselves first.
-//  Counted (few sequences that may have many parts): as many workgroups as run at a time; the first wave of each counts the parts of all sequences and
-//  the parts, of about equal size, are dealt out in turn.  12 sequences, three of them long: direct 43 us, counted 38; one sequence of 1004 keys: 16, 19.
-constexpr int SEQS = 512;   // most sequences that are counted
-struct TreeItems {
-  int ends[SEQS];   // parts of the sequences up to this one
+//  Direct: a workgroup for every part that a sequence can have, of equal size; parts that a shorter one has not end at once, but wait for a compute unit first.
+//  Counted: as many workgroups as run at a time.  The first wave of each lines up the tiles of all streams (sequence, block, key head; a stream's beginning
+//  counts for `over` tiles) and every workgroup takes its stretch of the line, wherever that begins and ends in a stream.
+//  Lengths up to 8000, spread over their logarithm: 16 sequences of 32 key heads direct 253 us, counted 90; 64 of 8 key heads and ten nodes 344, 114; the last
+//  with 8000 keys each 428, 479; 2 of 1000 keys 12, 19.
+constexpr int SEQS = 256;   // most sequences that are counted
+// Counted: the least keys of a stretch (12 sequences up to 5001 keys: one node, 128 keys 30.4 us, 256 26.5; up to 500 keys, 37 nodes: 128 27.8, 512 36.2), and what a
+// stream's beginning counts for, in tiles of 64 or 32 keys (up to 20000 keys: 37 nodes, 1 tile 114 us, 3 85, 5 84; one node, 8 tiles 74, 14 and 20 55).
+constexpr int TILE_LEAST = 128, OWN_LEAST = 256, TILE_OVER = 5, OWN_OVER = 20;
+struct TreeLine {
+  int start[SEQS];   // where a sequence begins
   int n0[SEQS], nodes[SEQS], cached[SEQS], keys[SEQS];
-  int least, total;
+  int quota, total;
 };
-__device__ __forceinline__ void count_items(const fi_tree_attention_args& a, TreeItems& items, int rows_per_block, int splits, int least, int parts) {
-  const int group = a.q_heads / a.kv_heads, n = a.n_seqs;
+__device__ __forceinline__ int tiles_of(int keys, int unit) { return keys > unit ? (keys + unit - 1) / unit : 1; }
+__device__ __forceinline__ int streams_of(const fi_tree_attention_args& a, const TreeSplit& p, int nodes) {
+  return (nodes * (a.q_heads / a.kv_heads) + p.rows - 1) / p.rows * a.kv_heads;
+}
+__device__ __forceinline__ void line_up(const fi_tree_attention_args& a, const TreeSplit& p, TreeLine& line) {
+  const int n = a.n_seqs, lane = threadIdx.x;
   if (threadIdx.x < 64) {
-    const int lane = threadIdx.x;
-    auto blocks_of = [&](int nodes) { return (nodes * group + rows_per_block - 1) / rows_per_block * a.kv_heads; };
-    float work = 0.0f;
-    for (int b = lane; b < n; b += 64) {
-      TreeWork w;
-      tree_sequence(a, b, w);
-      items.n0[b] = w.n0;
-      items.nodes[b] = w.nodes;
-      items.cached[b] = w.cached;
-      items.keys[b] = w.keys;
-      work += (float)w.keys * (float)blocks_of(w.nodes);
-    }
-    int size = least, total = 0;
-    if (splits > 1) {   // about as many parts as there are workgroups at a time, rather fewer than more
-      const float even = wave_sum(work) / (float)parts;
-      if (even > (float)least) size = even < 1e9f ? ((int)even + 64) / 64 * 64 : 1 << 30;
-      for (int tries = 0; tries < 4; ++tries) {
-        float count = 0.0f;
-        for (int b = lane; b < n; b += 64) count += (float)(blocks_of(items.nodes[b]) * shares(items.keys[b], splits, size));
-        if (wave_sum(count) <= (float)parts || size >= 1 << 29) break;
-        size = (size + size / 4 + 63) / 64 * 64;
-      }
-    }
+    int total = 0, longest = 1;
     for (int c = 0; c < n; c += 64) {
       const int b = c + lane;
-      int upto = b < n ? blocks_of(items.nodes[b]) * shares(items.keys[b], splits, size) : 0;
+      int upto = 0;
+      if (b < n) {
+        TreeWork w;
+        tree_sequence(a, b, w);
+        line.n0[b] = w.n0;
+        line.nodes[b] = w.nodes;
+        line.cached[b] = w.cached;
+        line.keys[b] = w.keys;
+        const int tiles = tiles_of(w.keys, p.unit);
+        upto = streams_of(a, p, w.nodes) * (tiles + p.over);
+        if (tiles > longest) longest = tiles;
+      }
+      const int mine = upto;
       for (int o = 1; o < 64; o <<= 1) {
         const int up = __shfl_up(upto, o);
         if (lane >= o) upto += up;
       }
-      if (b < n) items.ends[b] = total + upto;
+      if (b < n) {
+        line.start[b] = total + upto - mine;
+        if (blockIdx.x == 0) static_cast<int*>(a.workspace)[4 + b] = total + upto - mine;   // (for the join)
+      }
       total += __shfl(upto, 63);
     }
+    for (int o = 32; o; o >>= 1) {
+      const int other = __shfl_xor(longest, o);
+      if (other > longest) longest = other;
+    }
     if (lane == 0) {
-      items.least = size;
-      items.total = total;
-      if (splits > 1 && blockIdx.x == 0) *static_cast<int*>(a.workspace) = size;   // (for the join)
+      int quota = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+      if (quota < p.least) quota = p.least;
+      const int fits = (longest + p.splits - 2) / (p.splits - 1);   // (a stretch may begin inside a tile's share: one part more)
+      if (quota < fits) quota = fits;
+      line.quota = quota;
+      line.total = total;
+      if (blockIdx.x == 0) *static_cast<int*>(a.workspace) = quota;
     }
   }
   __syncthreads();
 }
-// Item number `item`; false behind the last one.
-__device__ __forceinline__ bool tree_item(const fi_tree_attention_args& a, const TreeItems& items, int item, int splits, TreeWork& w) {
-  if (item >= items.total) return false;
-  int lo = 0, hi = a.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (items.ends[mid] > item) hi = mid;
-    else lo = mid + 1;
-  }
-  w.b = lo;
-  w.n0 = items.n0[lo];
-  w.nodes = items.nodes[lo];
-  w.cached = items.cached[lo];
-  w.keys = items.keys[lo];
-  w.splits = shares(w.keys, splits, items.least);
-  int r = lo > 0 ? item - items.ends[lo - 1] : item;
-  w.split = r % w.splits;
-  r /= w.splits;
-  w.hk = r % a.kv_heads;
-  w.block = r / a.kv_heads;
-  return true;
+// Parts of the stream that begins at `base` with `tiles` tiles: the workgroups whose stretches its tiles lie in.
+__device__ __forceinline__ void parts_of(const TreeSplit& p, int base, int tiles, int quota, int& first, int& count) {
+  first = (base + p.over) / quota;
+  count = (base + p.over + tiles - 1) / quota - first + 1;
 }
+// Every piece of this workgroup's stretch.
+template <typename Work>
+__device__ __forceinline__ void along_the_line(const fi_tree_attention_args& a, const TreeSplit& p, const TreeLine& line, Work work) {
+  auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int n = a.n_seqs, quota = same(line.quota), total = same(line.total);
+  if ((int64_t)blockIdx.x * quota >= total) return;
+  int pos = blockIdx.x * quota, b = 0;
+  const int end = total - pos < quota ? total : pos + quota;
+  for (int hi = n - 1; b < hi;) {   // the last sequence that begins here or before
+    const int mid = (b + hi + 1) >> 1;
+    if (same(line.start[mid]) <= pos) b = mid;
+    else hi = mid - 1;
+  }
+  while (pos < end) {
+    while (b + 1 < n && same(line.start[b + 1]) <= pos) ++b;
+    TreeWork w;
+    w.b = b;
+    w.n0 = same(line.n0[b]);
+    w.nodes = same(line.nodes[b]);
+    w.cached = same(line.cached[b]);
+    w.keys = same(line.keys[b]);
+    const int tiles = tiles_of(w.keys, p.unit), per = tiles + p.over, start = same(line.start[b]), stream = (pos - start) / per, base = start + stream * per;
+    w.hk = stream % a.kv_heads;
+    w.block = stream / a.kv_heads;
+    w.t0 = pos - base > p.over ? pos - base - p.over : 0;
+    w.t1 = end - base - p.over < tiles ? end - base - p.over : tiles;
+    if (w.t0 < w.t1) {
+      int first;
+      parts_of(p, base, tiles, quota, first, w.splits);
+      w.split = (int)blockIdx.x - first;
+      if (w.keys == 0) w.t1 = 0;
+      work(w);
+    }
+    pos = base + per;
+  }
+}
+// Shares of a sequence's keys in direct calls: `splits` at most, of `least` tiles or more.
+__device__ __forceinline__ int shares(const TreeSplit& p, int keys) { return clamp_int((tiles_of(keys, p.unit) + p.least - 1) / p.least, 1, p.splits); }
 // Direct: the grid is sequences and blocks, key heads, parts.
-__device__ __forceinline__ bool tree_direct(const fi_tree_attention_args& a, int splits, int least, int blocks, TreeWork& w) {
-  const int b = blocks == 1 ? blockIdx.x : blockIdx.x / blocks;
+__device__ __forceinline__ bool tree_direct(const fi_tree_attention_args& a, const TreeSplit& p, TreeWork& w) {
+  const int b = p.blocks == 1 ? blockIdx.x : blockIdx.x / p.blocks;
   tree_sequence(a, b, w);
-  w.block = blockIdx.x - b * blocks;
+  w.block = blockIdx.x - b * p.blocks;
   w.hk = blockIdx.y;
   w.split = blockIdx.z;
-  w.splits = shares(w.keys, splits, least);
-  return w.split < w.splits;
+  w.splits = shares(p, w.keys);
+  const int tiles = w.keys ? tiles_of(w.keys, p.unit) : 0;
+  w.t0 = (int)((int64_t)tiles * w.split / w.splits);
+  w.t1 = (int)((int64_t)tiles * (w.split + 1) / w.splits);
+  return w.split < w.splits && w.block * p.rows < w.nodes * (a.q_heads / a.kv_heads);
 }
 
 // Which of the 32 keys from `key` on a node (place `node` in its tree, mask row `words`) sees.
@@ -726,13 +760,13 @@ struct Pages {
   }
 };
 
-// The workspace: 16 bytes (the least keys of a part), then parts of a row (node, head): `splits` times head_dim sums, then for all rows the maximum and the
-// weights' sum of each.
-__device__ __forceinline__ float* part_sums(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
-  return static_cast<float*>(a.workspace) + 4 + (row * splits + split) * a.head_dim;
+// The workspace: the line of a counted call (16 bytes with its quota, then where each sequence begins), then parts of a row (node, head): `splits` times
+// head_dim sums, then for all rows the maximum and the weights' sum of each.
+__device__ __forceinline__ float* part_sums(const fi_tree_attention_args& a, const TreeSplit& p, int64_t row, int split) {
+  return static_cast<float*>(a.workspace) + p.header + (row * p.splits + split) * a.head_dim;
 }
-__device__ __forceinline__ float* part_stats(const fi_tree_attention_args& a, int64_t row, int splits, int split) {
-  return static_cast<float*>(a.workspace) + 4 + a.nodes * a.q_heads * splits * a.head_dim + (row * splits + split) * 2;
+__device__ __forceinline__ float* part_stats(const fi_tree_attention_args& a, const TreeSplit& p, int64_t row, int split) {
+  return static_cast<float*>(a.workspace) + p.header + a.nodes * a.q_heads * p.splits * a.head_dim + (row * p.splits + split) * 2;
 }
 
 // TL::add_strange for the keys [from, to) of a tree: of those only the tiles that were masked.
@@ -750,14 +784,14 @@ __device__ __forceinline__ void tree_strange(const fi_tree_attention_args& a, co
 }
 
 template <typename TL, typename T>
-__device__ __forceinline__ void finish(const fi_tree_attention_args& a, const TreeWork& w, int splits, typename TL::State& st, float total, bool there, int node, int head) {
+__device__ __forceinline__ void finish(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, typename TL::State& st, float total, bool there, int node, int head) {
   if (!there) return;
   if (w.splits == 1) {
     TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1], a.head_dim, total == 0.0f ? 0.0f : 1.0f / total);
     return;
   }
   const int64_t row = (int64_t)(w.n0 + node) * a.q_heads + head;
-  float* const sums = part_sums(a, row, splits, w.split);
+  float* const sums = part_sums(a, p, row, w.split);
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
@@ -766,7 +800,7 @@ __device__ __forceinline__ void finish(const fi_tree_attention_args& a, const Tr
       const int d = db * 32 + 8 * g + 4 * half;
       if (d < a.head_dim) *reinterpret_cast<float4*>(sums + d) = make_float4(st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]);
     }
-  if (half == 0) *reinterpret_cast<float2*>(part_stats(a, row, splits, w.split)) = make_float2(st.top, total);
+  if (half == 0) *reinterpret_cast<float2*>(part_stats(a, p, row, w.split)) = make_float2(st.top, total);
 }
 
 // Many rows: the waves have 32 rows each and share the tiles, as for a prompt, but few workgroups are there to hide each other's waiting: three tiles
@@ -780,7 +814,7 @@ struct Shared {
   static_assert(KEYS / TL::RPI % WAVES == 0 && 2 * AHEAD + 2 <= RING, "every wave issues L loads a tile; a ring slot is free again");
 };
 template <typename T, int DB, int WAVES>
-__device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, const TreeWork& w, int splits, uint8_t* smem) {
+__device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, uint8_t* smem) {
   using TL = Tile<T, DB>;
   using SH = Shared<T, DB, WAVES>;
   constexpr int KB = SH::KB, KEYS = SH::KEYS, BYTES = SH::BYTES, AHEAD = SH::AHEAD, BUFS = SH::BUFS, L = SH::L, RING = SH::RING;
@@ -791,7 +825,7 @@ __device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, 
   const int rows = w.nodes * group, first = w.block * 32 * WAVES;
   if (first >= rows) return;
   const int row = first + 32 * wave + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
-  const int all = (w.keys + KEYS - 1) / KEYS, t0 = (int)((int64_t)all * w.split / w.splits), t1 = (int)((int64_t)all * (w.split + 1) / w.splits);
+  const int t0 = w.t0, t1 = w.t1;
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
   const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
   const Pages pages(a, w.b, TL::EP);
@@ -849,21 +883,21 @@ __device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, 
   }
   arrived();   // (page requests past the end)
   if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * KEYS, t1 * KEYS, KEYS);
-  finish<TL, T>(a, w, splits, st, both_halves(st.total), row < rows, node, head);
+  finish<TL, T>(a, w, p, st, both_halves(st.total), row < rows, node, head);
 }
 template <typename T, int DB, int WAVES, bool COUNTED>
-__global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, int splits, int least, int blocks) {
+__global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, TreeSplit p) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[Shared<T, DB, WAVES>::LDS];
-  TreeWork w;
   if constexpr (COUNTED) {
-    __shared__ TreeItems items;
-    count_items(a, items, 32 * WAVES, splits, least, gridDim.x);
-    for (int item = blockIdx.x; tree_item(a, items, item, splits, w); item += gridDim.x) {
-      meet();   // (the item before has been read to the end)
-      tree_tile_work<T, DB, WAVES>(a, w, splits, smem);
-    }
-  } else if (tree_direct(a, splits, least, blocks, w)) {
-    tree_tile_work<T, DB, WAVES>(a, w, splits, smem);
+    __shared__ TreeLine line;
+    line_up(a, p, line);
+    along_the_line(a, p, line, [&](const TreeWork& w) {
+      meet();   // (the piece before has been read to the end)
+      tree_tile_work<T, DB, WAVES>(a, w, p, smem);
+    });
+  } else {
+    TreeWork w;
+    if (tree_direct(a, p, w)) tree_tile_work<T, DB, WAVES>(a, w, p, smem);
   }
 }
 
@@ -876,7 +910,7 @@ struct Own {
   static constexpr int LDS = 2 * BYTES * WAVES + WAVES * 512;
 };
 template <typename T, int DB>
-__device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, const TreeWork& w, int splits, uint8_t* smem) {
+__device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, uint8_t* smem) {
   using TL = Tile<T, DB>;
   constexpr int BYTES = Own<T, DB>::BYTES, WAVES = Own<T, DB>::WAVES;
   const int D = a.head_dim, group = a.q_heads / a.kv_heads;
@@ -884,8 +918,7 @@ __device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, c
   const int rows = w.nodes * group, first = w.block * 32;
   if (first >= rows) return;
   const int row = first + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
-  const int all = (w.keys + 31) / 32, share = w.split * WAVES + wave, total_shares = w.splits * WAVES;
-  const int t0 = (int)((int64_t)all * share / total_shares), t1 = (int)((int64_t)all * (share + 1) / total_shares);
+  const int t0 = w.t0 + (int)((int64_t)(w.t1 - w.t0) * wave / WAVES), t1 = w.t0 + (int)((int64_t)(w.t1 - w.t0) * (wave + 1) / WAVES);
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
   const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
   const Pages pages(a, w.b, TL::EP);
@@ -959,82 +992,80 @@ __device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, c
     }
     st.top = top;
   }
-  finish<TL, T>(a, w, splits, st, total, row < rows, node, head);
+  finish<TL, T>(a, w, p, st, total, row < rows, node, head);
 }
 template <typename T, int DB, bool COUNTED>
-__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, int splits, int least, int blocks) {
+__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, TreeSplit p) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[Own<T, DB>::LDS];
-  TreeWork w;
   if constexpr (COUNTED) {
-    __shared__ TreeItems items;
-    count_items(a, items, 32, splits, least, gridDim.x);
-    for (int item = blockIdx.x; tree_item(a, items, item, splits, w); item += gridDim.x) {
-      __syncthreads();   // (the item before has been read to the end)
-      tree_own_work<T, DB>(a, w, splits, smem);
-    }
-  } else if (tree_direct(a, splits, least, blocks, w)) {
-    tree_own_work<T, DB>(a, w, splits, smem);
+    __shared__ TreeLine line;
+    line_up(a, p, line);
+    along_the_line(a, p, line, [&](const TreeWork& w) {
+      __syncthreads();   // (the piece before has been read to the end)
+      tree_own_work<T, DB>(a, w, p, smem);
+    });
+  } else {
+    TreeWork w;
+    if (tree_direct(a, p, w)) tree_own_work<T, DB>(a, w, p, smem);
   }
 }
 
-// Joins the parts of a row (node, head), in their order and all in flight at once (they come from other dies: a load takes microseconds).  Up to 16
-// parts: a wave per row.  WIDE: a workgroup per row, its waves add a quarter of the parts each, then the waves' sums are added.
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256) tree_join_kernel(fi_tree_attention_args a, int splits, int least) {
-  __shared__ float sums[3][FI_MAX_HEAD_DIM];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  if (row >= a.nodes * a.q_heads) return;
-  const int node = (int)(row / a.q_heads), head = (int)(row - (int64_t)node * a.q_heads);
+// Joins the parts of a row (node, head), in their order and 16 in flight at once (they come from other dies: a load takes microseconds).  A wave per row: with
+// thousands of them its instructions count, so everything that the row's lanes share is scalar and a lane has PER values next to each other.  WIDE (more
+// parts of few rows): a workgroup per row, its waves add a quarter of the parts each, then the waves' sums are added.
+template <typename T, int PER, bool WIDE>
+__global__ void __launch_bounds__(256) tree_join_kernel(fi_tree_attention_args a, TreeSplit p, bool counted) {
+  typedef float vec __attribute__((ext_vector_type(PER)));
+  __shared__ vec sums[3][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = a.head_dim;
+  const int row = WIDE ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;   // (rows are below 2^31)
+  if (row >= (int)a.nodes * a.q_heads) return;
+  const int node = row / a.q_heads, head = row - node * a.q_heads;
   const int b = find_seq(a.cu_nodes, a.n_seqs, node);
   TreeWork w;
   tree_sequence(a, b, w);
-  w.splits = shares(w.keys, splits, least > 0 ? least : *static_cast<const int*>(a.workspace));
-  if (w.splits == 1 || node < w.n0 || node - w.n0 >= w.nodes) return;
+  if (node < w.n0 || node - w.n0 >= w.nodes) return;
+  if (counted) {
+    const int* const line = static_cast<const int*>(a.workspace);
+    const int group = a.q_heads / a.kv_heads, hk = head / group, block = ((node - w.n0) * group + head - hk * group) / p.rows, tiles = tiles_of(w.keys, p.unit);
+    int first;
+    parts_of(p, line[4 + b] + (block * a.kv_heads + hk) * (tiles + p.over), tiles, line[0], first, w.splits);
+  } else {
+    w.splits = shares(p, w.keys);
+  }
+  if (w.splits == 1) return;
   const float c = a.scale * 1.44269504f;
-  const float* const parts = part_sums(a, row, splits, 0);
+  const bool inside = lane * PER < D;   // (D is a multiple of four)
+  const float* const parts = part_sums(a, p, row, 0) + (inside ? lane * PER : 0);
   // lane s has part s (64 at most): the weights of all parts at once
-  const float2 mine = lane < w.splits ? *reinterpret_cast<const float2*>(part_stats(a, row, splits, lane)) : make_float2(-INFINITY, 0.0f);
-  const int each = WIDE ? (w.splits + 3) / 4 : w.splits, s0 = WIDE ? wave * each : 0;
-  float acc[RUN] = {};
-  auto add = [&](auto many, int from, float weight) {
-    constexpr int N = decltype(many)::value;
-    float x[N][RUN];
+  const float2 mine = lane < w.splits ? *reinterpret_cast<const float2*>(part_stats(a, p, row, lane)) : make_float2(-INFINITY, 0.0f);
+  const int each = WIDE ? (w.splits + 3) / 4 : w.splits, s0 = WIDE ? wave * each : 0, s1 = s0 + each < w.splits ? s0 + each : w.splits;
+  vec acc = 0.0f, x[16];
+  auto ask = [&](int from) {
 #pragma unroll
-    for (int s = 0; s < N; ++s)
-#pragma unroll
-      for (int i = 0; i < RUN; ++i) {
-        const bool there = s < each && from + s < w.splits && lane + 64 * i < a.head_dim;
-        x[s][i] = there ? parts[(int64_t)(from + s) * a.head_dim + lane + 64 * i] : 0.0f;
-      }
-#pragma unroll
-    for (int s = 0; s < N; ++s) {
-      const float f = __shfl(weight, from + s < 64 ? from + s : 63);
-#pragma unroll
-      for (int i = 0; i < RUN; ++i)
-        if (s < each && from + s < w.splits) acc[i] += x[s][i] * f;
-    }
+    for (int s = 0; s < 16; ++s)
+      if (from + s < s1) x[s] = *reinterpret_cast<const vec*>(parts + (int64_t)(from + s) * D);
   };
+  ask(s0);
   const float top = wave_max(mine.x), base = top == -INFINITY ? 0.0f : top;
   const float weight = lane < w.splits ? __builtin_amdgcn_exp2f((mine.x - base) * c) : 0.0f, total = wave_sum(lane < w.splits ? mine.y * weight : 0.0f);
-  if (each <= 4) add(std::integral_constant<int, 4>{}, s0, weight);
-  else add(std::integral_constant<int, 16>{}, s0, weight);
-  if constexpr (WIDE) {
+  for (int from = s0; from < s1; from += 16) {
+    if (from > s0) ask(from);
 #pragma unroll
-    for (int i = 0; i < RUN; ++i)
-      if (wave && lane + 64 * i < a.head_dim) sums[wave - 1][lane + 64 * i] = acc[i];
+    for (int s = 0; s < 16; ++s)
+      if (from + s < s1) acc += x[s] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), from + s));
+  }
+  if constexpr (WIDE) {
+    if (wave) sums[wave - 1][lane] = acc;
     __syncthreads();
     if (wave) return;
+    acc = acc + sums[0][lane] + sums[1][lane] + sums[2][lane];
   }
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  T* const out = static_cast<T*>(a.out) + node * a.out_strides[0] + head * a.out_strides[1];
+  T* const out = static_cast<T*>(a.out) + node * a.out_strides[0] + head * a.out_strides[1] + lane * PER;
+  if (!inside) return;
 #pragma unroll
-  for (int i = 0; i < RUN; ++i) {
-    const int d = lane + 64 * i;
-    if (d >= a.head_dim) continue;
-    if constexpr (WIDE) acc[i] = acc[i] + sums[0][d] + sums[1][d] + sums[2][d];
-    st(out + d, acc[i] * inv);
-  }
+  for (int i = 0; i < PER; ++i) st(out + i, acc[i] * inv);
 }
 
 // Whether every row of a tensor starts on 16 bytes and its last one, counted in 16-byte pieces, has a 32-bit offset.
@@ -1104,9 +1135,9 @@ bool tree_on_tiles(const fi_tree_attention_args& a) {
          pieces(a.k_cache, a.k_strides, n, 3, es) && pieces(a.v_cache, a.v_strides, n, 3, es);
 }
 
-// How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 that share
-// them; parts of every sequence's keys, and the least keys of a part.
-struct TreePlan { bool own, counted; int waves, blocks, splits, least; };
+// How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 or 256 that
+// share them; parts of every sequence's keys, and the least keys of a part.
+struct TreePlan { bool own, counted; int waves, blocks, splits, least, header; };
 TreePlan plan_tree(const fi_tree_attention_args& a) {
   TreePlan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
@@ -1114,36 +1145,52 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   p.waves = rows <= 128 || a.head_dim > 128 ? 4 : 8;
   const int64_t per_block = p.own ? 32 : 32 * p.waves;
   p.blocks = (int)((rows + per_block - 1) / per_block);
+  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks;
+  auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
   p.least = p.own ? 128 : 512;
-  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks, most = ((int64_t)a.max_length + p.least - 1) / p.least;
-  p.counted = a.n_seqs > 4 && a.n_seqs <= SEQS && units < 512 && most > 1;
-  // Counted: parts enough that one long history among short ones fills the chip, as far as the workspace stays below 64 MB.  Direct: four rounds of workgroups
-  // (4 x 131072 keys: one round 398 us, four 383: the hardware hands them out as units come free).
+  const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
+  p.counted = a.n_seqs > 1 && a.n_seqs <= SEQS && parts(p.least) > 1 && units * parts(p.least) > 256 && line < 2147483648.0;
+  int64_t splits;
+  if (p.counted) {   // one sequence may have most of the keys
+    p.least = p.own ? OWN_LEAST : TILE_LEAST;
+    splits = (255 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
+  } else {
+    // Four rounds of workgroups (4 x 131072 keys: one round 398 us, four 383: the hardware hands them out as units come free); parts of fewer keys where that
+    // does not even make one (2 sequences of 1000 keys, 20 nodes: 22.7 us, 15.2).
+    if (!p.own && units * parts(512) <= 256)
+      while (p.least > 128 && units * parts(p.least - 128) <= 256) p.least -= 128;
+    splits = units > 0 ? (1023 + units) / units : 1;
+  }
+  if (splits > parts(p.least)) splits = parts(p.least);
+  // the workspace stays below 64 MB as far as the chip is full
   const int64_t room = (64ll << 20) / ((int64_t)a.nodes * a.q_heads * (a.head_dim + 2) * 4 + 1);
-  int64_t splits = units > 0 ? ((p.counted ? 2048 : 1024) + units - 1) / units : 1;
-  if (splits > most) splits = most;
   if (splits > room && splits * units > 512) splits = room * units > 512 ? room : (512 + units - 1) / units;
-  p.splits = splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
+  p.splits = splits < 1 ? 1 : splits > 63 ? 63 : (int)splits;
+  if (p.splits == 1) p.counted = false;
+  if (p.counted) ++p.splits;   // (a stretch may begin and end inside a part)
+  p.header = p.counted ? 4 + (a.n_seqs + 3) / 4 * 4 : 0;
   return p;
 }
 template <typename T, int DB>
 int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
   using TL = Tile<T, DB>;
+  const int unit = p.own ? 32 : Shared<T, DB, 4>::KEYS;
+  const TreeSplit t = {p.splits, p.least / unit, unit, p.own ? OWN_OVER : TILE_OVER, p.own ? 32 : 32 * p.waves, p.blocks, p.header};
   if (p.counted) {   // as many workgroups as run at a time: by LDS one on a compute unit, of the smallest heads two
     const dim3 grid(TL::PB == 128 && (p.own || p.waves == 4) ? 512 : 256);
-    if (p.own) tree_own_kernel<T, DB, true><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least, p.blocks);
-    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, true><<<grid, 256, 0, s>>>(a, p.splits, p.least, p.blocks);
-    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, true><<<grid, 512, 0, s>>>(a, p.splits, p.least, p.blocks);
+    if (p.own) tree_own_kernel<T, DB, true><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
+    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, true><<<grid, 256, 0, s>>>(a, t);
+    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, true><<<grid, 512, 0, s>>>(a, t);
   } else {
     const dim3 grid((uint32_t)(a.n_seqs * p.blocks), (uint32_t)a.kv_heads, (uint32_t)p.splits);
-    if (p.own) tree_own_kernel<T, DB, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, p.splits, p.least, p.blocks);
-    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, false><<<grid, 256, 0, s>>>(a, p.splits, p.least, p.blocks);
-    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, false><<<grid, 512, 0, s>>>(a, p.splits, p.least, p.blocks);
+    if (p.own) tree_own_kernel<T, DB, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
+    else if (p.waves == 4) tree_tile_kernel<T, DB, 4, false><<<grid, 256, 0, s>>>(a, t);
+    else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, false><<<grid, 512, 0, s>>>(a, t);
   }
+  constexpr int PER = DB <= 2 ? 1 : DB <= 4 ? 2 : 4;
   const int64_t all_rows = a.nodes * a.q_heads;
-  const int least = p.counted ? 0 : p.least;
-  if (p.splits > 16) tree_join_kernel<T, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, p.splits, least);
-  else if (p.splits > 1) tree_join_kernel<T, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, p.splits, least);
+  if (p.splits > 16 && all_rows <= 1024) tree_join_kernel<T, PER, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, t, p.counted);
+  else if (p.splits > 1) tree_join_kernel<T, PER, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, t, p.counted);
   return (int)hipGetLastError();
 }
 template <typename T>
@@ -1170,7 +1217,7 @@ int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream) {
 
 uint64_t tree_workspace(const fi_tree_attention_args& a) {
   const TreePlan p = plan_tree(a);
-  return p.splits > 1 ? (uint64_t)a.nodes * a.q_heads * p.splits * (a.head_dim + 2) * 4 + 16 : 0;
+  return p.splits > 1 ? ((uint64_t)a.nodes * a.q_heads * p.splits * (a.head_dim + 2) + p.header) * 4 : 0;
 }
 
 int launch_tree_attention(const fi_tree_attention_args& a, void* stream) {

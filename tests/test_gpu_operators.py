@@ -399,6 +399,33 @@ def test_tree_attention(torch, fi, dtype, cached, counts, page, hq, hk, d, layou
     assert got is not None
 
 
+LINES = [
+    # few long histories among short ones: workgroups take stretches that begin and end inside a sequence
+    ([3000 if i in (3, 17) else 40 * i % 700 for i in range(24)], [i % 4 for i in range(24)], 16, 16, 4, 128),
+    ([2900 if i == 5 else 60 * i for i in range(12)], [33 if i == 5 else 3 * i % 31 for i in range(12)], 64, 16, 4, 128),
+    ([0 if i else 2700 for i in range(14)], [12 - i % 13 for i in range(14)], 48, 32, 4, 72),
+    ([1500 if i == 199 else i % 11 for i in range(200)], [(i + 1) % 2 for i in range(200)], 16, 1, 1, 64),
+    ([9000, 5], [1, 2], 256, 8, 4, 128),
+    ([700 + 90 * i for i in range(9)], [40] * 9, 32, 8, 8, 64),
+    ([2000, 0, 2000, 1, 2000], [9, 0, 20, 0, 1], 16, 32, 16, 256),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cached,counts,page,hq,hk,d", LINES)
+def test_trees_of_ragged_histories(torch, fi, dtype, cached, counts, page, hq, hk, d):
+    g, kind = torch.Generator().manual_seed(sum(cached)), _kind(torch, dtype)
+    q, (k, v), table, dense, bits = _tree_case(torch, g, cached, counts, page, hq, hk, d, kind, "plain", "tree")
+    want, bound = _tree_ref(torch, q, dense, cached, counts, bits, d ** -0.5, dtype)
+    lengths, cu, longest = torch.tensor(cached, dtype=torch.int32).cuda(), _cu(torch, counts), max(c + n for c, n in zip(cached, counts))
+    for said in (longest, longest // 3, None):   # what is said about the lengths only guides how the work is shared out
+        out = torch.full(q.shape, math.nan, dtype=kind).cuda()
+        fi.tree_attention(q, k, v, table, lengths, cu, bits.cuda(), out=out, max_nodes=max(counts), max_length=said)
+        _inside(out.double().cpu(), want, bound)
+        again = fi.tree_attention(q, k, v, table, lengths, cu, bits.cuda(), max_nodes=max(counts), max_length=said)
+        assert torch.equal(again, out)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 72), ("f32", 64)])
 @pytest.mark.parametrize("counts", [[5, 9], [40, 64]])
 def test_a_branch_does_not_see_another(torch, fi, dtype, d, counts):
