@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
 // in the order that the first product leaves them in (key 8 g + 4 h + i is element 4 g + i of half h).
 // Keys and values come into LDS by direct loads, 16-byte pieces permuted at the source so that operand reads meet no bank twice; values are read
 // transposed (16 lanes get columns of 4 x 16 elements), fp32 ones column by column.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
@@ -361,17 +362,18 @@ struct Tile {
     add_values<KB>(st, s, tile, at);
   }
 
-  // The lane's outputs: o[db][4 g ..] are values 32 db + 8 g + 4 half .. of its query.
-  static __device__ __forceinline__ void store(const State& st, T* row, int D, float inv) {
+  // The lane's outputs, N blocks of values from block `from` on: o[b][4 g ..] are values 32 (from + b) + 8 g + 4 half .. of its query.
+  template <int N>
+  static __device__ __forceinline__ void store(const f32x16 (&o)[N], int from, T* row, int D, float inv) {
     const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int b = 0; b < N; ++b)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int d = db * 32 + 8 * g + 4 * half;
+        const int d = (from + b) * 32 + 8 * g + 4 * half;
         if (d >= D) continue;
-        if constexpr (F32) *reinterpret_cast<float4*>(row + d) = make_float4(st.o[db][4 * g] * inv, st.o[db][4 * g + 1] * inv, st.o[db][4 * g + 2] * inv, st.o[db][4 * g + 3] * inv);
-        else *reinterpret_cast<uint2*>(row + d) = make_uint2(pack_bf16x2(st.o[db][4 * g] * inv, st.o[db][4 * g + 1] * inv), pack_bf16x2(st.o[db][4 * g + 2] * inv, st.o[db][4 * g + 3] * inv));
+        if constexpr (F32) *reinterpret_cast<float4*>(row + d) = make_float4(o[b][4 * g] * inv, o[b][4 * g + 1] * inv, o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv);
+        else *reinterpret_cast<uint2*>(row + d) = make_uint2(pack_bf16x2(o[b][4 * g] * inv, o[b][4 * g + 1] * inv), pack_bf16x2(o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv));
       }
   }
 };
@@ -417,6 +419,148 @@ __device__ __forceinline__ bool prompt_work(const fi_prompt_attention_args& a, P
   w.keys = clamp_int(a.cu_k[lo + 1], w.k0, nk) - w.k0;
   w.first = (tile_id - (w.q0 / ROWS + lo)) * ROWS;
   return w.first >= 0 && w.first < w.rows;
+}
+
+// Few rows: every wave has the same 32 rows and keys of its own, 32 at a time, loaded by itself (no barriers); joined in LDS at the end.
+// SMALL, for many short histories: one wave and one tile in LDS, so that several workgroups are on a compute unit.
+template <typename T, int DB, bool SMALL = false>
+struct Own {
+  using TL = Tile<T, DB>;
+  static constexpr int BYTES = 2 * 32 * TL::PB;                                        // a tile
+  static constexpr int WAVES = SMALL ? 1 : TL::PB <= 256 ? 4 : TL::PB == 512 ? 2 : 1;  // 128 KB of tiles at most
+  static constexpr int BUFS = SMALL ? 1 : 2, LDS = BUFS * BYTES * WAVES + WAVES * 512;
+};
+// The tiles [first, end) of 32 keys.  query: the lane's; some query may not see all keys from `sure` on; find(t): where lane r's key of a tile is, asked for a
+// tile ahead, and offsets(place, ko, vo); visible(t): which of them the lane's query sees; strange(t0, t1): TL::add_strange for a wave's tiles.
+// A wave ends with the joined sums of some blocks of values.
+template <typename TL, int WAVES>
+struct Joined {
+  static constexpr int N = (TL::DB + WAVES - 1) / WAVES;   // (blocks past the last are not stored)
+  f32x16 o[N];
+  int from;
+  float top, total;
+};
+template <typename TL, typename T, int WAVES, int BUFS, typename Find, typename Offsets, typename Visible, typename Strange>
+__device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, const T* k, const T* v, const T* query, int D, float c, int first, int end, int sure, Find find,
+                                         Offsets offsets, Visible visible, Strange add_strange) {
+  constexpr int BYTES = 2 * 32 * TL::PB, DB = TL::DB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto share = [&](int x) { return first + (int)((int64_t)(end - first) * x / WAVES); };
+  const int t0 = share(wave), t1 = share(wave + 1);
+  typename TL::State st;
+  static_assert(BUFS == 2 || WAVES == 1, "the waves' sums fit the tiles");
+  uint8_t* const tiles = smem + wave * BUFS * BYTES;
+  clear_pads<TL, BUFS * BYTES * WAVES>(smem, D, 64 * WAVES);
+  u32x4 q[TL::KS];
+  TL::load_q(query, D, q);
+  typename TL::Addr at;
+  TL::addresses(at);
+  TL::clear(st);
+  decltype(find(0)) place{};
+  auto load = [&](int t) {
+    uint32_t mk, mv;
+    offsets(place, mk, mv);
+    TL::template load_tile<1, 1>(k, v, tiles + (t & (BUFS - 1)) * BYTES, 0, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
+      ko = __shfl(mk, r);
+      vo = __shfl(mv, r);
+    });
+    if (t + 1 < t1) place = find(t + 1);
+  };
+  bool strange = false;
+  if (t0 < t1) place = find(t0);
+  TL::have_q(q);
+  if (t0 < t1) load(t0);
+  for (int t = t0; t < t1; ++t) {
+    arrived();
+    if (BUFS > 1 && t + 1 < t1) load(t + 1);
+    uint8_t* const tile = tiles + (t & (BUFS - 1)) * BYTES;
+    if ((t + 1) * 32 > sure) strange |= __any(TL::template take_out<1>(tile, lane, 64)) != 0;
+    TL::template attend<1>(st, q, tile, at, c, (t + 1) * 32 > sure, [&](int) { return visible(t); });
+    if (BUFS == 1 && t + 1 < t1) {
+      arrived();   // (the tile has been read)
+      load(t + 1);
+    }
+  }
+  if (strange) add_strange(st, t0, t1);
+  const float total = both_halves(st.total);
+  if constexpr (WAVES == 1) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) r.o[db] = st.o[db];
+    r.from = 0;
+    r.top = st.top;
+    r.total = total;
+  } else {
+    // the waves' sums against the largest maximum, added in the order of the waves, some blocks by each
+    f32x4* const own = reinterpret_cast<f32x4*>(tiles) + lane;
+    float2* const stats = reinterpret_cast<float2*>(smem + 2 * BYTES * WAVES) + lane;
+    arrived();
+    if (t0 < t1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) own[(db * 4 + g) * 64] = f32x4{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+    }
+    stats[wave * 64] = make_float2(st.top, total);
+    __syncthreads();
+    float factor[WAVES];
+    r.top = stats[0].x;
+#pragma unroll
+    for (int x = 1; x < WAVES; ++x) r.top = fmaxf(r.top, stats[x * 64].x);
+    const float base = r.top == -INFINITY ? 0.0f : r.top;
+    r.total = 0.0f;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) {
+      factor[x] = __builtin_amdgcn_exp2f((stats[x * 64].x - base) * c);
+      r.total += stats[x * 64].y * factor[x];
+    }
+    r.from = wave * r.N;
+#pragma unroll
+    for (int b = 0; b < r.N; ++b) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) r.o[b][e] = 0.0f;
+      if (r.from + b >= DB) continue;
+#pragma unroll
+      for (int x = 0; x < WAVES; ++x) {
+        if (share(x) >= share(x + 1)) continue;
+        const f32x4* const other = reinterpret_cast<const f32x4*>(smem + x * 2 * BYTES) + lane;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 v4 = other[((r.from + b) * 4 + g) * 64];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.o[b][4 * g + i] += v4[i] * factor[x];
+        }
+      }
+    }
+  }
+}
+
+// Short prompts: 32 queries a workgroup, whose waves have keys of their own: four times the workgroups, each with a quarter of the walk.
+template <typename T, int DB, int DQ>
+__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) prompt_own_kernel(fi_prompt_attention_args a) {
+  using TL = Tile<T, DB, DQ>;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Own<T, DB>::LDS];
+  PromptWork w;
+  if (!prompt_work<32>(a, w)) return;
+  const int lane = threadIdx.x & 63, row = w.first + (lane & 31), mine = row < w.rows ? row : w.rows - 1, last = w.last(mine), least = w.last(w.first), most = w.last(w.first + 31);
+  const int D = a.head_dim, keys = w.keys;
+  const T* const k = static_cast<const T*>(a.k) + w.k0 * a.k_strides[0] + w.hk * a.k_strides[1];
+  const T* const v = static_cast<const T*>(a.v) + w.k0 * a.v_strides[0] + w.hk * a.v_strides[1];
+  const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
+  Joined<TL, Own<T, DB>::WAVES> r;
+  own_walk<TL, T, Own<T, DB>::WAVES, 2>(
+      r, smem, k, v, static_cast<const T*>(a.q) + (int64_t)(w.q0 + mine) * a.q_strides[0] + w.h * a.q_strides[1], D, a.scale * 1.44269504f, 0, (most + 32) / 32, least + 1,
+      [&](int t) { return (uint32_t)(t * 32 + (lane & 31) < keys ? t * 32 + (lane & 31) : keys - 1); },
+      [&](uint32_t key, uint32_t& ko, uint32_t& vo) {
+        ko = key * ks;
+        vo = key * vs;
+      },
+      [&](int t) { return low_bits(last + 1 - t * 32); },
+      [&](typename TL::State& st, int t0, int t1) {
+        const int masked = (least + 1) / 32 * 32;
+        TL::add_strange(st, D, t0 * 32 > masked ? t0 * 32 : masked, t1 * 32 <= most ? t1 * 32 : most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; },
+                        [&](int key) { return key <= last; });
+      });
+  if (row < w.rows) TL::store(r.o, r.from, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, r.total == 0.0f ? 0.0f : 1.0f / r.total);
 }
 
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
@@ -500,7 +644,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 ? 1 : 2) pr
   }
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
-  if (row < w.rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+  if (row < w.rows) TL::store(st.o, 0, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
 // Long prompts in bf16: 256 queries a workgroup, eight waves, four tiles in LDS of which three are on their way; the lanes' offsets of a whole tile stay in registers.
@@ -576,7 +720,7 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
   const float total = both_halves(st.total);
-  if (row < w.rows) TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
+  if (row < w.rows) TL::store(st.o, 0, static_cast<T*>(a.out) + (int64_t)(w.q0 + row) * a.out_strides[0] + w.h * a.out_strides[1], D, total == 0.0f ? 0.0f : 1.0f / total);
 }
 
 // What a workgroup of the tree kernels works on: a block of rows (node, head) of one key head of one sequence, and of its keys the tiles [t0, t1).
@@ -783,24 +927,25 @@ __device__ __forceinline__ void tree_strange(const fi_tree_attention_args& a, co
                   [&](int key) { return (tree_visible(a, w, node, words, key) & 1) != 0; });
 }
 
-template <typename TL, typename T>
-__device__ __forceinline__ void finish(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, typename TL::State& st, float total, bool there, int node, int head) {
+// Writes N blocks of values from block `from` on: results, or sums of a part.
+template <typename TL, typename T, int N>
+__device__ __forceinline__ void finish(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, const f32x16 (&o)[N], int from, float top, float total, bool there, int node, int head) {
   if (!there) return;
   if (w.splits == 1) {
-    TL::store(st, static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1], a.head_dim, total == 0.0f ? 0.0f : 1.0f / total);
+    TL::store(o, from, static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1], a.head_dim, total == 0.0f ? 0.0f : 1.0f / total);
     return;
   }
   const int64_t row = (int64_t)(w.n0 + node) * a.q_heads + head;
   float* const sums = part_sums(a, p, row, w.split);
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int db = 0; db < TL::DB; ++db)
+  for (int b = 0; b < N; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int d = db * 32 + 8 * g + 4 * half;
-      if (d < a.head_dim) *reinterpret_cast<float4*>(sums + d) = make_float4(st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]);
+      const int d = (from + b) * 32 + 8 * g + 4 * half;
+      if (d < a.head_dim) *reinterpret_cast<float4*>(sums + d) = make_float4(o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]);
     }
-  if (half == 0) *reinterpret_cast<float2*>(part_stats(a, p, row, w.split)) = make_float2(st.top, total);
+  if (half == 0 && from == 0) *reinterpret_cast<float2*>(part_stats(a, p, row, w.split)) = make_float2(top, total);
 }
 
 // Many rows: the waves have 32 rows each and share the tiles, as for a prompt, but few workgroups are there to hide each other's waiting: three tiles
@@ -883,7 +1028,7 @@ __device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, 
   }
   arrived();   // (page requests past the end)
   if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * KEYS, t1 * KEYS, KEYS);
-  finish<TL, T>(a, w, p, st, both_halves(st.total), row < rows, node, head);
+  finish<TL, T>(a, w, p, st.o, 0, st.top, both_halves(st.total), row < rows, node, head);
 }
 template <typename T, int DB, int WAVES, bool COUNTED>
 __global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attention_args a, TreeSplit p) {
@@ -901,112 +1046,40 @@ __global__ void __launch_bounds__(64 * WAVES, 1) tree_tile_kernel(fi_tree_attent
   }
 }
 
-// Few rows: every wave has the same 32 rows and keys of its own, 32 at a time, loaded by itself (no barriers); joined in LDS at the end.
-template <typename T, int DB>
-struct Own {
-  using TL = Tile<T, DB>;
-  static constexpr int BYTES = 2 * 32 * TL::PB;                                        // a tile
-  static constexpr int WAVES = TL::PB <= 256 ? 4 : TL::PB == 512 ? 2 : 1;              // 128 KB of tiles at most
-  static constexpr int LDS = 2 * BYTES * WAVES + WAVES * 512;
-};
-template <typename T, int DB>
+template <typename T, int DB, bool SMALL>
 __device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, const TreeWork& w, const TreeSplit& p, uint8_t* smem) {
   using TL = Tile<T, DB>;
-  constexpr int BYTES = Own<T, DB>::BYTES, WAVES = Own<T, DB>::WAVES;
   const int D = a.head_dim, group = a.q_heads / a.kv_heads;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
   const int rows = w.nodes * group, first = w.block * 32;
   if (first >= rows) return;
   const int row = first + (lane & 31), mine = row < rows ? row : rows - 1, node = mine / group, head = w.hk * group + mine % group;
-  const int t0 = w.t0 + (int)((int64_t)(w.t1 - w.t0) * wave / WAVES), t1 = w.t0 + (int)((int64_t)(w.t1 - w.t0) * (wave + 1) / WAVES);
   const T* const k = static_cast<const T*>(a.k_cache) + w.hk * a.k_strides[2];
   const T* const v = static_cast<const T*>(a.v_cache) + w.hk * a.v_strides[2];
   const Pages pages(a, w.b, TL::EP);
   const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
-  uint8_t* const tiles = smem + wave * 2 * BYTES;
-  clear_pads<TL, 2 * BYTES * WAVES>(smem, D, 64 * WAVES);
-  u32x4 q[TL::KS];
-  TL::load_q(static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, q);
-  typename TL::Addr at;
-  TL::addresses(at);
-  typename TL::State st;
-  TL::clear(st);
-  const float c = a.scale * 1.44269504f;
-  auto find = [&](int t) { return pages.find(t * 32 + (lane & 31) < w.keys ? t * 32 + (lane & 31) : w.keys - 1); };
-  typename Pages::Place place{0, 0};
-  auto load = [&](int t) {
-    uint32_t mk, mv;
-    pages.offsets(place, mk, mv);
-    TL::template load_tile<1, 1>(k, v, tiles + (t & 1) * BYTES, 0, D, [&](int, int r, uint32_t& ko, uint32_t& vo) {
-      ko = __shfl(mk, r);
-      vo = __shfl(mv, r);
-    });
-    if (t + 1 < t1) place = find(t + 1);
-  };
-  bool strange = false;
-  if (t0 < t1) place = find(t0);
-  TL::have_q(q);
-  if (t0 < t1) load(t0);
-  for (int t = t0; t < t1; ++t) {
-    arrived();
-    if (t + 1 < t1) load(t + 1);
-    uint8_t* const tile = tiles + (t & 1) * BYTES;
-    if ((t + 1) * 32 > w.cached) strange |= __any(TL::template take_out<1>(tile, lane, 64)) != 0;
-    TL::template attend<1>(st, q, tile, at, c, (t + 1) * 32 > w.cached, [&](int) { return tree_visible(a, w, node, words, t * 32); });
-  }
-  if (strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * 32, t1 * 32, 32);
-  float total = both_halves(st.total);
-  if constexpr (WAVES > 1) {
-    // the waves' sums against the largest maximum, added in the order of the waves by wave 0
-    float* const own = reinterpret_cast<float*>(smem + wave * 2 * BYTES);
-    float2* const stats = reinterpret_cast<float2*>(smem + 2 * BYTES * WAVES);
-    arrived();
-    if (wave) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) own[(db * 16 + e) * 64 + lane] = st.o[db][e];
-    }
-    stats[wave * 64 + lane] = make_float2(st.top, total);
-    __syncthreads();
-    if (wave) return;
-    float top = st.top;
-#pragma unroll
-    for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[x * 64 + lane].x);
-    const float base = top == -INFINITY ? 0.0f : top;
-    const float f0 = __builtin_amdgcn_exp2f((st.top - base) * c);
-    total *= f0;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) st.o[db][e] *= f0;
-#pragma unroll
-    for (int x = 1; x < WAVES; ++x) {
-      const float f = __builtin_amdgcn_exp2f((stats[x * 64 + lane].x - base) * c);
-      total += stats[x * 64 + lane].y * f;
-      const float* const other = reinterpret_cast<const float*>(smem + x * 2 * BYTES);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) st.o[db][e] += other[(db * 16 + e) * 64 + lane] * f;
-    }
-    st.top = top;
-  }
-  finish<TL, T>(a, w, p, st, total, row < rows, node, head);
+  using O = Own<T, DB, SMALL>;
+  Joined<TL, O::WAVES> r;
+  own_walk<TL, T, O::WAVES, O::BUFS>(
+      r, smem, k, v, static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, a.scale * 1.44269504f, w.t0, w.t1, w.cached,
+      [&](int t) { return pages.find(t * 32 + (lane & 31) < w.keys ? t * 32 + (lane & 31) : w.keys - 1); },
+      [&](const Pages::Place& place, uint32_t& ko, uint32_t& vo) { pages.offsets(place, ko, vo); }, [&](int t) { return tree_visible(a, w, node, words, t * 32); },
+      [&](typename TL::State& st, int t0, int t1) { tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * 32, t1 * 32, 32); });
+  finish<TL, T>(a, w, p, r.o, r.from, r.top, r.total, row < rows, node, head);
 }
-template <typename T, int DB, bool COUNTED>
-__global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, TreeSplit p) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[Own<T, DB>::LDS];
+template <typename T, int DB, bool COUNTED, bool SMALL>
+__global__ void __launch_bounds__((64 * Own<T, DB, SMALL>::WAVES), 1) tree_own_kernel(fi_tree_attention_args a, TreeSplit p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Own<T, DB, SMALL>::LDS];
   if constexpr (COUNTED) {
     __shared__ TreeLine line;
     line_up(a, p, line);
     along_the_line(a, p, line, [&](const TreeWork& w) {
       __syncthreads();   // (the piece before has been read to the end)
-      tree_own_work<T, DB>(a, w, p, smem);
+      tree_own_work<T, DB, SMALL>(a, w, p, smem);
     });
   } else {
     TreeWork w;
-    if (tree_direct(a, p, w)) tree_own_work<T, DB>(a, w, p, smem);
+    if (tree_direct(a, p, w)) tree_own_work<T, DB, SMALL>(a, w, p, smem);
   }
 }
 
@@ -1096,8 +1169,17 @@ bool prompt_on_tiles(const fi_prompt_attention_args& a) {
 bool prompt_is_long(const fi_prompt_attention_args& a) {
   return a.dtype == FI_BF16 && a.head_dim <= 128 && (a.q_tokens / LONG_ROWS) * a.q_heads >= LONG_GROUPS && a.k_strides[0] < 1 << 24 && a.v_strides[0] < 1 << 24;
 }
+// Workgroups of 32 queries up to which they are taken (us, 128 queries / 32; 12 heads, sequences spread over their logarithm).  bf16, heads of 64, two on a compute unit: 7 up to
+// 301 tokens, 346 workgroups, 8.8 / 7.4; up to 1000, 720: 16.1 / 14.6; up to 2000, 1200: 25.8 / 30.6.  Of 128, one on a unit: 256 tokens, 108: 12.2 / 8.7; 346: 11.5 / 12.8;
+// of 256: 17.6 / 13.7.  fp32, bound by its products until every unit has some: heads of 64, 346: 28 / 15.5; of 80, 720: 107 / 94; 4 images, 1088: 82 / 195; of 256 46.7 / 49.1.
+template <typename T, int DB>
+constexpr int own_most() { return sizeof(T) == 4 ? (DB <= 4 ? 768 : 0) : DB == 2 ? 768 : 256; }
 template <typename T, int DB, int DQ>
 void prompt_waves(const fi_prompt_attention_args& a, dim3 grid, bool two, hipStream_t s) {
+  const int64_t small = (a.q_tokens / 32 + a.n_seqs) * a.q_heads;
+  if constexpr (own_most<T, DB>() > 0) {
+    if (small <= own_most<T, DB>()) return (void)(prompt_own_kernel<T, DB, DQ><<<dim3((uint32_t)small), 64 * Own<T, DB>::WAVES, 0, s>>>(a));
+  }
   if constexpr (sizeof(T) == 2 && DB <= 4) {
     if (two) return (void)(prompt_tile_kernel<T, DB, 2, DQ><<<grid, 128 * PROMPT_WAVES, 0, s>>>(a));
   }
@@ -1117,9 +1199,10 @@ int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
       return (int)hipGetLastError();
     }
   }
-  // two groups where there is a workgroup or so per compute unit, and a walk is long
+  // two groups where there is a workgroup or so per compute unit, and a walk is long (12 heads, 7 sequences up to 1000 tokens, spread over their logarithm: heads of 64 19.8 us
+  // with one group, 16.4; of 128 27.1, 25.7; up to 301: 8.7, 8.4; 11.5, 12.7)
   const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
-  const bool two = (int64_t)grid.x < 512 && a.k_tokens >= 512 * (int64_t)a.n_seqs;
+  const bool two = (int64_t)grid.x < 512 && a.k_tokens >= (db == 2 ? 128 : 256) * (int64_t)a.n_seqs;
   if (db == 2) prompt_waves<T, 2, 64>(a, grid, two, s);
   else if (db == 3 && a.head_dim <= 80) prompt_waves<T, 3, 80>(a, grid, two, s);
   else if (db == 3) prompt_waves<T, 3, 96>(a, grid, two, s);
@@ -1137,19 +1220,26 @@ bool tree_on_tiles(const fi_tree_attention_args& a) {
 
 // How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 or 256 that
 // share them; parts of every sequence's keys, and the least keys of a part.
-struct TreePlan { bool own, counted; int waves, blocks, splits, least, header; };
+struct TreePlan { bool own, small, counted; int waves, blocks, splits, least, header; };
 TreePlan plan_tree(const fi_tree_attention_args& a) {
   TreePlan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
-  p.own = rows <= 32;
   p.waves = rows <= 128 || a.head_dim > 128 ? 4 : 8;
+  // Blocks of 32 rows with keys of their own, too, where the workgroups are few (us, shared / own; 64 nodes of one sequence of 100 keys, 8 heads 17.3 / 12.6), or keys are and
+  // the workgroups many (about 10 keys, 40 nodes: 61 sequences of 32 heads 53 / 25, 16 nodes of 8 heads 15.8 / 10.9; 12 sequences, 60 keys 12.0 / 13.8).
+  const int64_t streams = (int64_t)a.n_seqs * a.kv_heads;
+  p.own = rows <= 32 || streams * ((rows + 31) / 32) * (((int64_t)a.max_length + 127) / 128) <= 256 ||
+          (a.max_length <= 256 && streams * ((rows + 32 * p.waves - 1) / (32 * p.waves)) > 256);
   const int64_t per_block = p.own ? 32 : 32 * p.waves;
   p.blocks = (int)((rows + per_block - 1) / per_block);
-  const int64_t units = (int64_t)a.n_seqs * a.kv_heads * p.blocks;
+  const int64_t units = streams * p.blocks;
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
   p.least = p.own ? 128 : 512;
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
   p.counted = a.n_seqs > 1 && a.n_seqs <= SEQS && parts(p.least) > 1 && units * parts(p.least) > 256 && line < 2147483648.0;
+  // One wave, several workgroups on a compute unit (us, else / so; one node of 14 sequences of 32 heads: 7 keys 12.7 / 7.4, 100 keys 15.9 / 13.4; 64 of 32: 120 keys 64 / 32,
+  // 240 85 / 56; 64 of 8: 240 keys 21.2 / 21.4; 12 nodes of 61 sequences of 32 heads, no history 46 / 10).
+  p.small = p.own && (a.max_length <= 32 || (a.max_length <= 128 && units > 256) || (a.max_length <= 256 && units > 1024));
   int64_t splits;
   if (p.counted) {   // one sequence may have most of the keys
     p.least = p.own ? OWN_LEAST : TILE_LEAST;
@@ -1168,6 +1258,7 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   p.splits = splits < 1 ? 1 : splits > 63 ? 63 : (int)splits;
   if (p.splits == 1) p.counted = false;
   if (p.counted) ++p.splits;   // (a stretch may begin and end inside a part)
+  if (p.small) p.counted = false, p.splits = 1;
   p.header = p.counted ? 4 + (a.n_seqs + 3) / 4 * 4 : 0;
   return p;
 }
@@ -1178,12 +1269,13 @@ int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream
   const TreeSplit t = {p.splits, p.least / unit, unit, p.own ? OWN_OVER : TILE_OVER, p.own ? 32 : 32 * p.waves, p.blocks, p.header};
   if (p.counted) {   // as many workgroups as run at a time: by LDS one on a compute unit, of the smallest heads two
     const dim3 grid(TL::PB == 128 && (p.own || p.waves == 4) ? 512 : 256);
-    if (p.own) tree_own_kernel<T, DB, true><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
+    if (p.own) tree_own_kernel<T, DB, true, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
     else if (p.waves == 4) tree_tile_kernel<T, DB, 4, true><<<grid, 256, 0, s>>>(a, t);
     else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, true><<<grid, 512, 0, s>>>(a, t);
   } else {
     const dim3 grid((uint32_t)(a.n_seqs * p.blocks), (uint32_t)a.kv_heads, (uint32_t)p.splits);
-    if (p.own) tree_own_kernel<T, DB, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
+    if (p.own && p.small) tree_own_kernel<T, DB, false, true><<<grid, 64, 0, s>>>(a, t);
+    else if (p.own) tree_own_kernel<T, DB, false, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
     else if (p.waves == 4) tree_tile_kernel<T, DB, 4, false><<<grid, 256, 0, s>>>(a, t);
     else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, false><<<grid, 512, 0, s>>>(a, t);
   }
