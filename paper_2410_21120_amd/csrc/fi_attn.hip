@@ -567,9 +567,10 @@ constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
 
 // A workgroup has 128 queries of a head and walks the keys they see, 64 (32) at a time, two tiles in LDS; two workgroups on a compute unit.  GROUPS 2, for calls that
 // do not fill the chip: two groups of four waves have the same queries, one the even tiles, one the odd, joined in LDS at the end (bf16, causal, us with one / two:
-// 512 tokens of 8 heads of 64 12.2 / 10.9, 2048 33 / 25; heads of 128: 512 16.4 / 16.4, 2048 47 / 43; fp32 is bound by its products, 91 / 94).
+// 512 tokens of 8 heads of 64 12.2 / 10.9, 2048 33 / 25; heads of 128: 512 16.4 / 16.4, 2048 47 / 43; fp32 is bound by its products, 91 / 94; of heads of 256 the registers of two
+// groups do not fit, 124 / 298).  Heads of 256 in bf16 take all 256 registers so that two workgroups fit (12 heads, 6000 tokens: 462 us with one, 355).
 template <typename T, int DB, int GROUPS, int DQ>
-__global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
+__global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 && sizeof(T) == 4 ? 1 : 2) prompt_tile_kernel(fi_prompt_attention_args a) {
   constexpr int WAVES = PROMPT_WAVES;
   using TL = Tile<T, DB, DQ>;
   constexpr int KB = TL::PB <= 256 ? 2 : 1, KEYS = 32 * KB, BYTES = 2 * KEYS * TL::PB;
@@ -748,9 +749,11 @@ __device__ __forceinline__ void tree_sequence(const fi_tree_attention_args& a, i
 //  Lengths up to 8000, spread over their logarithm: 16 sequences of 32 key heads direct 253 us, counted 90; 64 of 8 key heads and ten nodes 344, 114; the last
 //  with 8000 keys each 428, 479; 2 of 1000 keys 12, 19.
 constexpr int SEQS = 256;   // most sequences that are counted
-// Counted: the least keys of a stretch (12 sequences up to 5001 keys: one node, 128 keys 30.4 us, 256 26.5; up to 500 keys, 37 nodes: 128 27.8, 512 36.2), and what a
-// stream's beginning counts for, in tiles of 64 or 32 keys (up to 20000 keys: 37 nodes, 1 tile 114 us, 3 85, 5 84; one node, 8 tiles 74, 14 and 20 55).
-constexpr int TILE_LEAST = 128, OWN_LEAST = 256, TILE_OVER = 5, OWN_OVER = 20;
+// Counted: the least keys of a stretch, and what a stream's beginning counts for, in tiles (64 keys, of own waves 32; fp32 tiles take longer).  12 sequences, lengths spread
+// over their logarithm, us: one node, least 128 keys 30.4, 256 26.5 up to 5001 keys; beginnings of 4, 8, 10, 20 tiles 63, 49, 49, 50 up to 20000; 37 nodes, of 1, 3, 5 tiles
+// 114, 85, 84; 10 sequences of 32 heads of 72, fp32, up to 1302 keys, of 4, 8, 20 tiles 47, 57, 85.
+struct Stretch { int least, over; };
+constexpr Stretch stretch(bool own, bool f32) { return own ? (f32 ? Stretch{128, 4} : Stretch{256, 12}) : (f32 ? Stretch{128, 1} : Stretch{128, 4}); }
 struct TreeLine {
   int start[SEQS];   // where a sequence begins
   int n0[SEQS], nodes[SEQS], cached[SEQS], keys[SEQS];
@@ -1242,7 +1245,7 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   p.small = p.own && (a.max_length <= 32 || (a.max_length <= 128 && units > 256) || (a.max_length <= 256 && units > 1024));
   int64_t splits;
   if (p.counted) {   // one sequence may have most of the keys
-    p.least = p.own ? OWN_LEAST : TILE_LEAST;
+    p.least = stretch(p.own, a.dtype == FI_F32).least;
     splits = (255 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
   } else {
     // Four rounds of workgroups (4 x 131072 keys: one round 398 us, four 383: the hardware hands them out as units come free); parts of fewer keys where that
@@ -1266,7 +1269,7 @@ template <typename T, int DB>
 int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
   using TL = Tile<T, DB>;
   const int unit = p.own ? 32 : Shared<T, DB, 4>::KEYS;
-  const TreeSplit t = {p.splits, p.least / unit, unit, p.own ? OWN_OVER : TILE_OVER, p.own ? 32 : 32 * p.waves, p.blocks, p.header};
+  const TreeSplit t = {p.splits, p.least / unit, unit, stretch(p.own, TL::F32).over, p.own ? 32 : 32 * p.waves, p.blocks, p.header};
   if (p.counted) {   // as many workgroups as run at a time: by LDS one on a compute unit, of the smallest heads two
     const dim3 grid(TL::PB == 128 && (p.own || p.waves == 4) ? 512 : 256);
     if (p.own) tree_own_kernel<T, DB, true, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
