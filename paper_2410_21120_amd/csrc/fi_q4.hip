@@ -620,7 +620,7 @@ Plan plan(const fi_q4_matmul_args& a) {
     p.kernel = WIDE;
     p.mb = a.rows > 16 ? 2 : 1;
     const int64_t groups = blocks * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
-    int64_t splits = groups > 0 ? (256 + groups - 1) / groups : 1;   // a workgroup per compute unit
+    int64_t splits = groups > 0 ? 256 / groups : 1;                   // a workgroup per compute unit at most: they run one at a time
     if (splits > steps / 4) splits = steps / 4;                       // (a join costs about as much as four steps)
     p.splits = splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
   } else if ((a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && (a.rows <= 4 || (a.rows <= 16 && a.outputs < 2048)))) {

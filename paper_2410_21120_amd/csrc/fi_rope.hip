@@ -3,8 +3,9 @@
 // y = rotate(x * w / sqrt(mean(x^2) + eps)).  Every value is read once and written once, so HBM bounds it, if the vector unit is kept from doing so.  A head's
 // row is held by a group of lanes, in registers from the load to the store: a lane has NP pairs (both halves of each, whichever way pairs are
 // formed) or 2 NP of the values behind the rotated part, so a rotation needs no neighbour, and the mean is one reduction over the group (in the
-// registers' own rotations: 4 additions for 16 lanes).  The lane keeps its pairs from head to head of a token: a wave computes each sine once (one per lane,
-// handed out through LDS), and weight, cosine and sine become two factors per value before the first head.
+// registers' own rotations: 4 additions for 16 lanes).  The lane keeps its pairs from head to head of a token: each sine is computed once (one per lane, handed out
+// through LDS to the waves of a workgroup that share the token: for each wave again, 500 tokens took 13.4 us, not 6.6), and weight, cosine and sine become two
+// factors per value before the first head.
 #include <hip/hip_runtime.h>
 
 #include "fi_device.h"
@@ -13,7 +14,9 @@
 namespace fi {
 namespace {
 
-constexpr int64_t FEWEST_WAVES = 4096;   // waves of a call, where it has rows for them (2187 tokens of 48 fp32 heads of 72: 2048 18 us, 4096 17, 8192 20)
+// Waves of a call, where it has rows for them, at least (2187 tokens of 48 fp32 heads of 72: one wave a token 15.7 us, two 14.4; 3000 of 20 heads of 128 13.8, 14.9), and
+// up to which waves without a row in their last turn cost nothing (64 tokens of 48 bf16 heads of 128: 8 waves a token 4.3 us, 16 3.9; 903 of 20: 4 waves 5.6, 8 8.2).
+constexpr int64_t FEWEST_WAVES = 2560, LATENCY_WAVES = 1024;
 constexpr int HEADS = 4;                 // rows that a group has in flight (16384 tokens of 48 bf16 heads of 128: one 101 us, two 95, three 88, four 88)
 
 template <typename T, int N>
@@ -39,19 +42,22 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
   return v;
 }
 
-// NP pairs per lane; ITEMS runs of them per lane (2: one pair at a time, rows that are not a whole number of longer runs).  INTER: pair t of a run is its values
-// 2 t and 2 t + 1, else value t of each half.  lanes: of a group, 1 << wave_bits: waves that share a token.
+// NP pairs per lane; ITEMS of them (2: one pair at a time, rows that are not a whole number of longer runs).  A lane's values are two runs of NP, the same run of
+// each half.  INTER: pairs are neighbours, inside the runs, else value t of one run and of the other.  lanes: of a group, 1 << wave_bits: waves that share a token.
 template <typename T, int NP, int ITEMS, bool INTER>
 __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int lanes, int wave_bits) {
   __shared__ float2 turns[4][FI_MAX_HEAD_DIM / 2];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, D = a.head_dim, half = a.rot_dim / 2;
   const uint32_t wave = blockIdx.x * 4 + w;
   const int token = (int)(wave >> wave_bits), part = (int)(wave & ((1u << wave_bits) - 1u));
-  if (token >= a.tokens) return;
   const int shift = __builtin_ctz(lanes), group = (part << (6 - shift)) + (lane >> shift), groups = 64 >> shift << wave_bits, in_group = lane & (lanes - 1);
   const int turned = half / NP;                                       // runs of the rotated part
   const int items = turned + (D - a.rot_dim + 2 * NP - 1) / (2 * NP); // and of the whole row
-  for (int pair = lane; pair < half; pair += 64) {
+  // The sines of a token, once for the two or four waves of a workgroup that share it.
+  const int sharing = wave_bits >= 2 ? 4 : 1 << wave_bits;
+  float2* const turn_of = turns[w & ~(sharing - 1)];
+  const int first_pair = token < a.tokens ? lane + 64 * (w & (sharing - 1)) : half;
+  for (int pair = first_pair; pair < half; pair += 64 * sharing) {
     int axis = 0, end = a.sections[0];
 #pragma unroll
     for (int x = 1; x < FI_MAX_AXES; ++x)
@@ -59,9 +65,11 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
     // the angle is one fp32 product, as models form it when they are trained
     float2 t;
     sincosf((float)a.positions[(int64_t)token * a.n_axes + axis] * a.inv_freq[pair], &t.y, &t.x);
-    turns[w][pair] = t;
+    turn_of[pair] = t;
   }
-  asm volatile("" ::: "memory");   // (a wave's writes and reads of LDS are done in order)
+  if (sharing > 1) __syncthreads();
+  else asm volatile("" ::: "memory");   // (a wave's writes and reads of LDS are done in order)
+  if (token >= a.tokens) return;
 
   int first[ITEMS], second[ITEMS];   // where the lane's values stand in a row; an absent value: -1
   bool turn[ITEMS];
@@ -73,8 +81,8 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
     first[u] = second[u] = -1;
     turn[u] = item < turned;
     if (turn[u]) {
-      first[u] = INTER ? item * 2 * NP : item * NP;
-      second[u] = INTER ? first[u] + NP : half + first[u];
+      first[u] = INTER && NP == 1 ? 2 * item : item * NP;
+      second[u] = INTER && NP == 1 ? first[u] + 1 : half + first[u];
     } else if (item < items) {
       first[u] = a.rot_dim + (item - turned) * 2 * NP;
       second[u] = first[u] + NP < D ? first[u] + NP : -1;   // (an odd row's last value, one pair at a time)
@@ -84,15 +92,14 @@ __global__ void __launch_bounds__(256) rope_kernel(fi_qk_norm_rope_args a, int l
       const float* const weight = x ? a.k_weight : a.q_weight;
       float wt[2 * NP];
 #pragma unroll
-      for (int t = 0; t < 2 * NP; ++t) {
-        const int at = (t < NP ? first[u] : second[u]) + t % NP;
-        const bool there = t < NP ? first[u] >= 0 : second[u] >= 0;
-        wt[t] = there && weight ? weight[at] : 1.0f;
-      }
+      for (int t = 0; t < 2 * NP; ++t) wt[t] = 1.0f;
+      if (weight && first[u] >= 0) __builtin_memcpy(wt, weight + first[u], NP * 4);
+      if (weight && second[u] >= 0) __builtin_memcpy(wt + NP, weight + second[u], NP * 4);
 #pragma unroll
       for (int t = 0; t < NP; ++t) {
-        const float2 cs = turn[u] ? turns[w][item * NP + t] : make_float2(1.0f, 0.0f);
         const int i = INTER ? 2 * t : t, j = INTER ? 2 * t + 1 : NP + t;
+        const int pair = INTER && NP > 1 ? (2 * t < NP ? first[u] : second[u] - NP) / 2 + t : item * NP + t;   // (runs start on even values)
+        const float2 cs = turn[u] ? turn_of[pair] : make_float2(1.0f, 0.0f);
         own[x][u][i] = wt[i] * cs.x;
         other[x][u][i] = -wt[j] * cs.y;
         own[x][u][j] = wt[j] * cs.x;
@@ -204,7 +211,8 @@ int launch_np(const fi_qk_norm_rope_args& a, hipStream_t s) {
   // A wave per token does the fewest preparations; with few tokens more waves share one, down to a row per group.
   const int heads = a.q_heads + a.kv_heads * (a.v ? 2 : 1), most = (heads + 64 / lanes - 1) / (64 / lanes);
   int bits = 0;
-  while (1 << bits < most && ((int64_t)a.tokens << bits) < FEWEST_WAVES) ++bits;
+  auto waves = [&] { return (int64_t)a.tokens << bits; };
+  while ((2 << bits <= most && waves() < FEWEST_WAVES) || (1 << bits < most && waves() < LATENCY_WAVES)) ++bits;
   const dim3 grid((uint32_t)((((int64_t)a.tokens << bits) + 3) / 4));
   if (a.interleaved) rope_kernel<T, NP, ITEMS, true><<<grid, 256, 0, s>>>(a, lanes, bits);
   else rope_kernel<T, NP, ITEMS, false><<<grid, 256, 0, s>>>(a, lanes, bits);
