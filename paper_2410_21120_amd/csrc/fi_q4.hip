@@ -607,15 +607,16 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
 //  FEW:  reads 2048 inputs a step; its time grows with rows x outputs (us, few / tile: 4096 x 1000 inputs x outputs, 1 row 3.2 / 8.4, 4 rows 5.2 / 9.1, 16 rows 7.9 / 11.3;
 //        4096 x 4096, 4 rows 7.8 / 10.0, 8 rows 10.9 / 10.8; 1024 x 16384, 2 rows 8.2 / 8.2, 4 rows 12.6 / 8.4; 512 x 8192, 1 row 4.2 / 3.6).
 //  WIDE: has two launches and about 8 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 12.0 / 11.8, 20 rows 13.6 / 19.4;
-//        1024 x 16384, 16 rows 12.3 / 8.8, 20 rows 14.1 / 15.4; 4096 x 8192, 8 rows 13.7 / 19.2; 4096 x 300, 20 rows 11.0 / 10.9; 8192 x 300, 20 rows 11.4 / 19.8; wide / few:
-//        8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4).
+//        1024 x 16384, 16 rows 12.3 / 8.8, 20 rows 14.1 / 15.4; 4096 x 8192, 8 rows 13.7 / 19.2; 2048 x 8666, 5 rows 12.8 / 22.4; 4096 x 300, 20 rows 11.0 / 10.9; 8192 x 300, 20 rows 11.4 / 19.8; wide / few:
+//        8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4; 16384 x 4096, 4 rows 18.8 / 19.8, 25088 x 4096 26.0 / 29.7, 8192 x 8192 17.7 / 17.3).
 enum Kernel { FEW, TILE, WIDE };
 struct Plan { Kernel kernel; int mb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
   Plan p = {TILE, 1, 1};
   const int64_t weights = (int64_t)a.inputs * a.outputs, blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
-  const bool wide = a.dtype == FI_BF16 && a.rows > 4 &&
-                    (weights * ((a.rows + 15) / 16) >= 3 << 23 || a.inputs >= 12288 || (a.inputs >= 8192 && a.rows > 16));
+  const bool wide = a.dtype == FI_BF16 && a.rows > (a.inputs >= 16384 ? 2 : 4) &&
+                    (weights * ((a.rows + 15) / 16) >= 3 << 23 || a.inputs >= 12288 || (a.inputs >= 8192 && a.rows > 16) ||
+                     (a.inputs >= 2048 && a.outputs > 8192));
   if (wide) {
     p.kernel = WIDE;
     p.mb = a.rows > 16 ? 2 : 1;
@@ -682,7 +683,9 @@ int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
     else launch_wide<2>(a, p, s);
     const uint32_t blocks = (uint32_t)((a.outputs + 255) / 256);
     if (p.splits > 1) q4_join_kernel<T><<<dim3(blocks * (uint32_t)a.rows), 256, 0, s>>>(a, p.splits, blocks);
-  } else if (a.outputs >= 16384) {   // (four blocks of outputs share the rows' inputs; fewer leave compute units without work)
+  } else if (a.outputs >= 16384 || (sizeof(T) == 4 && a.outputs >= 8192 && (a.inputs >= 2048 || a.rows > 16))) {
+    // four blocks of outputs share what is made of the rows' inputs, which is most of the work in fp32 (2048 x 12000, 64 rows 126 us, 82; 5 rows 27.1, 26.6; 1024 x 8200, 5 rows
+    // 11.8, 14.9); fewer leave compute units without work
     launch_tiles<T, 4, 8>(a, vw, s);
   } else if (a.inputs >= 2048) {
     launch_tiles<T, 1, 16>(a, vw, s);
