@@ -426,9 +426,11 @@ __device__ __forceinline__ bool prompt_work(const fi_prompt_attention_args& a, P
 template <typename T, int DB, bool SMALL = false>
 struct Own {
   using TL = Tile<T, DB>;
-  static constexpr int BYTES = 2 * 32 * TL::PB;                                        // a tile
-  static constexpr int WAVES = SMALL ? 1 : TL::PB <= 256 ? 4 : TL::PB == 512 ? 2 : 1;  // 128 KB of tiles at most
-  static constexpr int BUFS = SMALL ? 1 : 2, LDS = BUFS * BYTES * WAVES + WAVES * 512;
+  static constexpr int BYTES = 2 * 32 * TL::PB;   // a tile
+  // 128 KB of tiles at most: waves before a second tile each, so that all four matrix units are at work (12 fp32 heads of 128, 7 prompts up to 301 tokens: two waves with two
+  // tiles 34 us, four with one 25; 4 x 100000 keys of 8 bf16 heads of 256, one node: 172, 176)
+  static constexpr int WAVES = SMALL ? 1 : TL::PB <= 512 ? 4 : 2;
+  static constexpr int BUFS = SMALL || TL::PB >= 512 ? 1 : 2, LDS = BUFS * BYTES * WAVES + WAVES * 512;
 };
 // The tiles [first, end) of 32 keys.  query: the lane's; some query may not see all keys from `sure` on; find(t): where lane r's key of a tile is, asked for a
 // tile ahead, and offsets(place, ko, vo); visible(t): which of them the lane's query sees; strange(t0, t1): TL::add_strange for a wave's tiles.
@@ -448,7 +450,7 @@ __device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, co
   auto share = [&](int x) { return first + (int)((int64_t)(end - first) * x / WAVES); };
   const int t0 = share(wave), t1 = share(wave + 1);
   typename TL::State st;
-  static_assert(BUFS == 2 || WAVES == 1, "the waves' sums fit the tiles");
+  static_assert(WAVES == 1 || DB * 4096 <= BUFS * BYTES, "a wave's sums fit its tiles");
   uint8_t* const tiles = smem + wave * BUFS * BYTES;
   clear_pads<TL, BUFS * BYTES * WAVES>(smem, D, 64 * WAVES);
   u32x4 q[TL::KS];
@@ -492,7 +494,7 @@ __device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, co
   } else {
     // the waves' sums against the largest maximum, added in the order of the waves, some blocks by each
     f32x4* const own = reinterpret_cast<f32x4*>(tiles) + lane;
-    float2* const stats = reinterpret_cast<float2*>(smem + 2 * BYTES * WAVES) + lane;
+    float2* const stats = reinterpret_cast<float2*>(smem + BUFS * BYTES * WAVES) + lane;
     arrived();
     if (t0 < t1) {
 #pragma unroll
@@ -522,7 +524,7 @@ __device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, co
 #pragma unroll
       for (int x = 0; x < WAVES; ++x) {
         if (share(x) >= share(x + 1)) continue;
-        const f32x4* const other = reinterpret_cast<const f32x4*>(smem + x * 2 * BYTES) + lane;
+        const f32x4* const other = reinterpret_cast<const f32x4*>(smem + x * BUFS * BYTES) + lane;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const f32x4 v4 = other[((r.from + b) * 4 + g) * 64];
@@ -547,7 +549,7 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) prompt_own_kernel
   const T* const v = static_cast<const T*>(a.v) + w.k0 * a.v_strides[0] + w.hk * a.v_strides[1];
   const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
   Joined<TL, Own<T, DB>::WAVES> r;
-  own_walk<TL, T, Own<T, DB>::WAVES, 2>(
+  own_walk<TL, T, Own<T, DB>::WAVES, Own<T, DB>::BUFS>(
       r, smem, k, v, static_cast<const T*>(a.q) + (int64_t)(w.q0 + mine) * a.q_strides[0] + w.h * a.q_strides[1], D, a.scale * 1.44269504f, 0, (most + 32) / 32, least + 1,
       [&](int t) { return (uint32_t)(t * 32 + (lane & 31) < keys ? t * 32 + (lane & 31) : keys - 1); },
       [&](uint32_t key, uint32_t& ko, uint32_t& vo) {
@@ -1172,17 +1174,20 @@ bool prompt_on_tiles(const fi_prompt_attention_args& a) {
 bool prompt_is_long(const fi_prompt_attention_args& a) {
   return a.dtype == FI_BF16 && a.head_dim <= 128 && (a.q_tokens / LONG_ROWS) * a.q_heads >= LONG_GROUPS && a.k_strides[0] < 1 << 24 && a.v_strides[0] < 1 << 24;
 }
-// Workgroups of 32 queries up to which they are taken (us, 128 queries / 32; 12 heads, sequences spread over their logarithm).  bf16, heads of 64, two on a compute unit: 7 up to
-// 301 tokens, 346 workgroups, 8.8 / 7.4; up to 1000, 720: 16.1 / 14.6; up to 2000, 1200: 25.8 / 30.6.  Of 128, one on a unit: 256 tokens, 108: 12.2 / 8.7; 346: 11.5 / 12.8;
-// of 256: 17.6 / 13.7.  fp32, bound by its products until every unit has some: heads of 64, 346: 28 / 15.5; of 80, 720: 107 / 94; 4 images, 1088: 82 / 195; of 256 46.7 / 49.1.
+// Workgroups of 32 queries up to which they are taken (us, 128 queries / 32; 12 heads, sequences spread over their logarithm, causal).  bf16, heads of 64, two on a compute unit:
+// 7 up to 301 tokens, 276 workgroups, 8.8 / 7.1; up to 1000, 684: 16.1 / 14.6; up to 2000, 1200: 25.8 / 30.6.  Of 128, one on a unit: 256 tokens, 108: 12.2 / 8.7; 7 up to 301: 11.5 / 12.8.
+// Of 256: 7 up to 100 17.3 / 12.8; one of 2000, 756: 123 / 106.  fp32, bound by its products: heads of 128, 7 up to 301 48 / 25; one of 3000, 1128: 439 / 336; of 256, 7 up to 1000
+// 284 / 214.  Without a causal mask all walks of a sequence are as long and sharing them counts for more: 4 images of up to 729 fp32 patches, 16 heads of 72, 960: 82 / 120;
+// one of 729, 368: 78 / 65; of 256 in bf16, 336: 28 / 33.
 template <typename T, int DB>
-constexpr int own_most() { return sizeof(T) == 4 ? (DB <= 4 ? 768 : 0) : DB == 2 ? 768 : 256; }
+int64_t own_most(bool causal) {
+  constexpr bool SLOW = sizeof(T) == 4 || DB > 4;
+  return SLOW ? (DB <= 4 ? (causal ? 1200 : 384) : (causal ? 768 : 256)) : DB == 2 ? 768 : 256;
+}
 template <typename T, int DB, int DQ>
 void prompt_waves(const fi_prompt_attention_args& a, dim3 grid, bool two, hipStream_t s) {
   const int64_t small = (a.q_tokens / 32 + a.n_seqs) * a.q_heads;
-  if constexpr (own_most<T, DB>() > 0) {
-    if (small <= own_most<T, DB>()) return (void)(prompt_own_kernel<T, DB, DQ><<<dim3((uint32_t)small), 64 * Own<T, DB>::WAVES, 0, s>>>(a));
-  }
+  if (small <= own_most<T, DB>(a.causal != 0)) return (void)(prompt_own_kernel<T, DB, DQ><<<dim3((uint32_t)small), 64 * Own<T, DB>::WAVES, 0, s>>>(a));
   if constexpr (sizeof(T) == 2 && DB <= 4) {
     if (two) return (void)(prompt_tile_kernel<T, DB, 2, DQ><<<grid, 128 * PROMPT_WAVES, 0, s>>>(a));
   }
