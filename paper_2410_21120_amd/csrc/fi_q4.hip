@@ -377,30 +377,34 @@ __global__ void __launch_bounds__(256) q4_few_kernel(fi_q4_matmul_args a, uint32
   if (n < a.outputs && m < a.rows) st(static_cast<T*>(a.out) + m * a.out_stride + n, y);
 }
 
-// More rows (bf16): a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, AHEAD
+// More rows: a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, AHEAD
 // steps ahead: each wave's weights (32 outputs) and their scales and zero points for itself, of the rows a share each, which it weaves and sums by groups a step
 // before they are used.  What the zero points take off, scale * (16 + zero) * (sum of the group's x), is a product of its own over the groups: an fp32 matrix
 // instruction takes four of them, once a chunk.  The vector unit bounds it about as much as HBM (64 operations a step to unpack 2 KB of weights, 16 MB for the groups' scales).
 // GP: groups in a step (1: groups of 128 inputs and multiples).  Scales and zero points come in chunks of CS steps, so that a load takes pieces of rows
 // (two values of 32 rows at a time cost 7 of 37 us): every step brings S of the instructions that fill the chunk after its own.
-template <int MB, int GP>
+// fp32 rows: each eight inputs are woven as three bf16 terms, which meet the weights one after the other; 16 rows a workgroup.
+template <typename T, int MB, int GP>
 struct Wide {
+  static constexpr int TERMS = Run8<T>::TERMS;
   static constexpr int S = GP == 4 ? 2 : 1, CS = GP == 4 ? 1 : 4, GC = GP * CS;            // (a chunk's groups: 8 of 64 inputs, else 4)
   static constexpr int CHUNK = 32 * GC * 4, CHUNKS = GP == 4 ? 6 : 3;                       // of a wave: as much for scales as for zero points
-  static constexpr int WSTEP = WAVES * 2048, XSTEP = MB * 4096, SUMS = GC * 16 * MB * 4;    // a step's weights, its rows; a chunk's sums of the rows
-  static constexpr int LEFT = 160 * 1024 - CHUNKS * WAVES * 2 * CHUNK - 2 * XSTEP - 2 * SUMS + XSTEP, MOST = LEFT / (WSTEP + XSTEP);
+  static constexpr int WSTEP = WAVES * 2048, XSTEP = MB * 2048 * (int)sizeof(T), WOVEN_STEP = TERMS * MB * 4096, SUMS = GC * 16 * MB * 4;   // a step's weights, its rows, woven; a chunk's sums of the rows
+  static constexpr int LEFT = 160 * 1024 - CHUNKS * WAVES * 2 * CHUNK - 2 * WOVEN_STEP - 2 * SUMS + XSTEP, MOST = LEFT / (WSTEP + XSTEP);
   static constexpr int BUFS = MOST < 5 ? MOST : 5, AHEAD = BUFS - 1, L = 3 + 2 * S;         // L: loads of a wave in a step, its rows' first
   // in LDS: AHEAD + 1 steps of weights, AHEAD of rows as they come, two of woven rows, two chunks' sums, the waves' chunks
-  static constexpr int X = BUFS * WSTEP, WOVEN = X + AHEAD * XSTEP, ALL = WOVEN + 2 * XSTEP, SCALES = ALL + 2 * SUMS, BYTES = SCALES + CHUNKS * WAVES * 2 * CHUNK;
-  static_assert(BUFS >= 4 && AHEAD * L < 64 && (CS - 1 + AHEAD) / CS + 1 < CHUNKS, "waits can be counted; the chunk in use is not loaded over");
+  static constexpr int X = BUFS * WSTEP, WOVEN = X + AHEAD * XSTEP, ALL = WOVEN + 2 * WOVEN_STEP, SCALES = ALL + 2 * SUMS, BYTES = SCALES + CHUNKS * WAVES * 2 * CHUNK;
+  static_assert(BUFS >= 3 && (TERMS == 1 || MB == 1) && AHEAD * L < 64 && (CS - 1 + AHEAD) / CS + 1 < CHUNKS, "waits can be counted; the chunk in use is not loaded over");
 };
 template <int CTRL>
 __device__ __forceinline__ float swapped(float v) {   // of another lane of the row of 16
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
-template <int MB, int GP>
+template <typename T, int MB, int GP>
 __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_args a, int splits, int per_group) {
-  using Z = Wide<MB, GP>;
+  using Z = Wide<T, MB, GP>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int TERMS = Z::TERMS;
   constexpr int AHEAD = Z::AHEAD, GC = Z::GC, CS = Z::CS;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[Z::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i = lane & 15, K = a.inputs;
@@ -410,7 +414,8 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
   // What this lane loads: weights of two outputs (past the last one: the last once more, not stored), a piece of a row, a scale and a zero point or two.  All
   // from bases that the wave shares (the strides are below 2^24 elements).
   const int first_n = n0 < last ? n0 : last, left_n = last - first_n;
-  const int piece_w = (lane & 3) ^ (q & 3), share = wave & (4 * MB - 1), row_x = 4 * share + q, piece_x = i ^ (row_x & 15);
+  const int piece_w = (lane & 3) ^ (q & 3), share = F32 ? wave : wave & (4 * MB - 1);
+  const int row_x = F32 ? 2 * wave + (lane >> 5) : 4 * share + q, piece_x = F32 ? lane & 31 : i ^ (row_x & 15);
   const uint8_t* const w = a.w + (int64_t)first_n * a.w_stride;
   const float* const scale0 = a.scales + (int64_t)first_n * a.scales_stride;
   const uint8_t* const zero0 = a.zeros ? a.zeros + (int64_t)first_n * a.zeros_stride : nullptr;
@@ -421,8 +426,8 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
     off_w[b] = (uint32_t)(n < left_n ? n : left_n) * (uint32_t)a.w_stride + 16 * piece_w;
   }
   const int left_m = a.rows - 1 - m0;
-  const bf16_t* const x = static_cast<const bf16_t*>(a.x) + (int64_t)m0 * a.x_stride;
-  const uint32_t off_x = (uint32_t)(row_x < left_m ? row_x : left_m) * (uint32_t)a.x_stride * 2 + 16 * piece_x;
+  const T* const x = static_cast<const T*>(a.x) + (int64_t)m0 * a.x_stride;
+  const uint32_t off_x = (uint32_t)(row_x < left_m ? row_x : left_m) * (uint32_t)a.x_stride * (uint32_t)sizeof(T) + 16 * piece_x;
   uint8_t* const own = smem + Z::SCALES + wave * Z::CHUNKS * 2 * Z::CHUNK;   // the wave's chunks
   // instruction `part` of a chunk (64 / GC rows of it), into buffer `to`
   constexpr int PARTS = GC / 2;
@@ -444,7 +449,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
 #pragma unroll
       for (int b = 0; b < 2; ++b) load_lds_off<16>(w + (k >> 1), off_w[b], at + b * 1024);
     } else {   // pieces past the end of the inputs: the step's first once more, not multiplied
-      load_lds_off<16>(x + k, off_x - (k + 8 * piece_x < K ? 0 : 16 * piece_x), at_x);
+      load_lds_off<16>(x + k, off_x - (k + 16 / (int)sizeof(T) * piece_x < K ? 0 : 16 * piece_x), at_x);
 #pragma unroll
       for (int b = 0; b < 2; ++b) load_lds_off<16>(w + (k >> 1), off_w[b] - (k + 32 * piece_w < K ? 0 : 16 * piece_w), at + b * 1024);
     }
@@ -457,17 +462,34 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
   // The wave's own share of a step's rows (which it loaded itself), for all: woven, and summed by groups.
   uint32_t raw = 0;
   auto weave_step = [&](uint32_t step) {
-    if (wave < 4 * MB) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(smem + Z::X + raw * Z::XSTEP + share * 1024 + lane * 16);
-      *reinterpret_cast<u32x4*>(smem + Z::WOVEN + (step & 1) * Z::XSTEP + share * 1024 + lane * 16) = weave(v);
-      float sum = dot2(v[0], ONES, dot2(v[1], ONES, 0.0f)) + dot2(v[2], ONES, dot2(v[3], ONES, 0.0f));
+    const uint8_t* const from_raw = smem + Z::X + raw * Z::XSTEP + share * 1024;
+    uint8_t* const to_woven = smem + Z::WOVEN + (step & 1) * Z::WOVEN_STEP;
+    if (F32 ? lane < 32 : wave < 4 * MB) {
+      float sum;
+      int row = row_x, octet = piece_x;
+      if constexpr (F32) {   // a lane has eight inputs of one of the wave's two rows
+        row = 2 * wave + q;
+        octet = i;
+        Run8<float> v;
+        v.v[0] = reinterpret_cast<const float4*>(from_raw + q * 512 + i * 32)[0];
+        v.v[1] = reinterpret_cast<const float4*>(from_raw + q * 512 + i * 32)[1];
+        u32x4 terms[TERMS];
+        v.terms(terms);
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) *reinterpret_cast<u32x4*>(to_woven + t * 4096 + row * 256 + ((i ^ row) << 4)) = terms[t];
+        sum = (v.v[0].x + v.v[0].y) + (v.v[0].z + v.v[0].w) + ((v.v[1].x + v.v[1].y) + (v.v[1].z + v.v[1].w));
+      } else {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(from_raw + lane * 16);
+        *reinterpret_cast<u32x4*>(to_woven + share * 1024 + lane * 16) = weave(v);
+        sum = dot2(v[0], ONES, dot2(v[1], ONES, 0.0f)) + dot2(v[2], ONES, dot2(v[3], ONES, 0.0f));
+      }
       sum += swapped<0xB1>(sum);                          // lane ^ 1
       sum += swapped<0x4E>(sum);                          // lane ^ 2
       if constexpr (GP < 4) sum += swapped<0x141>(sum);   // 7 - lane of eight
       if constexpr (GP < 2) sum += swapped<0x140>(sum);   // 15 - lane
       if (i % (16 / GP) == 0) {
         float* const all = reinterpret_cast<float*>(smem + Z::ALL + (step / CS & 1) * Z::SUMS);
-        all[(step % CS * GP + piece_x / (16 / GP)) * 16 * MB + row_x] = sum;
+        all[(step % CS * GP + octet / (16 / GP)) * 16 * MB + row] = sum;
       }
     }
     raw = raw + 1 < AHEAD ? raw + 1 : 0;
@@ -497,13 +519,13 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
     if (step + 1 < s1) weave_step(step + 1);
     if (step + AHEAD < s1) load(step + AHEAD);   // into the slots that this wave has read
     const uint8_t* const at = smem + now * Z::WSTEP + wave * 2048 + i * 64 + q * 4;
-    const uint8_t* const rows = smem + Z::WOVEN + (step & 1) * Z::XSTEP + i * 256;
+    const uint8_t* const rows = smem + Z::WOVEN + (step & 1) * Z::WOVEN_STEP + i * 256;
     now = now + 1 < Z::BUFS ? now + 1 : 0;
     // the step's first group in its chunk
     const uint8_t* const chunk = own + from * 2 * Z::CHUNK;
     const uint8_t* const scales = chunk + 4 * (GP > 1 ? step % CS * GP : step / (uint32_t)per_group - step / CS * CS / (uint32_t)per_group);
     // all that the step multiplies, read at once
-    u32x4 v[4][MB];
+    u32x4 v[4][MB * TERMS];   // (block of rows, or term)
     uint32_t d[4][2];
     float scale[GP][2];
 #pragma unroll
@@ -511,7 +533,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
 #pragma unroll
       for (int b = 0; b < 2; ++b) d[r][b] = *reinterpret_cast<const uint32_t*>(at + b * 1024 + ((r ^ (i >> 2)) << 4));
 #pragma unroll
-      for (int t = 0; t < MB; ++t) v[r][t] = *reinterpret_cast<const u32x4*>(rows + t * 4096 + (((4 * r + q) ^ i) << 4));
+      for (int t = 0; t < MB * TERMS; ++t) v[r][t] = *reinterpret_cast<const u32x4*>(rows + t * 4096 + (((4 * r + q) ^ i) << 4));
     }
 #pragma unroll
     for (int g = 0; g < GP; ++g)
@@ -530,7 +552,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
           const uint32_t w4 = d[r][b];
           const u32x4 f = {(w4 << 3 & mask) | sixteen, (w4 >> 1 & mask) | sixteen, (w4 >> 5 & mask) | sixteen, (w4 >> 9 & mask) | sixteen};
 #pragma unroll
-          for (int t = 0; t < MB; ++t) dot[t][b] = mfma16(v[r][t], f, r == 4 / GP * g ? f32x4{0, 0, 0, 0} : dot[t][b]);
+          for (int t = 0; t < MB * TERMS; ++t) dot[t % MB][b] = mfma16(v[r][t], f, r == 4 / GP * g && t < MB ? f32x4{0, 0, 0, 0} : dot[t % MB][b]);
         }
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -566,7 +588,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
   }
   const uint32_t stride = splits > 1 ? (uint32_t)a.outputs : (uint32_t)a.out_stride;
   float* const part = static_cast<float*>(a.workspace) + ((int64_t)split * a.rows + m0) * a.outputs + n0;
-  bf16_t* const out = static_cast<bf16_t*>(a.out) + (int64_t)m0 * a.out_stride + n0;
+  T* const out = static_cast<T*>(a.out) + (int64_t)m0 * a.out_stride + n0;
 #pragma unroll
   for (int t = 0; t < MB; ++t)
 #pragma unroll
@@ -609,17 +631,21 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
 //  WIDE: has two launches and about 8 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 12.0 / 11.8, 20 rows 13.6 / 19.4;
 //        1024 x 16384, 16 rows 12.3 / 8.8, 20 rows 14.1 / 15.4; 4096 x 8192, 8 rows 13.7 / 19.2; 2048 x 8666, 5 rows 12.8 / 22.4; 4096 x 300, 20 rows 11.0 / 10.9; 8192 x 300, 20 rows 11.4 / 19.8; wide / few:
 //        8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4; 16384 x 4096, 4 rows 18.8 / 19.8, 25088 x 4096 26.0 / 29.7, 8192 x 8192 17.7 / 17.3).
+//        fp32, wide / tile: 4096 x 4096, 8 rows 12.3 / 13.1, 20 rows 13.5 / 25.4; 2048 x 4096, 16 rows 11.9 / 9.5, 20 rows 12.1 / 15.2; 1024 x 16384, 16 rows 12.8 / 10.3; 4096 x 1000,
+//        20 rows 11.1 / 15.4; 16384 x 4096, 16 rows 21 / 52, 64 rows 52 / 203; wide / few: 16384 x 1024, 5 rows 13.7 / 19.1.
 enum Kernel { FEW, TILE, WIDE };
 struct Plan { Kernel kernel; int mb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
   Plan p = {TILE, 1, 1};
   const int64_t weights = (int64_t)a.inputs * a.outputs, blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
-  const bool wide = a.dtype == FI_BF16 && a.rows > (a.inputs >= 16384 ? 2 : 4) &&
-                    (weights * ((a.rows + 15) / 16) >= 3 << 23 || a.inputs >= 12288 || (a.inputs >= 8192 && a.rows > 16) ||
+  const bool f32 = a.dtype == FI_F32;
+  const int64_t work = weights * ((a.rows + 15) / 16);
+  const bool wide = a.rows > (a.inputs >= 16384 && !f32 ? 2 : 4) &&
+                    (work >= (f32 && a.inputs >= 2048 ? 1 << 24 : 3 << 23) || a.inputs >= 12288 || (a.inputs >= (f32 ? 4096 : 8192) && a.rows > 16) ||
                      (a.inputs >= 2048 && a.outputs > 8192));
   if (wide) {
     p.kernel = WIDE;
-    p.mb = a.rows > 16 ? 2 : 1;
+    p.mb = a.rows > 16 && a.dtype == FI_BF16 ? 2 : 1;
     const int64_t groups = blocks * (((int64_t)a.rows + 16 * p.mb - 1) / (16 * p.mb));
     int64_t splits = groups > 0 ? 256 / groups : 1;                   // a workgroup per compute unit at most: they run one at a time
     if (splits > steps / 4) splits = steps / 4;                       // (a join costs about as much as four steps)
@@ -657,12 +683,12 @@ void launch_few(const fi_q4_matmul_args& a, hipStream_t s) {
   else if (a.inputs > 2048) q4_few_kernel<T, M, 1, 2><<<grid(1, 2), 256, 0, s>>>(a, inv);
   else q4_few_kernel<T, M, 1, 1><<<grid(1, 1), 256, 0, s>>>(a, inv);
 }
-template <int MB>
+template <typename T, int MB>
 void launch_wide(const fi_q4_matmul_args& a, const Plan& p, hipStream_t s) {
   const dim3 grid((uint32_t)(((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES) * p.splits), (uint32_t)(((int64_t)a.rows + 16 * MB - 1) / (16 * MB)));
-  if (a.group == 32) q4_wide_kernel<MB, 4><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
-  else if (a.group == 64) q4_wide_kernel<MB, 2><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
-  else q4_wide_kernel<MB, 1><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, a.group / 128);
+  if (a.group == 32) q4_wide_kernel<T, MB, 4><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
+  else if (a.group == 64) q4_wide_kernel<T, MB, 2><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, 1);
+  else q4_wide_kernel<T, MB, 1><<<grid, 64 * WAVES, 0, s>>>(a, p.splits, a.group / 128);
 }
 template <typename T>
 int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
@@ -679,13 +705,12 @@ int launch_t(const fi_q4_matmul_args& a, hipStream_t s) {
     else if (a.rows == 2) launch_few<T, 2>(a, s);
     else launch_few<T, 4>(a, s);
   } else if (p.kernel == WIDE && aligned && near) {
-    if (p.mb == 1) launch_wide<1>(a, p, s);
-    else launch_wide<2>(a, p, s);
+    if constexpr (sizeof(T) == 4) launch_wide<T, 1>(a, p, s);
+    else if (p.mb == 1) launch_wide<T, 1>(a, p, s);
+    else launch_wide<T, 2>(a, p, s);
     const uint32_t blocks = (uint32_t)((a.outputs + 255) / 256);
     if (p.splits > 1) q4_join_kernel<T><<<dim3(blocks * (uint32_t)a.rows), 256, 0, s>>>(a, p.splits, blocks);
-  } else if (a.outputs >= 16384 || (sizeof(T) == 4 && a.outputs >= 8192 && (a.inputs >= 2048 || a.rows > 16))) {
-    // four blocks of outputs share what is made of the rows' inputs, which is most of the work in fp32 (2048 x 12000, 64 rows 126 us, 82; 5 rows 27.1, 26.6; 1024 x 8200, 5 rows
-    // 11.8, 14.9); fewer leave compute units without work
+  } else if (a.outputs >= 16384) {   // (four blocks of outputs share the rows' inputs; fewer leave compute units without work)
     launch_tiles<T, 4, 8>(a, vw, s);
   } else if (a.inputs >= 2048) {
     launch_tiles<T, 1, 16>(a, vw, s);

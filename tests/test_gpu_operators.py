@@ -555,6 +555,24 @@ def test_q4_products_shared_out_over_the_inputs(torch, fi, rows, inputs, outputs
     assert torch.equal(again[kept], got[kept]) and not again[rows // 2].isfinite().any()
 
 
+@pytest.mark.parametrize("rows,inputs,outputs,group,zeros", [
+    (5, 12320, 33, 32, True), (17, 8288, 300, 32, False), (40, 12352, 270, 64, True), (9, 12352, 1, 64, False), (16, 12288, 17, 128, True), (20, 12288, 257, 384, True),
+    (7, 2048, 12300, 256, False), (33, 8192, 513, 2048, True)])
+def test_q4_fp32_products_shared_out_over_the_inputs(torch, fi, rows, inputs, outputs, group, zeros):
+    """The same for fp32 rows, blocks of 16."""
+    g = torch.Generator().manual_seed(inputs + outputs)
+    x, w, s, z = _q4_case(torch, g, rows, inputs, outputs, group, zeros, torch.float32, "wide")
+    got = fi.q4_matmul(x, w, s, z, group=group)
+    want, bound = _q4_ref(torch, x, w, s, z, group, "f32")
+    _inside(got.double().cpu(), want, bound)
+    assert float((got.double().cpu() - want).norm() / want.norm()) <= 64 * U or rows * outputs < 16
+    assert torch.equal(fi.q4_matmul(x, w, s, z, group=group), got)
+    x[rows // 2, inputs - 1] = math.inf
+    kept = [i for i in range(rows) if i != rows // 2]
+    again = fi.q4_matmul(x, w, s, z, group=group)
+    assert torch.equal(again[kept], got[kept]) and not again[rows // 2].isfinite().any()
+
+
 def test_q4_rows_do_not_touch_each_other(torch, fi):
     """A row of NaN or infinities stays a row; weights of zero times infinity are NaN, as in the formula."""
     g = torch.Generator().manual_seed(12)
