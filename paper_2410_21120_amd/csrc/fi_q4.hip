@@ -628,21 +628,22 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
 // Which kernel takes a call, from its sizes and type alone (the workspace goes by it), where the addresses allow all of them.
 //  FEW:  reads 2048 inputs a step; its time grows with rows x outputs (us, few / tile: 4096 x 1000 inputs x outputs, 1 row 3.2 / 8.4, 4 rows 5.2 / 9.1, 16 rows 7.9 / 11.3;
 //        4096 x 4096, 4 rows 7.8 / 10.0, 8 rows 10.9 / 10.8; 1024 x 16384, 2 rows 8.2 / 8.2, 4 rows 12.6 / 8.4; 512 x 8192, 1 row 4.2 / 3.6).
-//  WIDE: has two launches and about 8 us whatever it does, and the least time per weight (us, wide / tile: 4096 x 4096, 16 rows 12.0 / 11.8, 20 rows 13.6 / 19.4;
-//        1024 x 16384, 16 rows 12.3 / 8.8, 20 rows 14.1 / 15.4; 4096 x 8192, 8 rows 13.7 / 19.2; 2048 x 8666, 5 rows 12.8 / 22.4; 4096 x 300, 20 rows 11.0 / 10.9; 8192 x 300, 20 rows 11.4 / 19.8; wide / few:
-//        8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4; 16384 x 4096, 4 rows 18.8 / 19.8, 25088 x 4096 26.0 / 29.7, 8192 x 8192 17.7 / 17.3).
-//        fp32, wide / tile: 4096 x 4096, 8 rows 12.3 / 13.1, 20 rows 13.5 / 25.4; 2048 x 4096, 16 rows 11.9 / 9.5, 20 rows 12.1 / 15.2; 1024 x 16384, 16 rows 12.8 / 10.3; 4096 x 1000,
-//        20 rows 11.1 / 15.4; 16384 x 4096, 16 rows 21 / 52, 64 rows 52 / 203; wide / few: 16384 x 1024, 5 rows 13.7 / 19.1.
+//  TILE: its time is that of a wave's walk over its share of the inputs, once a round of 256 workgroups; smaller groups and fp32 rows make a step longer.
+//  WIDE: has two launches and about 10 us whatever it does, and the least time per weight (us, wide / tile, groups of 64, 16 rows: 2048 x 4096 10.9 / 7.2, 4096 x 4096 12.0 / 11.8,
+//        8192 x 3000 13.6 / 20.5, 2048 x 8000, two rounds, 11.9 / 12.6; 1024 x 16384, four times the work a step, 12.1 / 8.8, 32 rows 15.5 / 15.8; groups of 32: 2048 x 4096 12.2 / 9.9,
+//        4096 x 2048 12.8 / 17.0, 1024 x 16384 13.2 / 14.9; fp32: 2048 x 4096 11.9 / 9.3, 4096 x 4096 12.8 / 15.8, 1024 x 16384 13.1 / 10.2, 64 rows x 16384 x 4096 52 / 203;
+//        wide / few: 8192 x 1024, 8 rows 11.4 / 9.2; 12288 x 600, 8 rows 11.9 / 12.5; 25088 x 300, 8 rows 16.1 / 19.4; 16384 x 4096, 4 rows 18.8 / 19.8, 25088 x 4096 26.0 / 29.7,
+//        fp32 30 / 41).
 enum Kernel { FEW, TILE, WIDE };
 struct Plan { Kernel kernel; int mb, splits; };
 Plan plan(const fi_q4_matmul_args& a) {
   Plan p = {TILE, 1, 1};
-  const int64_t weights = (int64_t)a.inputs * a.outputs, blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
-  const bool f32 = a.dtype == FI_F32;
-  const int64_t work = weights * ((a.rows + 15) / 16);
-  const bool wide = a.rows > (a.inputs >= 16384 && !f32 ? 2 : 4) &&
-                    (work >= (f32 && a.inputs >= 2048 ? 1 << 24 : 3 << 23) || a.inputs >= 12288 || (a.inputs >= (f32 ? 4096 : 8192) && a.rows > 16) ||
-                     (a.inputs >= 2048 && a.outputs > 8192));
+  const int64_t blocks = ((int64_t)a.outputs + 32 * WAVES - 1) / (32 * WAVES), steps = ((int64_t)a.inputs + 127) / 128;
+  const bool f32 = a.dtype == FI_F32, few = a.inputs >= 2048 && a.rows <= 16 && a.outputs < 2048;
+  const int64_t per = a.outputs >= 16384 ? 64 : 16, tiles = (a.outputs + per - 1) / per * (((int64_t)a.rows + 15) / 16);
+  const int64_t walk = a.inputs * ((tiles + 255) / 256) * (per == 64 ? 3 : 1);   // (of TILE)
+  const int64_t most = a.group < 64 ? 3000 : a.group < 128 ? (f32 ? 4000 : 5000) : (f32 ? 5000 : 7000);
+  const bool wide = a.rows > 4 ? a.inputs >= 12288 || (!few && walk >= most) : a.rows > 2 && a.inputs >= 16384;
   if (wide) {
     p.kernel = WIDE;
     p.mb = a.rows > 16 && a.dtype == FI_BF16 ? 2 : 1;
@@ -650,7 +651,7 @@ Plan plan(const fi_q4_matmul_args& a) {
     int64_t splits = groups > 0 ? 256 / groups : 1;                   // a workgroup per compute unit at most: they run one at a time
     if (splits > steps / 4) splits = steps / 4;                       // (a join costs about as much as four steps)
     p.splits = splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
-  } else if ((a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && (a.rows <= 4 || (a.rows <= 16 && a.outputs < 2048)))) {
+  } else if (few || (a.inputs >= 1024 && a.rows <= 2) || (a.inputs >= 2048 && a.rows <= 4)) {
     p.kernel = FEW;
   }
   return p;
