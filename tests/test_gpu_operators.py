@@ -650,3 +650,69 @@ def test_operators_in_a_graph(torch, fi):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
+
+
+# ---- tensors that do not fit --------------------------------------------------------------------------------
+def test_tensors_that_do_not_fit_are_refused(torch, fi):
+    """Every check on the way from tensors to the entry points: types, shapes, strides, devices; nothing is launched."""
+    d = dict(dtype=torch.bfloat16, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q, k, cu = torch.zeros((4, 4, 64), **d), torch.zeros((4, 2, 64), **d), torch.tensor([0, 4], **i32)
+    positions, freq = torch.zeros(4, **i32), torch.zeros(32, device="cuda")
+    cache, slots = torch.zeros((2, 16, 2, 64), **d), torch.zeros(4, dtype=torch.int64, device="cuda")
+    table, cached = torch.zeros((1, 2), **i32), torch.zeros(1, **i32)
+    x, w, s = torch.zeros((3, 128), **d), torch.zeros((8, 64), dtype=torch.uint8, device="cuda"), torch.zeros((8, 2), device="cuda")
+    wrong = [
+        (TypeError, lambda: fi.qk_norm_rope(q.half(), k, k, positions, freq)),
+        (TypeError, lambda: fi.qk_norm_rope(q, None, k, positions, freq)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k.float(), k, positions, freq)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k[:3], k, positions, freq)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k.cpu(), positions, freq)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions.long(), freq)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, sections=[16, 16])),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, q_weight=torch.ones(63, device="cuda"))),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, slots=slots)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, slots=slots, k_out=cache)),
+        (ValueError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, q_out=torch.zeros((4, 64, 4), **d).transpose(1, 2))),
+        (TypeError, lambda: fi.qk_norm_rope(q, k, k, positions, freq, eps="small")),
+        (fi.FiError, lambda: fi.qk_norm_rope(q, k, k, positions, torch.zeros(40, device="cuda"))),
+        (ValueError, lambda: fi.prompt_attention(q, k, k[:, :1], cu)),
+        (ValueError, lambda: fi.prompt_attention(q, k, k, cu.long())),
+        (ValueError, lambda: fi.prompt_attention(q, k, k, cu, torch.tensor([0, 2, 4], **i32))),
+        (ValueError, lambda: fi.prompt_attention(q, k, k, cu, out=torch.zeros((4, 4, 32), **d))),
+        (fi.FiError, lambda: fi.prompt_attention(q[:, :3], k, k, cu)),
+        (fi.FiError, lambda: fi.prompt_attention(q, k, k, cu, scale=-1.0)),
+        (ValueError, lambda: fi.tree_attention(q, cache, cache[:1], table, cached, cu)),
+        (ValueError, lambda: fi.tree_attention(q, cache, cache, table, cached, cu, torch.zeros((3, 1), dtype=torch.int64, device="cuda"))),
+        (ValueError, lambda: fi.tree_attention(q, cache, cache, table, torch.zeros(2, **i32), cu)),
+        (ValueError, lambda: fi.tree_attention(q, cache, cache, table, cached, cu, max_length=1 << 40)),
+        (ValueError, lambda: fi.tree_attention(q, cache, cache, table, cached, cu, workspace=torch.zeros(64, device="cuda"))),
+        (ValueError, lambda: fi.q4_matmul(x, w[:, :63], s)),
+        (ValueError, lambda: fi.q4_matmul(x, w, s, group=32)),
+        (ValueError, lambda: fi.q4_matmul(x, w, s, torch.zeros((8, 1), dtype=torch.uint8, device="cuda"))),
+        (ValueError, lambda: fi.q4_matmul(x, w.t().contiguous().t(), s)),
+        (TypeError, lambda: fi.q4_matmul(x, w, s, out="here")),
+    ]
+    for number, (kind, call) in enumerate(wrong):
+        with pytest.raises(kind):
+            call()
+            pytest.fail(f"number {number} was taken")
+    assert torch.equal(fi.q4_matmul(x, w, s), torch.zeros((3, 8), **d))
+
+
+def test_a_workspace_of_the_callers(torch, fi):
+    """Products that are shared out take the caller's workspace, and refuse one that is too small."""
+    g = torch.Generator().manual_seed(4)
+    x, w, s, z = _q4_case(torch, g, 9, 12288, 70, 64, True, torch.bfloat16, "plain")
+    args = fi.fi_q4_matmul_args(dtype=fi.FI_BF16, rows=9, inputs=12288, outputs=70, group=64)
+    need = fi.fi_q4_matmul_workspace(args)
+    assert need > 0
+    want = fi.q4_matmul(x, w, s, z)
+    assert torch.equal(fi.q4_matmul(x, w, s, z, workspace=torch.empty(need, dtype=torch.uint8, device="cuda")), want)
+    with pytest.raises(fi.FiError):
+        fi.q4_matmul(x, w, s, z, workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = fi.q4_matmul(x, w, s, z, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, want)
