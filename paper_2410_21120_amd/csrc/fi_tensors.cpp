@@ -45,7 +45,7 @@ struct {
   fi_status (*q4_workspace)(const fi_q4_matmul_args*, uint64_t*);
   PyObject *check;    // check(status, entry point's name): raises
   PyObject *stream;   // stream(device index): the current one as a number
-  PyObject *lend;     // lend(tensor, stream, device index): its memory is handed out again only after that stream is done with it
+  PyObject *room;     // room(shape, type, stream, device index): a tensor from the memory that torch keeps for that stream
 } py;
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
@@ -107,10 +107,24 @@ struct Call {
     if (!fits(t, want, shape) || !t.is_contiguous()) misfit(t, name, want, shape, "contiguous ");
     return static_cast<T*>(t.data_ptr());
   }
+  // Memory for a call on `stream` (None: the current one).  It has to come from what torch keeps for that stream: a block that another stream's pool hands out may
+  // have been freed a moment ago with kernels of that other stream, for which nothing makes this one wait, still at work on it.
+  at::Tensor room(at::ScalarType kind, Shape shape, PyObject* stream) const {
+    if (stream == Py_None) return at::empty(at::IntArrayRef(shape), at::TensorOptions().dtype(kind).device(at::Device(at::kCUDA, (c10::DeviceIndex)index)));
+    PyObject* const sizes = PyTuple_New((Py_ssize_t)shape.size());
+    if (!sizes) throw Raised{};
+    Py_ssize_t i = 0;
+    for (int64_t n : shape) PyTuple_SET_ITEM(sizes, i++, PyLong_FromLongLong(n));
+    PyObject* const o = PyObject_CallFunction(py.room, "NsOi", sizes, c10::toString(kind), stream, index);
+    if (!o) throw Raised{};
+    const at::Tensor made = THPVariable_Unpack(o);
+    Py_DECREF(o);
+    return made;
+  }
   // A caller's output, or one made here.
-  at::Tensor output(PyObject* o, const char* name, Shape shape) const {
+  at::Tensor output(PyObject* o, const char* name, Shape shape, PyObject* stream) const {
     if (o != Py_None) return tensor(o, name);
-    return at::empty(at::IntArrayRef(shape), at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)index)));
+    return room(type, shape, stream);
   }
 
   template <typename Args>
@@ -147,14 +161,7 @@ struct Call {
       uint64_t need = 0;
       check(needed(&args, &need), name, &args);
       if (!need) return w;
-      w = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(at::Device(at::kCUDA, (c10::DeviceIndex)index)));
-      if (stream != Py_None) {
-        PyObject* const o = THPVariable_Wrap(w);
-        PyObject* const r = o ? PyObject_CallFunction(py.lend, "OOi", o, stream, index) : nullptr;
-        Py_XDECREF(o);
-        if (!r) throw Raised{};
-        Py_DECREF(r);
-      }
+      w = room(at::kByte, {(int64_t)need}, stream);
     }
     args.workspace = w.data_ptr();
     args.workspace_bytes = (uint64_t)w.numel();
@@ -211,7 +218,7 @@ PyObject* qk_norm_rope(PyObject* const* arg) {
   if (arg[6] != Py_None) a.k_weight = c.plain<float>(tensor(arg[6], "k_weight"), "k_weight", at::kFloat, {dim});
   a.positions = positions.dim() == 1 ? c.plain<int32_t>(positions, "positions", at::kInt, {tokens}) : c.plain<int32_t>(positions, "positions", at::kInt, {tokens, axes});
   a.inv_freq = c.plain<float>(inv_freq, "inv_freq", at::kFloat, {pairs});
-  const at::Tensor q_out = c.output(arg[11], "q_out", {tokens, heads, dim});
+  const at::Tensor q_out = c.output(arg[11], "q_out", {tokens, heads, dim}, arg[14]);
   a.q_out = c.rows(q_out, "q_out", {tokens, heads, dim}, a.q_out_strides);
   at::Tensor k_out, v_out;
   if (paged) {
@@ -225,9 +232,9 @@ PyObject* qk_norm_rope(PyObject* const* arg) {
     a.k_out = c.rows(k_out, "k_out", {pages, page, kv_heads, dim}, a.k_out_strides);
     if (has_v) v_out = tensor(arg[13], "v_out"), a.v_out = c.rows(v_out, "v_out", {pages, page, kv_heads, dim}, a.v_out_strides);
   } else {
-    k_out = c.output(arg[12], "k_out", {tokens, kv_heads, dim});
+    k_out = c.output(arg[12], "k_out", {tokens, kv_heads, dim}, arg[14]);
     a.k_out = c.rows(k_out, "k_out", {tokens, kv_heads, dim}, a.k_out_strides + 1);
-    if (has_v) v_out = c.output(arg[13], "v_out", {tokens, kv_heads, dim}), a.v_out = c.rows(v_out, "v_out", {tokens, kv_heads, dim}, a.v_out_strides + 1);
+    if (has_v) v_out = c.output(arg[13], "v_out", {tokens, kv_heads, dim}, arg[14]), a.v_out = c.rows(v_out, "v_out", {tokens, kv_heads, dim}, a.v_out_strides + 1);
   }
   if (has_v) a.v = c.rows(tensor(arg[2], "v"), "v", {tokens, kv_heads, dim}, a.v_strides);
   c.make(py.qk_norm_rope, "fi_qk_norm_rope", a, arg[14]);
@@ -254,7 +261,7 @@ PyObject* prompt_attention(PyObject* const* arg) {
   a.v = c.rows(v, "v", {keys, kv_heads, dim}, a.v_strides);
   a.cu_q = c.plain<int32_t>(cu_q, "cu_q", at::kInt, {ends});
   a.cu_k = arg[4] == Py_None ? a.cu_q : c.plain<int32_t>(tensor(arg[4], "cu_k"), "cu_k", at::kInt, {ends});
-  const at::Tensor out = c.output(arg[7], "out", {tokens, heads, dim});
+  const at::Tensor out = c.output(arg[7], "out", {tokens, heads, dim}, arg[8]);
   a.out = c.rows(out, "out", {tokens, heads, dim}, a.out_strides);
   c.make(py.prompt_attention, "fi_prompt_attention", a, arg[8]);
   return returned(arg[7], out);
@@ -293,7 +300,7 @@ PyObject* tree_attention(PyObject* const* arg) {
   a.v_cache = c.rows(v, "v_cache", {pages, page, kv_heads, dim}, a.v_strides);
   a.cached = c.plain<int32_t>(cached, "cached", at::kInt, {seqs});
   a.cu_nodes = c.plain<int32_t>(cu, "cu_nodes", at::kInt, {seqs + 1});
-  const at::Tensor out = c.output(arg[10], "out", {nodes, heads, dim});
+  const at::Tensor out = c.output(arg[10], "out", {nodes, heads, dim}, arg[12]);
   a.out = c.rows(out, "out", {nodes, heads, dim}, a.out_strides);
   const at::Tensor workspace = c.workspace(py.tree_workspace, "fi_tree_attention_workspace", a, arg[11], arg[12]);
   c.make(py.tree_attention, "fi_tree_attention", a, arg[12]);
@@ -317,7 +324,7 @@ PyObject* q4_matmul(PyObject* const* arg) {
   a.w = static_cast<uint8_t*>(c.rows(w, "w", at::kByte, {outputs, inputs / 2}, &a.w_stride));
   a.scales = static_cast<float*>(c.rows(scales, "scales", at::kFloat, {outputs, groups}, &a.scales_stride));
   if (arg[3] != Py_None) a.zeros = static_cast<uint8_t*>(c.rows(tensor(arg[3], "zeros"), "zeros", at::kByte, {outputs, groups}, &a.zeros_stride));
-  const at::Tensor out = c.output(arg[5], "out", {rows, outputs});
+  const at::Tensor out = c.output(arg[5], "out", {rows, outputs}, arg[7]);
   a.out = c.rows(out, "out", {rows, outputs}, &a.out_stride);
   const at::Tensor workspace = c.workspace(py.q4_workspace, "fi_q4_matmul_workspace", a, arg[6], arg[7]);
   c.make(py.q4_matmul, "fi_q4_matmul", a, arg[7]);
@@ -339,7 +346,7 @@ PyObject* guarded(PyObject*, PyObject* const* arg, Py_ssize_t n) {
   return nullptr;
 }
 
-// bind(addresses of the six entry points, check, stream, lend)
+// bind(addresses of the six entry points, check, stream, room)
 PyObject* bind(PyObject*, PyObject* const* arg, Py_ssize_t n) {
   if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments, not %zd", n);
   void* at[6];
@@ -356,7 +363,7 @@ PyObject* bind(PyObject*, PyObject* const* arg, Py_ssize_t n) {
   for (int i = 6; i < 9; ++i) Py_INCREF(arg[i]);   // (for the life of the process)
   py.check = arg[6];
   py.stream = arg[7];
-  py.lend = arg[8];
+  py.room = arg[8];
   Py_RETURN_NONE;
 }
 

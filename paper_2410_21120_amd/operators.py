@@ -6,8 +6,9 @@ check that they fit together, fill the argument struct of include/fusedinf.h and
 and the structs are done in csrc/fi_tensors.cpp (a call of fi_qk_norm_rope or fi_q4_matmul takes the host 3 to 4 us that way, in
 Python 11 and 8, more than the kernels of a decoding step).
 
-A tensor that is used on another stream than the one it was made on is the caller's to order, as for any launch.  ValueError
-and TypeError tell what does not fit; what the library itself refuses is FiError.
+A tensor that is used on another stream than the one it was made on is the caller's to order, as for any launch.  What a call makes
+itself (outputs that are None, workspaces) comes from the memory that torch keeps for the call's stream, so `stream` has nothing to wait
+for there; such an output belongs to that stream.  ValueError and TypeError tell what does not fit; what the library itself refuses is FiError.
 """
 from __future__ import annotations
 
@@ -92,12 +93,15 @@ def _load():
         _build.build_tensors()
     from . import _tensors
 
-    def lend(tensor, stream, index):
-        tensor.record_stream(torch.cuda.ExternalStream(stream, device=index))
+    kinds = {"Byte": torch.uint8, "BFloat16": torch.bfloat16, "Float": torch.float32}
+
+    def room(shape, kind, stream, index):
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=index)):
+            return torch.empty(shape, dtype=kinds[kind], device=torch.device("cuda", index))
 
     entries = ("fi_qk_norm_rope", "fi_prompt_attention", "fi_tree_attention", "fi_q4_matmul", "fi_tree_attention_workspace", "fi_q4_matmul_workspace")
     stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-    _tensors.bind(*(C.cast(getattr(library, name), C.c_void_p).value for name in entries), _b._check, stream, lend)
+    _tensors.bind(*(C.cast(getattr(library, name), C.c_void_p).value for name in entries), _b._check, stream, room)
     _ext = _tensors
     return _ext
 

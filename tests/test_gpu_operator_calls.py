@@ -1,0 +1,85 @@
+"""Calls of the decoder operators on tensors: the memory that a call makes for itself, and on which stream."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+@pytest.fixture(scope="module")
+def fi():
+    import paper_2410_21120_amd as fi
+    return fi
+
+
+def _stream_of(torch, t):
+    """The stream whose pool a tensor's memory comes from."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not torch's memory")
+
+
+def _pool(torch, stream):
+    return sum(s["total_size"] for s in torch.cuda.memory_snapshot() if s["stream"] == stream)
+
+
+def _shared_product(torch):
+    """Arguments of a product that needs a workspace."""
+    g = torch.Generator().manual_seed(21)
+    return (torch.randn((9, 12288), generator=g).bfloat16().cuda(), torch.randint(0, 256, (70, 6144), generator=g, dtype=torch.uint8).cuda(),
+            torch.rand((70, 192), generator=g).cuda())
+
+
+def test_what_a_call_makes_on_a_stream_is_that_streams_memory(torch, fi):
+    """Outputs and workspaces made inside a call come from the pool of the call's stream: another pool's block may still be in use on its own stream."""
+    g = torch.Generator().manual_seed(20)
+    q, k = torch.randn((40, 4, 64), generator=g).bfloat16().cuda(), torch.randn((40, 2, 64), generator=g).bfloat16().cuda()
+    cu, positions, freq = torch.tensor([0, 40], dtype=torch.int32).cuda(), torch.arange(40, dtype=torch.int32).cuda(), torch.rand(32, generator=g).cuda()
+    cache, table, cached = k.view(10, 4, 2, 64).clone(), torch.arange(10, dtype=torch.int32)[None].cuda(), torch.tensor([39], dtype=torch.int32).cuda()
+    x, w, s = _shared_product(torch)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls = [lambda **m: fi.qk_norm_rope(q, k, k, positions, freq, **m), lambda **m: (fi.prompt_attention(q, k, k, cu, **m),),
+             lambda **m: (fi.tree_attention(q[:1], cache, cache, table, cached, cu.clamp(max=1), **m),), lambda **m: (fi.q4_matmul(x, w, s, group=64, **m),)]
+    for call in calls:
+        want = call()
+        torch.cuda.synchronize()
+        got = call(stream=side.cuda_stream)
+        side.synchronize()
+        for a, b in zip(got, want):
+            assert _stream_of(torch, a) == side.cuda_stream and _stream_of(torch, b) != side.cuda_stream
+            assert torch.equal(a, b)
+    # the workspace
+    del got, a
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    out = torch.empty((9, 70), dtype=torch.bfloat16, device="cuda")
+    assert _pool(torch, side.cuda_stream) == 0
+    fi.q4_matmul(x, w, s, group=64, out=out, stream=side.cuda_stream)
+    assert _pool(torch, side.cuda_stream) > 0
+    side.synchronize()
+    assert torch.equal(out, want[0])
+
+
+def test_a_block_that_another_stream_is_still_at_work_on(torch, fi):
+    """A temporary of the workspace's size is freed with its kernels pending on the current stream; the call's stream owes that one no wait."""
+    x, w, s = _shared_product(torch)
+    need = fi.fi_q4_matmul_workspace(fi.fi_q4_matmul_args(dtype=fi.FI_BF16, rows=9, inputs=12288, outputs=70, group=64))
+    want = fi.q4_matmul(x, w, s, group=64)
+    side, a = torch.cuda.Stream(), torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(8):
+        a @ a
+    temporary = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for _ in range(200):
+        temporary.fill_(255)   # NaN, to the sums
+    del temporary
+    got = fi.q4_matmul(x, w, s, group=64, stream=side.cuda_stream)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
