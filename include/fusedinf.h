@@ -473,7 +473,8 @@ void fi_destroy(fi_dag* dag);
  *    result is rounded once, when it is stored (attention on bf16 also rounds the weights it multiplies the values with).
  *  - All tensor pointers are device pointers.  Strides are in elements of the tensor's type; the last dimension (head_dim,
  *    inputs, outputs) is contiguous.  Inputs may have any strides >= 0; rows that start on 16-byte boundaries take the fast kernels.
- *    Outputs must not overlap themselves or an input, except that q_out may be q, k_out k and v_out v with equal strides.
+ *    Outputs must not overlap themselves (every dimension, from the shortest stride on, strides over all that the ones before it
+ *    reach) or an input, except that q_out may be q, k_out k and v_out v with equal strides.
  *  - What sits in device memory (offsets, lengths, page and slot numbers) cannot be checked by the call: the kernels clamp
  *    it to the sizes given here, so that nothing outside the tensors is read or written, and the rows concerned are unspecified.
  *  - FI_EINVAL for a null or misaligned pointer, a negative size or stride or sizes that contradict each other,

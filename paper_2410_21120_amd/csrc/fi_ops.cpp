@@ -1,7 +1,9 @@
 // Entry points of the decoder operators: argument checks, then the launch.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "fi_internal.h"
 #include "fi_ops.h"
@@ -31,9 +33,21 @@ bool good_strides(const int64_t* s, int n, const char* name) {
   return true;
 }
 
-// Rows of an output may not share memory: a dimension of more than one entry strides over whole rows of the ones inside it or lies inside one.
-bool apart(int64_t stride, int64_t count, int64_t row, const char* name) {
-  if (count > 1 && stride < row) { set_error("%s: its rows overlap (stride %lld, row %lld)", name, (long long)stride, (long long)row); return false; }
+// Rows of an output (`row` elements each) may not share memory: every dimension, from the shortest stride on, strides over all that the ones before it reach.
+bool apart(std::initializer_list<int64_t> strides, std::initializer_list<int64_t> counts, int64_t row, const char* name) {
+  struct Dim { int64_t stride, count; } dims[3];
+  int n = 0;
+  for (size_t i = 0; i < strides.size(); ++i)
+    if (counts.begin()[i] > 1) dims[n++] = Dim{strides.begin()[i], counts.begin()[i]};
+  std::sort(dims, dims + n, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  __int128 reach = row;
+  for (int i = 0; i < n; ++i) {
+    if (dims[i].stride < reach) {
+      set_error("%s: its rows overlap (a stride of %lld over %.0f elements)", name, (long long)dims[i].stride, (double)reach);
+      return false;
+    }
+    reach += (__int128)dims[i].stride * (dims[i].count - 1);
+  }
   return true;
 }
 
@@ -113,7 +127,7 @@ fi_status fi_qk_norm_rope(const fi_qk_norm_rope_args* args, void* hip_stream) {
   const int es = elem_size(a.dtype), D = a.head_dim;
   if (a.rot_dim && (!good(a.positions, 4, "positions") || !good(a.inv_freq, 4, "inv_freq"))) return FI_EINVAL;
   if (a.q_heads && (!good(a.q, es, "q") || !good(a.q_out, es, "q_out") || !good_strides(a.q_strides, 2, "q") || !good_strides(a.q_out_strides, 2, "q_out") ||
-                    !apart(a.q_out_strides[1], a.q_heads, D, "q_out") || !apart(a.q_out_strides[0], a.tokens, D, "q_out"))) return FI_EINVAL;
+                    !apart({a.q_out_strides[0], a.q_out_strides[1]}, {a.tokens, a.q_heads}, D, "q_out"))) return FI_EINVAL;
   if ((a.q_weight && !good(a.q_weight, 4, "q_weight")) || (a.k_weight && !good(a.k_weight, 4, "k_weight"))) return FI_EINVAL;
   if (a.kv_heads) {
     if (!good(a.k, es, "k") || !good(a.k_out, es, "k_out") || !good_strides(a.k_strides, 2, "k") || !good_strides(a.k_out_strides, 3, "k_out")) return FI_EINVAL;
@@ -123,11 +137,10 @@ fi_status fi_qk_norm_rope(const fi_qk_norm_rope_args* args, void* hip_stream) {
       if (a.page_size < 1 || a.n_slots < 0) set_error("pages of %d tokens, %lld slots", a.page_size, (long long)a.n_slots);
       return FI_EINVAL;
     }
-    const int64_t rows = a.slots ? a.page_size : a.tokens;
+    const int64_t pages = a.slots ? a.n_slots / a.page_size + (a.n_slots % a.page_size != 0) : 1, rows = a.slots ? a.page_size : a.tokens;
     for (int t = 0; t < (a.v ? 2 : 1); ++t) {
       const int64_t* s = t ? a.v_out_strides : a.k_out_strides;
-      const char* name = t ? "v_out" : "k_out";
-      if (!apart(s[2], a.kv_heads, D, name) || !apart(s[1], rows, D, name) || (a.slots && !apart(s[0], a.n_slots / a.page_size, D, name))) return FI_EINVAL;
+      if (!apart({s[0], s[1], s[2]}, {pages, rows, a.kv_heads}, D, t ? "v_out" : "k_out")) return FI_EINVAL;
     }
   }
   return done(launch_qk_norm_rope(a, hip_stream), "fi_qk_norm_rope");
@@ -150,7 +163,7 @@ fi_status fi_prompt_attention(const fi_prompt_attention_args* args, void* hip_st
   if (!good(a.q, es, "q") || !good(a.out, es, "out") || !good(a.cu_q, 4, "cu_q") || !good(a.cu_k, 4, "cu_k")) return FI_EINVAL;
   if (a.k_tokens && (!good(a.k, es, "k") || !good(a.v, es, "v"))) return FI_EINVAL;
   if (!good_strides(a.q_strides, 2, "q") || !good_strides(a.k_strides, 2, "k") || !good_strides(a.v_strides, 2, "v") || !good_strides(a.out_strides, 2, "out")) return FI_EINVAL;
-  if (!apart(a.out_strides[0], a.q_tokens, a.head_dim, "out") || !apart(a.out_strides[1], a.q_heads, a.head_dim, "out")) return FI_EINVAL;
+  if (!apart({a.out_strides[0], a.out_strides[1]}, {a.q_tokens, a.q_heads}, a.head_dim, "out")) return FI_EINVAL;
   return done(launch_prompt_attention(a, hip_stream), "fi_prompt_attention");
 }
 
@@ -175,7 +188,7 @@ fi_status fi_tree_attention(const fi_tree_attention_args* args, void* hip_stream
   }
   if (!good_strides(a.q_strides, 2, "q") || !good_strides(a.k_strides, 3, "k_cache") || !good_strides(a.v_strides, 3, "v_cache") || !good_strides(a.out_strides, 2, "out") ||
       !good_strides(&a.table_stride, 1, "block_table")) return FI_EINVAL;
-  if (!apart(a.out_strides[0], a.nodes, a.head_dim, "out") || !apart(a.out_strides[1], a.q_heads, a.head_dim, "out")) return FI_EINVAL;
+  if (!apart({a.out_strides[0], a.out_strides[1]}, {a.nodes, a.q_heads}, a.head_dim, "out")) return FI_EINVAL;
   if (!good_workspace(a.workspace, a.workspace_bytes, tree_workspace(a))) return FI_EINVAL;
   return done(launch_tree_attention(a, hip_stream), "fi_tree_attention");
 }
@@ -196,7 +209,7 @@ fi_status fi_q4_matmul(const fi_q4_matmul_args* args, void* hip_stream) {
   if (!good(a.out, es, "out")) return FI_EINVAL;
   if (a.inputs && (!good(a.x, es, "x") || !good(a.w, 1, "w") || !good(a.scales, 4, "scales"))) return FI_EINVAL;
   const int64_t strides[5] = {a.x_stride, a.w_stride, a.scales_stride, a.zeros ? a.zeros_stride : 0, a.out_stride};
-  if (!good_strides(strides, 5, "x, w, scales, zeros or out") || !apart(a.out_stride, a.rows, a.outputs, "out")) return FI_EINVAL;
+  if (!good_strides(strides, 5, "x, w, scales, zeros or out") || !apart({a.out_stride}, {a.rows}, a.outputs, "out")) return FI_EINVAL;
   if (!good_workspace(a.workspace, a.workspace_bytes, q4_workspace(a))) return FI_EINVAL;
   return done(launch_q4_matmul(a, hip_stream), "fi_q4_matmul");
 }

@@ -83,3 +83,23 @@ def test_a_block_that_another_stream_is_still_at_work_on(torch, fi):
     side.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_outputs_of_any_order(torch, fi):
+    """Heads in front of tokens, in outputs and caches: the rows lie apart, so they are taken, and hold what others do."""
+    g = torch.Generator().manual_seed(22)
+    q, k = torch.randn((40, 4, 64), generator=g).bfloat16().cuda(), torch.randn((40, 2, 64), generator=g).bfloat16().cuda()
+    cu, positions, freq = torch.tensor([0, 40], dtype=torch.int32).cuda(), torch.arange(40, dtype=torch.int32).cuda(), torch.rand(32, generator=g).cuda()
+    turned = lambda heads: torch.zeros((heads, 40, 64), dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    want = fi.qk_norm_rope(q, k, k, positions, freq)
+    got = fi.qk_norm_rope(q, k, k, positions, freq, q_out=turned(4), k_out=turned(2), v_out=turned(2))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(fi.prompt_attention(q, k, k, cu, out=turned(4)), fi.prompt_attention(q, k, k, cu))
+    caches = torch.zeros((2, 5, 2, 8, 64), dtype=torch.bfloat16, device="cuda").transpose(2, 3)   # 5 pages of 8 tokens
+    slots = torch.randperm(40, generator=g).cuda()
+    fi.qk_norm_rope(q, k, k, positions, freq, slots=slots, k_out=caches[0], v_out=caches[1])
+    flat = caches.reshape(2, 40, 2, 64)
+    assert torch.equal(flat[0][slots], want[1]) and torch.equal(flat[1][slots], want[2])
+    table, cached, one = torch.arange(5, dtype=torch.int32)[None].cuda(), torch.tensor([20], dtype=torch.int32).cuda(), cu.clamp(max=20)
+    plain = caches.contiguous()
+    assert torch.equal(fi.tree_attention(q[:20], caches[0], caches[1], table, cached, one, out=turned(4)[:20]), fi.tree_attention(q[:20], plain[0], plain[1], table, cached, one))

@@ -1,0 +1,24 @@
+"""What the decoder operators refuse beyond single arguments: outputs whose rows share memory (no device is touched: the checks come before any launch)."""
+import pytest
+
+import paper_2410_21120_amd as fi
+from tests.test_host_operators import P, prompt, rope, tree
+
+PAGED = dict(slots=P, page_size=16, n_slots=64, k_out_page=2048, v_out_page=2048)   # 4 pages of 16 tokens, 2 heads of 64
+OVERLAPPING = [
+    # (token 0, head 1) and (token 1, head 0) are one row, or share a part of one
+    (rope, dict(q_out_token=64, q_out_head=64)), (rope, dict(q_out_token=255)), (rope, dict(q_out_token=64, q_out_head=191)), (rope, dict(k_out_token=64)),
+    (rope, dict(v_out_token=127, v_out_head=64)), (prompt, dict(out_token=64, out_head=64)), (prompt, dict(out_token=255)), (prompt, dict(out_token=64, out_head=190)),
+    (tree, dict(out_token=64, out_head=64)), (tree, dict(out_token=192)),
+    # pages
+    (rope, dict(PAGED, k_out_page=64)), (rope, dict(PAGED, v_out_page=2047)), (rope, dict(PAGED, k_out_token=64, k_out_head=64)),
+    (rope, dict(PAGED, k_out_page=64, k_out_token=256, k_out_head=255)), (rope, dict(PAGED, v_out_token=127)),
+]
+
+
+@pytest.mark.parametrize("make,change", OVERLAPPING, ids=lambda v: getattr(v, "__name__", None) or "-".join(v))
+def test_outputs_whose_rows_share_memory_are_refused(make, change):
+    call, args = make(**change)
+    with pytest.raises(fi.FiError) as e:
+        call(args)
+    assert e.value.status == fi.FI_EINVAL and "overlap" in fi.fi_last_error()
