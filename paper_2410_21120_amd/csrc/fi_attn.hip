@@ -853,18 +853,33 @@ __device__ __forceinline__ void along_the_line(const fi_tree_attention_args& a, 
 }
 // Shares of a sequence's keys in direct calls: `splits` at most, of `least` tiles or more.
 __device__ __forceinline__ int shares(const TreeSplit& p, int keys) { return clamp_int((tiles_of(keys, p.unit) + p.least - 1) / p.least, 1, p.splits); }
-// Direct: the grid is sequences and blocks, key heads, parts.
+// Direct: the grid is sequences and blocks, key heads, parts.  Every sequence has `blocks` blocks, or (packed, blocks 0) sequence b those from its first row over the
+// rows of a block, plus b, on: enough for its rows wherever they start, and no more than one for each sequence than rows fill.
 __device__ __forceinline__ bool tree_direct(const fi_tree_attention_args& a, const TreeSplit& p, TreeWork& w) {
-  const int b = p.blocks == 1 ? blockIdx.x : blockIdx.x / p.blocks;
+  int b;
+  if (p.blocks > 0) {
+    b = p.blocks == 1 ? blockIdx.x : blockIdx.x / p.blocks;
+    w.block = blockIdx.x - b * p.blocks;
+  } else {
+    const int group = a.q_heads / a.kv_heads, id = blockIdx.x, total = (int)a.nodes;
+    auto begins = [&](int s) { return clamp_int(a.cu_nodes[s], 0, total) * group / p.rows + s; };
+    b = 0;
+    for (int hi = a.n_seqs - 1; b < hi;) {
+      const int mid = (b + hi + 1) >> 1;
+      if (begins(mid) <= id) b = mid;
+      else hi = mid - 1;
+    }
+    w.block = id - begins(b);
+    if (w.block < 0) return false;   // (offsets that do not ascend)
+  }
   tree_sequence(a, b, w);
-  w.block = blockIdx.x - b * p.blocks;
   w.hk = blockIdx.y;
   w.split = blockIdx.z;
   w.splits = shares(p, w.keys);
   const int tiles = w.keys ? tiles_of(w.keys, p.unit) : 0;
   w.t0 = (int)((int64_t)tiles * w.split / w.splits);
   w.t1 = (int)((int64_t)tiles * (w.split + 1) / w.splits);
-  return w.split < w.splits && w.block * p.rows < w.nodes * (a.q_heads / a.kv_heads);
+  return w.split < w.splits && (int64_t)w.block * p.rows < w.nodes * (a.q_heads / a.kv_heads);
 }
 
 // Which of the 32 keys from `key` on a node (place `node` in its tree, mask row `words`) sees.
@@ -1199,6 +1214,7 @@ int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
   const int db = blocks_of(a.head_dim);
   if constexpr (sizeof(T) == 2) {
     if (prompt_is_long(a)) {
+      if (!one_launch((a.q_tokens / LONG_ROWS + a.n_seqs) * a.q_heads, 512)) return kTooLarge;
       const dim3 grid((uint32_t)((a.q_tokens / LONG_ROWS + a.n_seqs) * a.q_heads));
       if (db == 2) prompt_long_kernel<2, 64><<<grid, 512, 0, s>>>(a);
       else if (db == 3 && a.head_dim <= 80) prompt_long_kernel<3, 80><<<grid, 512, 0, s>>>(a);
@@ -1209,6 +1225,7 @@ int launch_prompt_tiles(const fi_prompt_attention_args& a, hipStream_t s) {
   }
   // two groups where there is a workgroup or so per compute unit, and a walk is long (12 heads, 7 sequences up to 1000 tokens, spread over their logarithm: heads of 64 19.8 us
   // with one group, 16.4; of 128 27.1, 25.7; up to 301: 8.7, 8.4; 11.5, 12.7)
+  if (!one_launch((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads, 64 * PROMPT_WAVES)) return kTooLarge;   // (two groups: 511 workgroups at most)
   const dim3 grid((uint32_t)((a.q_tokens / PROMPT_ROWS + a.n_seqs) * a.q_heads));
   const bool two = (int64_t)grid.x < 512 && a.k_tokens >= (db == 2 ? 128 : 256) * (int64_t)a.n_seqs;
   if (db == 2) prompt_waves<T, 2, 64>(a, grid, two, s);
@@ -1228,7 +1245,7 @@ bool tree_on_tiles(const fi_tree_attention_args& a) {
 
 // How a tree call is shared out, from its sizes alone (the workspace goes by it): rows of 32 whose waves have keys of their own, or of 128 or 256 that
 // share them; parts of every sequence's keys, and the least keys of a part.
-struct TreePlan { bool own, small, counted; int waves, blocks, splits, least, header; };
+struct TreePlan { bool own, small, counted; int waves, blocks, splits, least, header; int64_t packed; };   // packed: blocks of all sequences together, if so dealt out
 TreePlan plan_tree(const fi_tree_attention_args& a) {
   TreePlan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
@@ -1236,7 +1253,8 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   // Blocks of 32 rows with keys of their own, too, where the workgroups are few (us, shared / own; 64 nodes of one sequence of 100 keys, 8 heads 17.3 / 12.6), or keys are and
   // the workgroups many (about 10 keys, 40 nodes: 61 sequences of 32 heads 53 / 25, 16 nodes of 8 heads 15.8 / 10.9; 12 sequences, 60 keys 12.0 / 13.8).
   const int64_t streams = (int64_t)a.n_seqs * a.kv_heads;
-  p.own = rows <= 32 || streams * ((rows + 31) / 32) * (((int64_t)a.max_length + 127) / 128) <= 256 ||
+  auto some = [](int64_t n) { return n < 1 << 20 ? n : 1 << 20; };   // (products of two stay in 64 bits)
+  p.own = rows <= 32 || some(streams * ((rows + 31) / 32)) * (((int64_t)a.max_length + 127) / 128) <= 256 ||
           (a.max_length <= 256 && streams * ((rows + 32 * p.waves - 1) / (32 * p.waves)) > 256);
   const int64_t per_block = p.own ? 32 : 32 * p.waves;
   p.blocks = (int)((rows + per_block - 1) / per_block);
@@ -1244,7 +1262,7 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
   p.least = p.own ? 128 : 512;
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
-  p.counted = a.n_seqs > 1 && a.n_seqs <= SEQS && parts(p.least) > 1 && units * parts(p.least) > 256 && line < 2147483648.0;
+  p.counted = a.n_seqs > 1 && a.n_seqs <= SEQS && parts(p.least) > 1 && some(units) * parts(p.least) > 256 && line < 2147483648.0;
   // One wave, several workgroups on a compute unit (us, else / so; one node of 14 sequences of 32 heads: 7 keys 12.7 / 7.4, 100 keys 15.9 / 13.4; 64 of 32: 120 keys 64 / 32,
   // 240 85 / 56; 64 of 8: 240 keys 21.2 / 21.4; 12 nodes of 61 sequences of 32 heads, no history 46 / 10).
   p.small = p.own && (a.max_length <= 32 || (a.max_length <= 128 && units > 256) || (a.max_length <= 256 && units > 1024));
@@ -1255,40 +1273,47 @@ TreePlan plan_tree(const fi_tree_attention_args& a) {
   } else {
     // Four rounds of workgroups (4 x 131072 keys: one round 398 us, four 383: the hardware hands them out as units come free); parts of fewer keys where that
     // does not even make one (2 sequences of 1000 keys, 20 nodes: 22.7 us, 15.2).
-    if (!p.own && units * parts(512) <= 256)
-      while (p.least > 128 && units * parts(p.least - 128) <= 256) p.least -= 128;
+    if (!p.own && some(units) * parts(512) <= 256)
+      while (p.least > 128 && some(units) * parts(p.least - 128) <= 256) p.least -= 128;
     splits = units > 0 ? (1023 + units) / units : 1;
   }
   if (splits > parts(p.least)) splits = parts(p.least);
   // the workspace stays below 64 MB as far as the chip is full
   const int64_t room = (64ll << 20) / ((int64_t)a.nodes * a.q_heads * (a.head_dim + 2) * 4 + 1);
-  if (splits > room && splits * units > 512) splits = room * units > 512 ? room : (512 + units - 1) / units;
+  if (splits > room && splits * some(units) > 512) splits = room * some(units) > 512 ? room : (512 + units - 1) / units;
   p.splits = splits < 1 ? 1 : splits > 63 ? 63 : (int)splits;
   if (p.splits == 1) p.counted = false;
   if (p.counted) ++p.splits;   // (a stretch may begin and end inside a part)
   if (p.small) p.counted = false, p.splits = 1;
   p.header = p.counted ? 4 + (a.n_seqs + 3) / 4 * 4 : 0;
+  // Blocks for the most nodes of every sequence grow with sequences times nodes where one may have them all (max_nodes left out): past what a launch takes, and mostly without rows.
+  // Packed ones cost a search for the sequence (us, single tokens of 32 heads of 128 with nothing said about them, direct / packed, and direct with max_nodes 1: 64 of 40 keys
+  // 21.8 / 9.5, 8.5; 512 of 500 1895 / 285, 235; 2048 of 40 3436 / 100, 94).
+  const int64_t packed = a.nodes * (a.q_heads / a.kv_heads) / per_block + a.n_seqs;
+  p.packed = !p.counted && (int64_t)a.n_seqs * p.blocks > 4 * packed ? packed : 0;
   return p;
 }
 template <typename T, int DB>
 int launch_tree_db(const fi_tree_attention_args& a, const TreePlan& p, hipStream_t s) {
   using TL = Tile<T, DB>;
   const int unit = p.own ? 32 : Shared<T, DB, 4>::KEYS;
-  const TreeSplit t = {p.splits, p.least / unit, unit, stretch(p.own, TL::F32).over, p.own ? 32 : 32 * p.waves, p.blocks, p.header};
+  const TreeSplit t = {p.splits, p.least / unit, unit, stretch(p.own, TL::F32).over, p.own ? 32 : 32 * p.waves, p.packed ? 0 : p.blocks, p.header};
+  const int64_t direct = p.packed ? p.packed : (int64_t)a.n_seqs * p.blocks, all_rows = a.nodes * a.q_heads;
+  if (!p.counted && !one_launch(direct, p.small ? 64 : p.own ? 64 * Own<T, DB>::WAVES : 64 * p.waves)) return kTooLarge;
+  if (p.splits > 1 && !one_launch((all_rows + 3) / 4, 256)) return kTooLarge;
   if (p.counted) {   // as many workgroups as run at a time: by LDS one on a compute unit, of the smallest heads two
     const dim3 grid(TL::PB == 128 && (p.own || p.waves == 4) ? 512 : 256);
     if (p.own) tree_own_kernel<T, DB, true, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
     else if (p.waves == 4) tree_tile_kernel<T, DB, 4, true><<<grid, 256, 0, s>>>(a, t);
     else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, true><<<grid, 512, 0, s>>>(a, t);
   } else {
-    const dim3 grid((uint32_t)(a.n_seqs * p.blocks), (uint32_t)a.kv_heads, (uint32_t)p.splits);
+    const dim3 grid((uint32_t)direct, (uint32_t)a.kv_heads, (uint32_t)p.splits);
     if (p.own && p.small) tree_own_kernel<T, DB, false, true><<<grid, 64, 0, s>>>(a, t);
     else if (p.own) tree_own_kernel<T, DB, false, false><<<grid, 64 * Own<T, DB>::WAVES, 0, s>>>(a, t);
     else if (p.waves == 4) tree_tile_kernel<T, DB, 4, false><<<grid, 256, 0, s>>>(a, t);
     else if constexpr (DB <= 4) tree_tile_kernel<T, DB, 8, false><<<grid, 512, 0, s>>>(a, t);
   }
   constexpr int PER = DB <= 2 ? 1 : DB <= 4 ? 2 : 4;
-  const int64_t all_rows = a.nodes * a.q_heads;
   if (p.splits > 16 && all_rows <= 1024) tree_join_kernel<T, PER, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, t, p.counted);
   else if (p.splits > 1) tree_join_kernel<T, PER, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, t, p.counted);
   return (int)hipGetLastError();
@@ -1309,6 +1334,7 @@ int launch_tree_tiles(const fi_tree_attention_args& a, hipStream_t s) {
 int launch_prompt_attention(const fi_prompt_attention_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (prompt_on_tiles(a)) return a.dtype == FI_F32 ? launch_prompt_tiles<float>(a, s) : launch_prompt_tiles<bf16_t>(a, s);
+  if (!one_launch(a.q_tokens, 64)) return kTooLarge;
   const dim3 grid((uint32_t)a.q_tokens, (uint32_t)a.q_heads);
   if (a.dtype == FI_F32) prompt_row_kernel<float><<<grid, 64, 0, s>>>(a);
   else prompt_row_kernel<bf16_t><<<grid, 64, 0, s>>>(a);
@@ -1323,6 +1349,7 @@ uint64_t tree_workspace(const fi_tree_attention_args& a) {
 int launch_tree_attention(const fi_tree_attention_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (tree_on_tiles(a)) return a.dtype == FI_F32 ? launch_tree_tiles<float>(a, s) : launch_tree_tiles<bf16_t>(a, s);
+  if (!one_launch(a.nodes, 64)) return kTooLarge;
   const dim3 grid((uint32_t)a.nodes, (uint32_t)a.q_heads);
   if (a.dtype == FI_F32) tree_row_kernel<float><<<grid, 64, 0, s>>>(a);
   else tree_row_kernel<bf16_t><<<grid, 64, 0, s>>>(a);

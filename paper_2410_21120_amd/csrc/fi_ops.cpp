@@ -16,6 +16,10 @@ constexpr int64_t kStride = 1ll << 40; // elements: products of strides and indi
 
 fi_status done(int e, const char* where) {
   if (e == 0) return FI_OK;
+  if (e == kTooLarge) {
+    set_error("%s: more work than one launch takes", where);
+    return FI_EUNSUPPORTED;
+  }
   set_error("%s: %s", where, hipGetErrorString(static_cast<hipError_t>(e)));
   return FI_EHIP;
 }

@@ -213,7 +213,8 @@ int launch_np(const fi_qk_norm_rope_args& a, hipStream_t s) {
   int bits = 0;
   auto waves = [&] { return (int64_t)a.tokens << bits; };
   while ((2 << bits <= most && waves() < FEWEST_WAVES) || (1 << bits < most && waves() < LATENCY_WAVES)) ++bits;
-  const dim3 grid((uint32_t)((((int64_t)a.tokens << bits) + 3) / 4));
+  if (!one_launch((waves() + 3) / 4, 256)) return kTooLarge;
+  const dim3 grid((uint32_t)((waves() + 3) / 4));
   if (a.interleaved) rope_kernel<T, NP, ITEMS, true><<<grid, 256, 0, s>>>(a, lanes, bits);
   else rope_kernel<T, NP, ITEMS, false><<<grid, 256, 0, s>>>(a, lanes, bits);
   return (int)hipGetLastError();

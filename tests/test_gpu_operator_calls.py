@@ -103,3 +103,21 @@ def test_outputs_of_any_order(torch, fi):
     table, cached, one = torch.arange(5, dtype=torch.int32)[None].cuda(), torch.tensor([20], dtype=torch.int32).cuda(), cu.clamp(max=20)
     plain = caches.contiguous()
     assert torch.equal(fi.tree_attention(q[:20], caches[0], caches[1], table, cached, one, out=turned(4)[:20]), fi.tree_attention(q[:20], plain[0], plain[1], table, cached, one))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_thousands_of_single_tokens_with_nothing_said_about_them(torch, fi, dtype):
+    """Without max_nodes a sequence may have all the nodes: the workgroups grow with the nodes and the sequences, not with their product."""
+    n, hq, hk, d, before = 24000, 8, 2, 64, 3
+    kind, g = getattr(torch, dtype), torch.Generator(device="cuda").manual_seed(23)
+    q = torch.randn((n, hq, d), generator=g, device="cuda").to(kind)
+    k, v = (torch.randn((n, before + 1, hk, d), generator=g, device="cuda").to(kind) for _ in range(2))   # a page a sequence
+    table = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[:, None]
+    cached, cu = torch.full((n,), before, dtype=torch.int32, device="cuda"), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    got = fi.tree_attention(q, k, v, table, cached, cu, out=torch.full_like(q, float("nan"))).double()
+    keys, values = (x[table[:, 0].long()].double().repeat_interleave(hq // hk, 2) for x in (k, v))   # [n, keys, heads, d]
+    p = torch.softmax((q.double()[:, None] * keys).sum(-1) * d ** -0.5, 1)[..., None]
+    want, size = (p * values).sum(1), (p * values.abs()).sum(1)
+    # a score: d + 2 roundings of sum |q k|, at most |q| |k| < 256; a weight of bf16 and a result of bf16 a rounding each
+    u, h = 2.0 ** -24, 2.0 ** -8 if dtype == "bfloat16" else 0.0
+    assert ((got - want).abs() <= size * (2 * (d + 2) * 256 * d ** -0.5 * u + 200 * u + 1.01 * h) + want.abs() * 1.01 * h + 1e-30).all()

@@ -22,3 +22,19 @@ def test_outputs_whose_rows_share_memory_are_refused(make, change):
     with pytest.raises(fi.FiError) as e:
         call(args)
     assert e.value.status == fi.FI_EINVAL and "overlap" in fi.fi_last_error()
+
+
+MORE_THAN_A_LAUNCH = [
+    # 2^32 threads and more along a grid's first dimension: well-formed, not covered, nothing launched
+    (rope, dict(tokens=1 << 27)), (prompt, dict(q_tokens=1 << 30, k_tokens=1 << 30)), (prompt, dict(q_tokens=1 << 27, q_token=257)),
+    (prompt, dict(n_seqs=1 << 25, q_tokens=1 << 25)), (tree, dict(nodes=1 << 27, q_token=257)), (tree, dict(nodes=1 << 28, n_seqs=1 << 28, max_nodes=1)),
+    (tree, dict(nodes=1 << 28, n_seqs=1 << 28, max_nodes=1 << 28)), (tree, dict(nodes=1 << 28, n_seqs=1 << 28, max_nodes=1 << 28, dtype=fi.FI_F32)),
+]
+
+
+@pytest.mark.parametrize("make,change", MORE_THAN_A_LAUNCH, ids=lambda v: getattr(v, "__name__", None) or "-".join(v))
+def test_more_work_than_a_launch_takes_is_refused(make, change):
+    call, args = make(**change)
+    with pytest.raises(fi.FiError) as e:
+        call(args)
+    assert e.value.status == fi.FI_EUNSUPPORTED and "launch" in fi.fi_last_error()
