@@ -546,7 +546,7 @@ typedef struct {
   int32_t page_size, n_pages;    /* tokens per page, pages of the caches */
   int32_t table_columns;         /* pages that a row of block_table names; page_size * table_columns below 2^31 - 1024 */
   int32_t mask_words;            /* 64-bit words per node; a sequence has at most 64 * mask_words nodes (later ones are not seen).  0 without a mask */
-  int32_t max_nodes;             /* most nodes of a sequence: later ones are not computed */
+  int32_t max_nodes;             /* most nodes of a sequence: later ones are neither computed nor seen */
   int32_t max_length;            /* most committed tokens and nodes of a sequence together; only guides how the work is shared out */
   float scale;                   /* finite, > 0 */
   int64_t nodes;                 /* rows of q and out, of all sequences; nodes * q_heads below 2^31 - 1024 */

@@ -93,10 +93,10 @@ __global__ void __launch_bounds__(64) tree_row_kernel(fi_tree_attention_args a) 
   __shared__ float lds[FI_MAX_HEAD_DIM];
   const int row = blockIdx.x, h = blockIdx.y, hk = h / (a.q_heads / a.kv_heads);
   const int b = find_seq(a.cu_nodes, a.n_seqs, row), total = (int)a.nodes;
-  const int n0 = clamp_int(a.cu_nodes[b], 0, total), n1 = clamp_int(a.cu_nodes[b + 1], n0, total);
+  const int n0 = clamp_int(a.cu_nodes[b], 0, total), all = clamp_int(a.cu_nodes[b + 1], n0, total) - n0, nodes = all < a.max_nodes ? all : a.max_nodes;
   if (row - n0 >= a.max_nodes) return;
   const int places = a.n_pages ? a.page_size * a.table_columns : 0;
-  const int cached = clamp_int(a.cached[b], 0, places), keys = n1 - n0 < places - cached ? cached + n1 - n0 : places;
+  const int cached = clamp_int(a.cached[b], 0, places), keys = nodes < places - cached ? cached + nodes : places;
   const int32_t* const table = a.block_table + b * a.table_stride;
   auto seen = [&](int j) {
     const int node = j - cached;

@@ -131,7 +131,7 @@ def tree_attention(q, k_cache, v_cache, block_table, cached, cu_nodes, mask=None
     q [nodes, q heads, head dim], packed by cu_nodes (int32 [sequences + 1]); k_cache and v_cache [pages, page size, kv heads, head dim];
     block_table int32 [sequences, columns]; cached int32 [sequences]: committed tokens, whose pages the nodes' own keys and values follow;
     mask int64 [nodes, words]: bit j of a row is set where the node sees node j of its sequence, None for chains.
-    max_nodes: most nodes of a sequence (default: all nodes), max_length: most committed tokens and nodes together (default: what
+    max_nodes: most nodes of a sequence, later ones are neither computed nor seen (default: all nodes), max_length: most committed tokens and nodes together (default: what
     the table can name; it guides how the work is shared out).  workspace: uint8, fi_tree_attention_workspace bytes; made here if
     None.  Returns out [nodes, q heads, head dim]."""
     return (_ext or _load()).tree_attention(q, k_cache, v_cache, block_table, cached, cu_nodes, mask, scale, max_nodes, max_length, out, workspace, stream)

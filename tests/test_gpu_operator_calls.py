@@ -121,3 +121,26 @@ def test_thousands_of_single_tokens_with_nothing_said_about_them(torch, fi, dtyp
     # a score: d + 2 roundings of sum |q k|, at most |q| |k| < 256; a weight of bf16 and a result of bf16 a rounding each
     u, h = 2.0 ** -24, 2.0 ** -8 if dtype == "bfloat16" else 0.0
     assert ((got - want).abs() <= size * (2 * (d + 2) * 256 * d ** -0.5 * u + 200 * u + 1.01 * h) + want.abs() * 1.01 * h + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("nodes", [5, 90])
+def test_nodes_past_max_nodes_are_neither_computed_nor_seen(torch, fi, dtype, nodes):
+    """Whatever the strides: rows that start on odd elements go to another kernel."""
+    kind, g, most, before, d = getattr(torch, dtype), torch.Generator().manual_seed(24), nodes - 3, 10, 64
+    q = torch.randn((nodes, 4, d), generator=g).to(kind)
+    kv = torch.randn((2, (before + nodes + 15) // 16, 16, 2, d), generator=g).to(kind)
+    mask = torch.full((nodes, 2), -1, dtype=torch.int64).cuda()   # every node sees every node
+    table = torch.arange(kv.shape[1], dtype=torch.int32)[None].cuda()
+    cached, cu = torch.tensor([before], dtype=torch.int32).cuda(), torch.tensor([0, nodes], dtype=torch.int32).cuda()
+    k, v = kv.flatten(1, 2)[:, :before + most].double().repeat_interleave(2, 2)
+    p = torch.softmax(torch.einsum("nhd,khd->hnk", q[:most].double(), k) * d ** -0.5, 2)
+    want, size = torch.einsum("hnk,khd->nhd", p, v), torch.einsum("hnk,khd->nhd", p, v.abs())
+    u, h = 2.0 ** -24, 2.0 ** -8 if dtype == "bfloat16" else 0.0
+    bound = size * (2 * (d + 2) * 256 * d ** -0.5 * u + 400 * u + 1.01 * h) + want.abs() * 1.01 * h + 1e-30
+    for pad in (0, 3):
+        wide = torch.zeros((*kv.shape[:-1], d + pad), dtype=kind).cuda()
+        wide[..., pad:] = kv.cuda()
+        out = torch.full(q.shape, 7.0, dtype=kind).cuda()
+        fi.tree_attention(q.cuda(), wide[0][..., pad:], wide[1][..., pad:], table, cached, cu, mask, max_nodes=most, out=out)
+        assert ((out[:most].double().cpu() - want).abs() <= bound).all() and (out[most:] == 7).all()
