@@ -5,6 +5,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -48,9 +49,14 @@ struct {
   PyObject *room;     // room(shape, type, stream, device index): a tensor from the memory that torch keeps for that stream
 } py;
 
+// The operators have no gradients: a call that would have to be recorded for one is refused.
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "%s is no tensor", name);
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && c10::GradMode::is_enabled()) refuse(PyExc_ValueError, "%s requires a gradient, and there is none: detach it, or call under torch.no_grad()", name);
+  if (t._fw_grad(0).defined()) refuse(PyExc_ValueError, "%s has a tangent, and there is no forward derivative: detach it", name);
+  if (t.is_neg()) refuse(PyExc_ValueError, "%s is a negated view: resolve_neg() makes its values", name);
+  return t;
 }
 int32_t int32(int64_t v, const char* name) {
   if (v < INT32_MIN || v > INT32_MAX) refuse(PyExc_ValueError, "%s: %lld does not fit 32 bits", name, (long long)v);
@@ -171,6 +177,7 @@ struct Call {
 
 PyObject* returned(PyObject* given, const at::Tensor& t) {
   if (given == Py_None) return THPVariable_Wrap(t);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // (tells autograd that the values of a caller's output have changed)
   Py_INCREF(given);
   return given;
 }

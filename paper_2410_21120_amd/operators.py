@@ -8,7 +8,8 @@ Python 11 and 8, more than the kernels of a decoding step).
 
 A tensor that is used on another stream than the one it was made on is the caller's to order, as for any launch.  What a call makes
 itself (outputs that are None, workspaces) comes from the memory that torch keeps for the call's stream, so `stream` has nothing to wait
-for there; such an output belongs to that stream.  ValueError and TypeError tell what does not fit; what the library itself refuses is FiError.
+for there; such an output belongs to that stream.  There are no gradients: a tensor that requires one is refused
+unless torch's gradient mode is off, and outputs count as changed in place.  ValueError and TypeError tell what does not fit; what the library itself refuses is FiError.
 """
 from __future__ import annotations
 

@@ -144,3 +144,44 @@ def test_nodes_past_max_nodes_are_neither_computed_nor_seen(torch, fi, dtype, no
         out = torch.full(q.shape, 7.0, dtype=kind).cuda()
         fi.tree_attention(q.cuda(), wide[0][..., pad:], wide[1][..., pad:], table, cached, cu, mask, max_nodes=most, out=out)
         assert ((out[:most].double().cpu() - want).abs() <= bound).all() and (out[most:] == 7).all()
+
+
+def test_no_gradients_and_outputs_that_count_as_changed(torch, fi):
+    """Every tensor of every call: refused where it requires a gradient, taken without gradient mode; what autograd has saved of an output is known to be stale."""
+    g = torch.Generator().manual_seed(25)
+    q, k = torch.randn((40, 4, 64), generator=g).cuda(), torch.randn((40, 2, 64), generator=g).cuda()
+    cu, positions, freq, ones = torch.tensor([0, 40], dtype=torch.int32).cuda(), torch.arange(40, dtype=torch.int32).cuda(), torch.rand(32, generator=g).cuda(), torch.ones(64).cuda()
+    cache, table, cached = k.view(10, 4, 2, 64).clone(), torch.arange(10, dtype=torch.int32)[None].cuda(), torch.tensor([39], dtype=torch.int32).cuda()
+    x, w, s = torch.randn((3, 256), generator=g).cuda(), torch.randint(0, 256, (8, 128), generator=g, dtype=torch.uint8).cuda(), torch.rand((8, 4), generator=g).cuda()
+    calls = [
+        (fi.qk_norm_rope, dict(q=q, k=k, v=k.clone(), positions=positions, inv_freq=freq, q_weight=ones, k_weight=ones.clone(), slots=torch.arange(40).cuda(),
+                               q_out=torch.zeros_like(q), k_out=torch.zeros_like(cache), v_out=torch.zeros_like(cache)), ("q_out", "k_out", "v_out")),
+        (fi.prompt_attention, dict(q=q, k=k, v=k.clone(), cu_q=cu, out=torch.zeros_like(q)), ("out",)),
+        (fi.tree_attention, dict(q=q[:1].clone(), k_cache=cache, v_cache=cache.clone(), block_table=table, cached=cached, cu_nodes=cu.clamp(max=1), out=torch.zeros_like(q[:1])), ("out",)),
+        (fi.q4_matmul, dict(x=x, w=w, scales=s, out=torch.zeros((3, 8)).cuda()), ("out",)),
+    ]
+    for call, args, outs in calls:
+        call(**args)
+        want = [args[o].clone() for o in outs]
+        for name, t in args.items():
+            if not t.is_floating_point():
+                continue
+            wants = t.detach().clone().requires_grad_()
+            with pytest.raises(ValueError, match=name + " requires a gradient"):
+                call(**{**args, name: wants})
+            with torch.no_grad():
+                call(**{**args, name: wants})
+        assert all(torch.equal(args[o], y) for o, y in zip(outs, want))
+        for o in outs:
+            before = args[o]._version
+            call(**args)
+            assert args[o]._version == before + 1
+        factor = torch.ones((), device="cuda", requires_grad=True)
+        loss = (factor * args[outs[0]]).sum()   # (saves the output)
+        call(**args)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        with torch.inference_mode():
+            made = torch.zeros_like(args[outs[0]])
+        call(**{**args, outs[0]: made})   # inference tensors have no counter
+        assert torch.equal(made, want[0])

@@ -38,3 +38,21 @@ def test_more_work_than_a_launch_takes_is_refused(make, change):
     with pytest.raises(fi.FiError) as e:
         call(args)
     assert e.value.status == fi.FI_EUNSUPPORTED and "launch" in fi.fi_last_error()
+
+
+def test_tensors_that_want_a_derivative_are_refused():
+    """There is none to give: a result that is cut off from its inputs would train nothing, in silence."""
+    import torch
+    from torch.autograd import forward_ad
+    x, cu = torch.zeros((2, 4, 64)), torch.tensor([0, 2], dtype=torch.int32)
+    wants = torch.zeros((2, 4, 64), requires_grad=True)
+    for q, k, v in ((wants, x, x), (x, wants, x), (x, x, wants * 2)):
+        with pytest.raises(ValueError, match="gradient"):
+            fi.prompt_attention(q, k, v, cu)
+        with torch.no_grad(), pytest.raises(ValueError, match="device memory"):
+            fi.prompt_attention(q, k, v, cu)
+    with forward_ad.dual_level():
+        with pytest.raises(ValueError, match="tangent"):
+            fi.prompt_attention(forward_ad.make_dual(x, torch.ones_like(x)), x, x, cu)
+    with pytest.raises(ValueError, match="negated"):
+        fi.prompt_attention(x, torch._neg_view(x), x, cu)
