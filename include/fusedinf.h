@@ -567,9 +567,11 @@ fi_status fi_tree_attention_workspace(const fi_tree_attention_args* args, uint64
 fi_status fi_tree_attention(const fi_tree_attention_args* args, void* hip_stream);
 
 /* y[m][n] = sum over groups g of scales[n][g] * sum over k in g of (w[n][k] - zeros[n][g]) * x[m][k]: a few rows times a
- * matrix of 4-bit weights, read once per 16 or 32 rows.  w holds two weights in [0, 15] per byte, the even one in the low half;
- * a group is `group` consecutive inputs.  The weights enter the products exactly, scales are applied to fp32 sums; a row
- * that holds an infinity, a NaN or values beyond 1e37 yields no finite numbers, the others are not touched by it.
+ * matrix of 4-bit weights, read once per 1 to 32 rows, by the sizes.  w holds two weights in [0, 15] per byte, the even one in the low half;
+ * a group is `group` consecutive inputs.  The weights enter the products exactly, scales are applied to fp32 sums; fp32 inputs may enter as
+ * three bf16 terms, exactly from about 1e-33 on, below that to 2^-133.  A result that is no finite number that way is computed
+ * again term by term, (q - zero) * scale * x in fp32: infinities, NaNs and inputs near the largest number give what the formula gives
+ * (a row with them takes longer), and the other rows are not touched by it.
  * With more than a few rows the inputs are shared out over workgroups, whose sums a second launch adds, always in the same
  * order; they are kept in `workspace` meanwhile, the caller's, of at least fi_q4_matmul_workspace bytes (0: may be NULL).
  * Calls that overlap in time need a workspace each. */

@@ -4,7 +4,7 @@
 // matrix cores, 16 rows x 16 outputs x 32 inputs an instruction.  A weight becomes bf16 in one operation and a share of a shift: 16 + q is the bit
 // pattern 0x4180 | q << 3, two of them at a time, exact; sums of (16 + q) x and of x (the same instruction with ones) are kept in fp32 over a group,
 // and (16 + zero) times the second comes off the first when the scale is applied.  fp32 rows are split into three bf16 terms
-// (24 bits), so that they enter exactly, too.
+// (24 bits), so that they enter exactly, too (down to 1e-33: what is left for the third is subnormal then).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -17,6 +17,29 @@ namespace fi {
 namespace {
 
 constexpr int ROWS = 8;   // rows that a wave of the row kernel has sums of
+
+// One result, term by term as the formula says: what a kernel stores in place of a sum that is no finite number.  Sums of (16 + q) x overflow earlier than those of
+// (q - zero) x, and an infinite x makes them NaN, where the formula may have an infinity or a number.  Rare, so it takes few registers and its time (us, without / with
+// a row of NaN: 24 x 25088 x 4096 inputs x outputs 28 / 810, 1 x 4096 x 4096 4 / 105; the test for it: 24 rows 0.2, 5 rows of 4096 x 1000 0.07).
+template <typename T>
+__device__ __forceinline__ float q4_term_by_term(const fi_q4_matmul_args& a, int64_t m, int64_t n) {
+  const uint8_t* w = a.w + n * a.w_stride;
+  const T* x = static_cast<const T*>(a.x) + m * a.x_stride;
+  float y = 0.0f;
+#pragma unroll 1
+  for (int g = 0; g < a.inputs / a.group; ++g) {
+    const float scale = a.scales[n * a.scales_stride + g], zero = a.zeros ? (float)a.zeros[n * a.zeros_stride + g] : 8.0f;
+#pragma unroll 1
+    for (int k = 0; k < a.group; k += 8, w += 4, x += 8)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) y += ((float)(w[t / 2] >> (t % 2 * 4) & 15) - zero) * scale * ld(x + t);
+  }
+  return y;
+}
+template <typename T>
+__device__ __forceinline__ float q4_result(const fi_q4_matmul_args& a, int64_t m, int64_t n, float y) {
+  return __builtin_isfinite(y) ? y : q4_term_by_term<T>(a, m, n);
+}
 
 // Any strides and alignment: one wave per output, a lane takes eight weights at a time.
 template <typename T>
@@ -31,13 +54,15 @@ __global__ void __launch_bounds__(256) q4_row_kernel(fi_q4_matmul_args a) {
       const float scale = a.scales[n * a.scales_stride + g], zero = a.zeros ? (float)a.zeros[n * a.zeros_stride + g] : 8.0f;
       float q[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) q[t] = ((float)((w[k / 2 + t / 2] >> (t % 2 * 4)) & 15) - zero) * scale;
+      for (int t = 0; t < 8; ++t) q[t] = (float)((w[k / 2 + t / 2] >> (t % 2 * 4)) & 15) - zero;
 #pragma unroll
       for (int m = 0; m < ROWS; ++m) {
         if (m0 + m >= a.rows) break;
         const T* const x = static_cast<const T*>(a.x) + (m0 + m) * a.x_stride + k;
+        float part = 0.0f;   // (eight inputs lie in one group)
 #pragma unroll
-        for (int t = 0; t < 8; ++t) sum[m] += q[t] * ld(x + t);
+        for (int t = 0; t < 8; ++t) part += q[t] * ld(x + t);
+        sum[m] += scale * part;
       }
     }
 #pragma unroll
@@ -45,7 +70,7 @@ __global__ void __launch_bounds__(256) q4_row_kernel(fi_q4_matmul_args a) {
       if (m0 + m >= a.rows) break;
       float v = sum[m];
       for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-      if (lane == 0) st(static_cast<T*>(a.out) + (m0 + m) * a.out_stride + n, v);
+      if (lane == 0) st(static_cast<T*>(a.out) + (m0 + m) * a.out_stride + n, q4_result<T>(a, m0 + m, n, v));
     }
   }
 }
@@ -216,7 +241,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) q4_tile_kernel(fi_q4_ma
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (row + e >= a.rows) continue;
-      st(static_cast<T*>(a.out) + (row + e) * a.out_stride + col, y[e]);
+      st(static_cast<T*>(a.out) + (row + e) * a.out_stride + col, q4_result<T>(a, row + e, col, y[e]));
     }
   }
 }
@@ -374,7 +399,7 @@ __global__ void __launch_bounds__(256) q4_few_kernel(fi_q4_matmul_args a, uint32
 #pragma unroll
   for (int v = 1; v < WK; ++v) y += parts[wave + v][lane];
   const int n = n0 + lane / M, m = m0 + lane % M;
-  if (n < a.outputs && m < a.rows) st(static_cast<T*>(a.out) + m * a.out_stride + n, y);
+  if (n < a.outputs && m < a.rows) st(static_cast<T*>(a.out) + m * a.out_stride + n, q4_result<T>(a, m, n, y));
 }
 
 // More rows: a workgroup computes 16 MB rows x 256 outputs over a share of the inputs, 128 at a time.  Everything comes into LDS by direct loads, AHEAD
@@ -601,7 +626,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) q4_wide_kernel(fi_q4_matmul_arg
         if (n0 + col > last) continue;
         const uint32_t to = row * stride + col;
         if (splits > 1) part[to] = acc[t][b][e];
-        else st(out + to, acc[t][b][e]);
+        else st(out + to, q4_result<T>(a, m0 + row, n0 + col, acc[t][b][e]));
       }
     }
 }
@@ -622,7 +647,7 @@ __global__ void __launch_bounds__(256) q4_join_kernel(fi_q4_matmul_args a, int s
     for (int u = 0; u < 8; ++u) y += part[u];
     at += 8 * size;
   }
-  st(static_cast<T*>(a.out) + (int64_t)row * a.out_stride + col, y);
+  st(static_cast<T*>(a.out) + (int64_t)row * a.out_stride + col, q4_result<T>(a, row, col, y));
 }
 
 // Which kernel takes a call, from its sizes and type alone (the workspace goes by it), where the addresses allow all of them.
