@@ -156,7 +156,8 @@ def main(argv=None):
                 at = t[at]
             alone = PagedCache(40, 16, a.kv_heads, a.head_dim, layer.dtype, layer.device)
             _, whole = run_prompts(layer, alone, [torch.cat([x, d[path[::-1]]])])
-            worst = max(worst, float((whole[0][-1].float() - y[node].float()).norm() / whole[0][-1].float().norm()))
+            off = float((whole[0][-1].float() - y[node].float()).norm() / whole[0][-1].float().norm())
+            worst = max(worst, off) if math.isfinite(off) else math.inf   # (max() drops a NaN)
     print(f"{sum(len(t) for t in trees)} nodes of {len(trees)} trees against prompts that end in them: relative difference {worst:.1e} at most")
 
     def timed(call, n=50):
