@@ -317,7 +317,11 @@ struct Tile {
         st.total += s[kb][e];
       }
   }
-  template <int KB>
+  // The matrix cores take the weights in bf16 where the values are.  FINE: in two terms, what the first leaves out by itself (16 bits, so that what is rounded to bf16 is the result
+  // alone); else rounded once (8 bits), their sum as it is.  Rounding halves the products, which counts where they bound the call: us in two terms / rounded, 8192 queries of 32 heads
+  // of 128 716 / 533, 12 trees of up to 37 nodes over up to 5001 keys 39.8 / 35.8; 4 single tokens over 131071 keys each, which HBM bounds, 391 / 389, one over 1003 10.6 / 10.5.
+  // So blocks of 32 rows over a cache (single tokens, small trees) take two terms, all others one.
+  template <int KB, bool FINE>
   static __device__ __forceinline__ void add_values(State& st, const f32x16 (&s)[KB], const uint8_t* tile, const Addr& at) {
     const uint8_t* const values = tile + KB * 32 * PB;
 #pragma unroll
@@ -340,26 +344,33 @@ struct Tile {
           u32x4 p;
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] = pack_bf16x2(s[kb][8 * h + 2 * i], s[kb][8 * h + 2 * i + 1]);
+          u32x4 rest;
+          if constexpr (FINE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rest[i] = pack_bf16x2(s[kb][8 * h + 2 * i] - __uint_as_float(p[i] << 16), s[kb][8 * h + 2 * i + 1] - __uint_as_float(p[i] & 0xFFFF0000u));
+          }
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
             const uint8_t* const from = values + at.v[db & 3] + (db >> 2) * 256 + (kb * 32 + 16 * h) * PB;
             const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)from));
             const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(from + 8 * PB)));
-            st.o[db] = product(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, st.o[db]);
+            const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+            st.o[db] = product(v, p, st.o[db]);
+            if constexpr (FINE) st.o[db] = product(v, rest, st.o[db]);
           }
         }
       }
     }
   }
   // All five.  masked: the same for the wave.
-  template <int KB, typename Visible>
+  template <int KB, bool FINE, typename Visible>
   static __device__ __forceinline__ void attend(State& st, const u32x4 (&q)[KS], const uint8_t* tile, const Addr& at, float c, bool masked, Visible visible) {
     f32x16 s[KB];
     scores<KB>(s, q, tile, at);
     if (masked) hide<KB>(s, visible);
     follow(st, highest<KB>(s), c);
     weigh<KB>(st, s, c);
-    add_values<KB>(st, s, tile, at);
+    add_values<KB, FINE>(st, s, tile, at);
   }
 
   // The lane's outputs, N blocks of values from block `from` on: o[b][4 g ..] are values 32 (from + b) + 8 g + 4 half .. of its query.
@@ -442,7 +453,7 @@ struct Joined {
   int from;
   float top, total;
 };
-template <typename TL, typename T, int WAVES, int BUFS, typename Find, typename Offsets, typename Visible, typename Strange>
+template <typename TL, typename T, int WAVES, int BUFS, bool FINE, typename Find, typename Offsets, typename Visible, typename Strange>
 __device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, const T* k, const T* v, const T* query, int D, float c, int first, int end, int sure, Find find,
                                          Offsets offsets, Visible visible, Strange add_strange) {
   constexpr int BYTES = 2 * 32 * TL::PB, DB = TL::DB;
@@ -477,7 +488,7 @@ __device__ __forceinline__ void own_walk(Joined<TL, WAVES>& r, uint8_t* smem, co
     if (BUFS > 1 && t + 1 < t1) load(t + 1);
     uint8_t* const tile = tiles + (t & (BUFS - 1)) * BYTES;
     if ((t + 1) * 32 > sure) strange |= __any(TL::template take_out<1>(tile, lane, 64)) != 0;
-    TL::template attend<1>(st, q, tile, at, c, (t + 1) * 32 > sure, [&](int) { return visible(t); });
+    TL::template attend<1, FINE>(st, q, tile, at, c, (t + 1) * 32 > sure, [&](int) { return visible(t); });
     if (BUFS == 1 && t + 1 < t1) {
       arrived();   // (the tile has been read)
       load(t + 1);
@@ -549,7 +560,7 @@ __global__ void __launch_bounds__((64 * Own<T, DB>::WAVES), 1) prompt_own_kernel
   const T* const v = static_cast<const T*>(a.v) + w.k0 * a.v_strides[0] + w.hk * a.v_strides[1];
   const uint32_t ks = (uint32_t)(a.k_strides[0] / TL::EP), vs = (uint32_t)(a.v_strides[0] / TL::EP);
   Joined<TL, Own<T, DB>::WAVES> r;
-  own_walk<TL, T, Own<T, DB>::WAVES, Own<T, DB>::BUFS>(
+  own_walk<TL, T, Own<T, DB>::WAVES, Own<T, DB>::BUFS, false>(
       r, smem, k, v, static_cast<const T*>(a.q) + (int64_t)(w.q0 + mine) * a.q_strides[0] + w.h * a.q_strides[1], D, a.scale * 1.44269504f, 0, (most + 32) / 32, least + 1,
       [&](int t) { return (uint32_t)(t * 32 + (lane & 31) < keys ? t * 32 + (lane & 31) : keys - 1); },
       [&](uint32_t key, uint32_t& ko, uint32_t& vo) {
@@ -620,7 +631,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 && sizeof(T
       meet_lds();
     }
     if (t * KEYS <= wave_most)
-      TL::template attend<KB>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
+      TL::template attend<KB, false>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
   }
   float total = both_halves(st.total);
   if constexpr (GROUPS == 2) {
@@ -718,7 +729,7 @@ __global__ void __launch_bounds__(512, 1) prompt_long_kernel(fi_prompt_attention
       meet_lds();
     }
     if (t * KEYS <= wave_most)
-      TL::template attend<KB>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
+      TL::template attend<KB, false>(st, q, tile, at, c, t * KEYS + KEYS - 1 > wave_least, [&](int kb) { return low_bits(last + 1 - t * KEYS - 32 * kb); });
   }
   if (tiles > 0 && *strange)   // (written before the last barrier)
     TL::add_strange(st, D, (least + 1) / KEYS * KEYS, wave_most + 1, [&](int key) { return v + (uint64_t)((uint32_t)key * vs) * TL::EP; }, [&](int key) { return key <= last; });
@@ -1044,7 +1055,7 @@ __device__ __forceinline__ void tree_tile_work(const fi_tree_attention_args& a, 
       meet_lds();
     }
     if (first + 32 * wave >= rows) continue;
-    TL::template attend<KB>(st, q, tile, at, c, (t + 1) * KEYS > w.cached, [&](int kb) { return tree_visible(a, w, node, words, t * KEYS + 32 * kb); });
+    TL::template attend<KB, false>(st, q, tile, at, c, (t + 1) * KEYS > w.cached, [&](int kb) { return tree_visible(a, w, node, words, t * KEYS + 32 * kb); });
   }
   arrived();   // (page requests past the end)
   if (t0 < t1 && *strange) tree_strange<TL, T>(a, w, st, v, pages, words, node, t0 * KEYS, t1 * KEYS, KEYS);
@@ -1080,7 +1091,7 @@ __device__ __forceinline__ void tree_own_work(const fi_tree_attention_args& a, c
   const uint64_t* const words = a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr;
   using O = Own<T, DB, SMALL>;
   Joined<TL, O::WAVES> r;
-  own_walk<TL, T, O::WAVES, O::BUFS>(
+  own_walk<TL, T, O::WAVES, O::BUFS, true>(
       r, smem, k, v, static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1], D, a.scale * 1.44269504f, w.t0, w.t1, w.cached,
       [&](int t) { return pages.find(t * 32 + (lane & 31) < w.keys ? t * 32 + (lane & 31) : w.keys - 1); },
       [&](const Pages::Place& place, uint32_t& ko, uint32_t& vo) { pages.offsets(place, ko, vo); }, [&](int t) { return tree_visible(a, w, node, words, t * 32); },

@@ -188,3 +188,18 @@ def test_shared_out_work_in_a_graph(torch, fi, dtype, nodes):  # noqa: F811
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
         assert outs[0][:sum(n)].isfinite().all() and outs[0][:sum(n)].abs().sum() > 0
+
+
+# ---- single tokens and small trees: nothing but the result is rounded to bf16 ------------------------------------
+@pytest.mark.parametrize("cached,counts,page,hq,hk,d", [
+    ([4000], [1], 16, 32, 8, 128), ([1003, 5, 64], [1, 1, 1], 64, 8, 8, 64), ([2000, 0, 700, 31], [4, 2, 1, 3], 16, 16, 2, 72), ([900], [7], 1, 8, 2, 256),
+    ([100 + i for i in range(40)], [1] * 40, 16, 32, 32, 96), ([3000, 100, 900] * 8, [1, 2, 3] * 8, 48, 16, 16, 128)])
+def test_few_nodes_keep_their_weights(torch, fi, cached, counts, page, hq, hk, d):  # noqa: F811
+    """Weights that meet the values in two terms of bf16 are off by (2^-8)^2; the bound has no rounding of 2^-8 but that of the result."""
+    g = torch.Generator().manual_seed(sum(cached) + d)
+    q, (k, v), table, dense, bits = _tree_case(torch, g, cached, counts, page, hq, hk, d, torch.bfloat16, "plain", "tree")
+    want, bound = _tree_ref(torch, q, dense, cached, counts, bits, d ** -0.5, "f32")
+    size, _ = _tree_ref(torch, q, [torch.stack([kv[0], kv[1].abs()]) for kv in dense], cached, counts, bits, d ** -0.5, "f32")
+    lengths, cu, longest = torch.tensor(cached, dtype=torch.int32).cuda(), _cu(torch, counts), max(c + n for c, n in zip(cached, counts))
+    got = fi.tree_attention(q, k, v, table, lengths, cu, bits.cuda(), max_nodes=max(counts), max_length=longest)
+    _inside(got.double().cpu(), want, bound + size * H * H + 1.01 * H * want.abs())
