@@ -300,6 +300,7 @@ PyObject* tree_attention(PyObject* const* arg) {
     const at::Tensor& mask = tensor(arg[6], "mask");
     const int64_t words = mask.dim() ? mask.size(-1) : 0;
     a.mask = c.plain<uint64_t>(mask, "mask", at::kLong, {nodes, words});
+    if (words < 1) refuse(PyExc_ValueError, "a mask of no words: None is the mask of chains");   // (its address is null, as None's)
     a.mask_words = int32(words, "mask words");
   }
   a.q = c.rows(q, "q", {nodes, heads, dim}, a.q_strides);

@@ -185,3 +185,12 @@ def test_no_gradients_and_outputs_that_count_as_changed(torch, fi):
             made = torch.zeros_like(args[outs[0]])
         call(**{**args, outs[0]: made})   # inference tensors have no counter
         assert torch.equal(made, want[0])
+
+
+def test_a_mask_without_words_is_refused(torch, fi):
+    """It has no address, as no mask at all has none, which stands for chains; no node would see another, or itself."""
+    q, cache = torch.ones((3, 2, 64), device="cuda"), torch.ones((1, 16, 2, 64), device="cuda")
+    table, cached, cu = torch.zeros((1, 1), dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32).cuda(), torch.tensor([0, 3], dtype=torch.int32).cuda()
+    with pytest.raises(ValueError, match="no words"):
+        fi.tree_attention(q, cache, cache, table, cached, cu, torch.zeros((3, 0), dtype=torch.int64).cuda())
+    assert torch.equal(fi.tree_attention(q, cache, cache, table, cached, cu, torch.zeros((3, 1), dtype=torch.int64).cuda()), torch.zeros_like(q))
