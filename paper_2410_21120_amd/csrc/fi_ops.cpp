@@ -134,13 +134,14 @@ fi_status fi_qk_norm_rope(const fi_qk_norm_rope_args* args, void* hip_stream) {
                     !apart({a.q_out_strides[0], a.q_out_strides[1]}, {a.tokens, a.q_heads}, D, "q_out"))) return FI_EINVAL;
   if ((a.q_weight && !good(a.q_weight, 4, "q_weight")) || (a.k_weight && !good(a.k_weight, 4, "k_weight"))) return FI_EINVAL;
   if (a.kv_heads) {
-    if (!good(a.k, es, "k") || !good(a.k_out, es, "k_out") || !good_strides(a.k_strides, 2, "k") || !good_strides(a.k_out_strides, 3, "k_out")) return FI_EINVAL;
-    if (!a.v != !a.v_out) { set_error("v and v_out come together"); return FI_EINVAL; }
-    if (a.v && (!good(a.v, es, "v") || !good(a.v_out, es, "v_out") || !good_strides(a.v_strides, 2, "v") || !good_strides(a.v_out_strides, 3, "v_out"))) return FI_EINVAL;
     if (a.slots && (!good(a.slots, 8, "slots") || a.page_size < 1 || a.n_slots < 0)) {
       if (a.page_size < 1 || a.n_slots < 0) set_error("pages of %d tokens, %lld slots", a.page_size, (long long)a.n_slots);
       return FI_EINVAL;
     }
+    const bool kept = !a.slots || a.n_slots > 0;   // a cache without pages has no address, and takes nothing
+    if (!good(a.k, es, "k") || (kept && !good(a.k_out, es, "k_out")) || !good_strides(a.k_strides, 2, "k") || !good_strides(a.k_out_strides, 3, "k_out")) return FI_EINVAL;
+    if (kept && !a.v != !a.v_out) { set_error("v and v_out come together"); return FI_EINVAL; }
+    if (a.v && (!good(a.v, es, "v") || (kept && !good(a.v_out, es, "v_out")) || !good_strides(a.v_strides, 2, "v") || !good_strides(a.v_out_strides, 3, "v_out"))) return FI_EINVAL;
     const int64_t pages = a.slots ? a.n_slots / a.page_size + (a.n_slots % a.page_size != 0) : 1, rows = a.slots ? a.page_size : a.tokens;
     for (int t = 0; t < (a.v ? 2 : 1); ++t) {
       const int64_t* s = t ? a.v_out_strides : a.k_out_strides;

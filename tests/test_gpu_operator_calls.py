@@ -194,3 +194,13 @@ def test_a_mask_without_words_is_refused(torch, fi):
     with pytest.raises(ValueError, match="no words"):
         fi.tree_attention(q, cache, cache, table, cached, cu, torch.zeros((3, 0), dtype=torch.int64).cuda())
     assert torch.equal(fi.tree_attention(q, cache, cache, table, cached, cu, torch.zeros((3, 1), dtype=torch.int64).cuda()), torch.zeros_like(q))
+
+
+def test_a_cache_without_pages_takes_nothing(torch, fi):
+    """Every slot is outside then: the queries are written, and nothing else."""
+    x = torch.randn((5, 8, 64), generator=torch.Generator().manual_seed(26)).cuda()
+    positions, freq, none = torch.arange(5, dtype=torch.int32).cuda(), torch.ones(32).cuda(), torch.zeros((0, 16, 2, 64)).cuda()
+    want, _, _ = fi.qk_norm_rope(x[:, :4], x[:, 4:6], x[:, 6:], positions, freq)
+    for v in (x[:, 6:], None):
+        q, k_out, v_out = fi.qk_norm_rope(x[:, :4], x[:, 4:6], v, positions, freq, slots=torch.tensor([0, 1, -1, 5, 16]).cuda(), k_out=none, v_out=none.clone())
+        assert torch.equal(q, want) and k_out.shape == none.shape
