@@ -471,7 +471,7 @@ void fi_destroy(fi_dag* dag);
  *    nothing, synchronises nothing and may be recorded into a HIP graph.  The argument struct is read during the call only.
  *  - dtype is FI_BF16 or FI_F32 and holds for every tensor of data; sums, softmax statistics and norms are fp32, and a
  *    result is rounded once, when it is stored.  Attention on bf16 also rounds the softmax weights that it multiplies the values
- *    with (to 8 bits; single tokens and trees of up to 32 rows, nodes times query heads of a key head, to 16 and more).
+ *    with (to 8 bits; to 16 and more over a cache where max_nodes times the query heads of a key head is 32 at most).
  *  - All tensor pointers are device pointers.  Strides are in elements of the tensor's type; the last dimension (head_dim,
  *    inputs, outputs) is contiguous.  Inputs may have any strides >= 0; rows that start on 16-byte boundaries take the fast kernels.
  *    Outputs must not overlap themselves (every dimension, from the shortest stride on, strides over all that the ones before it

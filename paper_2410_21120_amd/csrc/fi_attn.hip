@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES * GROUPS, DB > 4 && sizeof(T
 
 // Long prompts in bf16: 256 queries a workgroup, eight waves, four tiles in LDS of which three are on their way; the lanes' offsets of a whole tile stay in registers.
 // 8192 queries of 32 heads of 128, causal: 529 to 548 us (1.0 PFLOP/s of the seen half, three quarters of what a large library product reaches; with four waves and two
-// tiles 565).  What bounds it: the matrix unit is busy 46 % of the time and the vector unit, with the exponentials, 44 %, and they hardly overlap.
+// tiles 565).  What bounds it: the matrix unit is busy 47 % of the time and the vector unit, with the exponentials, 45 %, and they hardly overlap.
 // Tried: the next block's scores among this one's exponentials in a wave 608; the two waves of a unit half a tile apart by barriers 594; wave priorities 543 to 552.
 constexpr int LONG_ROWS = 256, LONG_GROUPS = 512;
 template <int DB, int DQ>
