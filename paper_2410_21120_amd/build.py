@@ -22,7 +22,7 @@ def stale() -> bool:
     if not os.path.exists(OUT) or not os.path.exists(TENSORS):
         return True
     t = min(os.path.getmtime(OUT), os.path.getmtime(TENSORS))
-    headers = [os.path.join(CSRC, h) for h in ("fi_internal.h", "fi_device.h", "fi_ops.h", "fi_ops_device.h", "fi_tensors.cpp")]
+    headers = [os.path.join(CSRC, h) for h in ("fi_internal.h", "fi_device.h", "fi_ops.h", "fi_ops_device.h", "fi_tree_device.h", "fi_tensors.cpp")]
     deps = sources() + headers + [os.path.join(HERE, "..", "include", "fusedinf.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
