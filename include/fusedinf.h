@@ -594,6 +594,141 @@ typedef struct {
 fi_status fi_q4_matmul_workspace(const fi_q4_matmul_args* args, uint64_t* bytes);
 fi_status fi_q4_matmul(const fi_q4_matmul_args* args, void* hip_stream);
 
+/* ---- beams over a cache held in 4 bits ----
+ * What a decoder member needs when several continuations of a request live at a time: a paged cache that takes a quarter of the memory, attention
+ * over it, the selection of the continuations, and the bookkeeping of pages that they share.  All of it stays on the device, so that a whole step is one
+ * graph: fi_beam_select's parents are fi_fork_pages' parents, whose slots are fi_fp4_cache_write's slots.
+ * What is common to the decoder operators above holds for these too.
+ *
+ * The 4-bit cache: a head's values in blocks of FI_FP4_BLOCK, the last one maybe shorter.  A value is a code times the block's power of two.  Codes are
+ * E2M1: 0 to 7 are 0, 0.5, 1, 1.5, 2, 3, 4, 6, plus 8 negative; two to a byte, the even value in the low half.  A block's scale is one byte b: 2^(b - 127), b in
+ * [0, 252], or 255: every value of the block is NaN.  (253 and 254 count as 255 where a query does not see the key, and may give infinities where it does.)
+ * codes are [n_pages, page_size, kv_heads, head_dim / 2] and scales [n_pages, page_size, kv_heads, blocks], with strides in bytes: the tokens of a head in
+ * a page should lie together in memory (strides of a page kv_heads * page_size rows, of a head page_size rows, of a token one row).  Strides and starts of codes are
+ * multiples of 4 bytes. */
+#define FI_FP4_BLOCK 32
+
+/* A step's keys and values into the cache.  A block's scale is the smallest power of two from 2^-125 to 2^125 whose six-fold no value of the block exceeds (what
+ * exceeds 6 * 2^125 is cut to that), its codes are the nearest ones, on a border the even code; a block with a NaN or an infinity gets scale 255 and codes 0. */
+typedef struct {
+  int32_t dtype;                 /* of k, v, k_held and v_held */
+  int32_t tokens, kv_heads, head_dim; /* head_dim: a multiple of 8, at most FI_MAX_HEAD_DIM */
+  int32_t page_size;
+  int32_t reserved;
+  int64_t n_slots;               /* pages x page_size; a token whose slot lies outside [0, n_slots) leaves the cache as it is */
+  const void *k, *v;             /* [tokens, kv_heads, head_dim]; v may be NULL (then v_codes, v_scales and v_held are, too) */
+  const int64_t* slots;          /* [tokens]: page * page_size + place in the page; no two tokens share a slot */
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  void *k_held, *v_held;         /* NULL, or [tokens, kv_heads, head_dim]: what the cache holds for the tokens, for attention over a prompt that is to
+                                  * agree with later steps; written for tokens without a slot, too */
+  int64_t k_strides[2], v_strides[2], k_held_strides[2], v_held_strides[2];                     /* token, head; elements */
+  int64_t k_codes_strides[3], k_scales_strides[3], v_codes_strides[3], v_scales_strides[3];     /* page, token, head; bytes */
+} fi_fp4_cache_write_args;
+fi_status fi_fp4_cache_write(const fi_fp4_cache_write_args* args, void* hip_stream);
+
+/* fi_tree_attention over such a cache; the values of the cache enter the products exactly. */
+typedef struct {
+  int32_t dtype;                 /* of q and out */
+  int32_t n_seqs, q_heads, kv_heads, head_dim;
+  int32_t page_size, n_pages, table_columns, mask_words, max_nodes, max_length;
+  float scale;
+  int64_t nodes;
+  const void* q;                 /* [nodes, q_heads, head_dim] */
+  const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  const int32_t* block_table;    /* from here on as in fi_tree_attention_args */
+  const int32_t* cached;
+  const int32_t* cu_nodes;
+  const uint64_t* mask;
+  void* out;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t q_strides[2], out_strides[2]; /* token, head; elements */
+  int64_t k_codes_strides[3], k_scales_strides[3], v_codes_strides[3], v_scales_strides[3]; /* page, token, head; bytes */
+  int64_t table_stride;
+} fi_fp4_tree_attention_args;
+fi_status fi_fp4_tree_attention_workspace(const fi_fp4_tree_attention_args* args, uint64_t* bytes);
+fi_status fi_fp4_tree_attention(const fi_fp4_tree_attention_args* args, void* hip_stream);
+
+/* The `keep` best continuations of every sequence over its beams and the vocabulary.  Row s * beams + b of logits is beam b of sequence s, whose score is
+ * scores[s][b]; a continuation with token t scores scores[s][b] + logits[row][t] - log(sum over u of exp(logits[row][u])), and one that is NaN or minus infinity is none (so a
+ * beam with score minus infinity has none, and a row with a NaN or an infinity of logits neither).  Best first; equal scores by beam, then by logit, then by token: the
+ * lowest first.  Where there are fewer than `keep`, the rest is token -1, parent -1, score minus infinity.
+ * end >= 0: the token that ends a sequence.  A beam with ended[s][b] != 0 has one continuation, itself: token `end`, its score unchanged; its logits are not looked at. ended_out
+ * tells for each continuation whether it has ended. */
+#define FI_MAX_BEAMS 64
+typedef struct {
+  int32_t dtype;                 /* of logits */
+  int32_t n_seqs, beams, keep, vocab; /* beams and keep in [1, FI_MAX_BEAMS]; beams * vocab below 2^31 - 1024 */
+  int32_t end;                   /* below vocab; negative: none */
+  int64_t logits_stride;         /* elements between rows */
+  const void* logits;            /* [n_seqs * beams, vocab] */
+  const float* scores;           /* [n_seqs, beams] */
+  const uint8_t* ended;          /* [n_seqs, beams] or NULL (none has); only with end >= 0 */
+  int32_t* tokens_out;           /* [n_seqs, keep] */
+  int32_t* parents_out;          /* [n_seqs, keep]: rows of logits */
+  float* scores_out;             /* [n_seqs, keep] */
+  uint8_t* ended_out;            /* [n_seqs, keep], 0 / 1; NULL without end */
+  void* workspace;               /* 16-byte aligned */
+  uint64_t workspace_bytes;
+} fi_beam_select_args;
+fi_status fi_beam_select_workspace(const fi_beam_select_args* args, uint64_t* bytes);
+fi_status fi_beam_select(const fi_beam_select_args* args, void* hip_stream);
+
+/* One cache whose pages are copied: page p is the page_bytes bytes from base + p * page_stride (bytes) on. */
+typedef struct {
+  void* base;
+  int64_t page_stride, page_bytes;
+} fi_page_cache;
+
+/* The rows of a block table after a selection.  Row r of block_table holds ceil(held[r] / page_size) pages for its lengths[r] committed tokens and those that room was
+ * made for; refs[p] counts how often page p is held (by these rows or anyone else), 0: it is free.
+ *  1. All rows let go of what they hold.  New row i continues row parents[i]: it shares the pages of that row's committed tokens.  A parent
+ *     outside [0, rows) is none: the new row is empty, length 0, and holds nothing.
+ *  2. With room > 0 every continuing row gets pages for `room` tokens behind the committed ones, in the order of the rows, the lowest free page first.  Its last page, if
+ *     it is partly filled and still held by another (counting rows after this one, rows before it that copied no more), is replaced by a copy, whose
+ *     page is the first that the row gets.  A row whose tokens do not fit the table's columns, or for which, counting what all rows before it need, pages are
+ *     lacking, gets nothing and copies nothing.
+ * Written are the new rows (-1 behind the pages that a row holds), lengths, held (lengths + room for the rows that got it, else lengths), refs, and the slots of the
+ * `room` tokens, page * page_size + place (-1 where there is no room: what writes to a cache leaves such tokens out).  A copy is of the whole page, in every one of
+ * `caches`; nothing else in them changes.  Entries that are no pages are kept, count nowhere and are no slots. */
+typedef struct {
+  int32_t rows, new_rows;        /* of block_table, of what comes out; at most 2^16 each */
+  int32_t columns, page_size, n_pages, room; /* page_size * columns and n_pages below 2^31 - 1024, room at most 2^16 */
+  int32_t n_caches;              /* at most FI_MAX_PAGE_CACHES */
+  int32_t reserved;
+  int64_t table_stride, table_out_stride;
+  const int32_t* block_table;    /* [rows, columns] */
+  const int32_t* lengths;        /* [rows] */
+  const int32_t* held;           /* [rows] or NULL (lengths) */
+  const int32_t* refs;           /* [n_pages] */
+  const int32_t* parents;        /* [new_rows], or NULL: row i continues row i */
+  const fi_page_cache* caches;   /* [n_caches], host memory, read during the call only */
+  int32_t *table_out, *lengths_out, *held_out, *refs_out; /* [new_rows, columns], [new_rows], [new_rows], [n_pages]; none of them may be an input */
+  int64_t* slots_out;            /* [new_rows, room]; NULL with room 0 */
+  void* workspace;               /* 16-byte aligned */
+  uint64_t workspace_bytes;
+} fi_fork_pages_args;
+#define FI_MAX_PAGE_CACHES 128
+fi_status fi_fork_pages_workspace(const fi_fork_pages_args* args, uint64_t* bytes);
+fi_status fi_fork_pages(const fi_fork_pages_args* args, void* hip_stream);
+
+/* Moves the pages in use (refs > 0), `live` of them, to the page numbers below `live`: those there stay, the ones above move into the free ones below,
+ * in ascending order both.  A page is copied in every one of `caches`; what it leaves is not cleared.  Entries of block_table that are pages in use are renumbered, others are kept. */
+typedef struct {
+  int32_t rows, columns, n_pages, n_caches; /* rows at most 2^16, n_pages below 2^31 - 1024 */
+  int64_t table_stride, table_out_stride;
+  const int32_t* block_table;    /* [rows, columns] */
+  const int32_t* refs;           /* [n_pages] */
+  const fi_page_cache* caches;   /* [n_caches], host memory, read during the call only */
+  int32_t *table_out, *refs_out; /* none of them may be an input */
+  int32_t* moved_out;            /* [n_pages]: the new number of every page, -1 for a free one */
+  int32_t* live_out;             /* [1] */
+  void* workspace;               /* 16-byte aligned */
+  uint64_t workspace_bytes;
+} fi_compact_pages_args;
+fi_status fi_compact_pages_workspace(const fi_compact_pages_args* args, uint64_t* bytes);
+fi_status fi_compact_pages(const fi_compact_pages_args* args, void* hip_stream);
+
 const char* fi_last_error(void); /* thread-local, valid until the next call on this thread */
 const char* fi_version(void);
 

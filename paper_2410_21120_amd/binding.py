@@ -116,6 +116,8 @@ LIB_PATH = _build.OUT
 EXPORTS = ["fi_model_packed_size", "fi_model_pack", "fi_build_dag", "fi_footprint", "fi_partition", "fi_round_robin", "fi_query", "fi_node", "fi_launch", "fi_launch_at", "fi_member", "fi_load",
            "fi_run", "fi_run_static", "fi_run_inputs", "fi_run_batches", "fi_run_lane", "fi_profile", "fi_timeline", "fi_swap_model", "fi_server_start", "fi_server_submit", "fi_server_wait", "fi_server_query", "fi_server_swap", "fi_server_stop",
            "fi_qk_norm_rope", "fi_prompt_attention", "fi_tree_attention_workspace", "fi_tree_attention", "fi_q4_matmul_workspace", "fi_q4_matmul",
+           "fi_fp4_cache_write", "fi_fp4_tree_attention_workspace", "fi_fp4_tree_attention", "fi_beam_select_workspace", "fi_beam_select", "fi_fork_pages_workspace",
+           "fi_fork_pages", "fi_compact_pages_workspace", "fi_compact_pages",
            "fi_unload", "fi_destroy", "fi_last_error", "fi_version"]
 _lib = None
 
@@ -159,9 +161,11 @@ def lib():
         L.fi_server_query.argtypes = [vp, C.POINTER(fi_server_stats)]
         L.fi_server_stop.argtypes = [vp]
         L.fi_server_swap.argtypes = [vp, i32, C.POINTER(fi_model_spec)]
-        for name in ("fi_qk_norm_rope", "fi_prompt_attention", "fi_tree_attention", "fi_q4_matmul"):   # structs: operators.py
+        for name in ("fi_qk_norm_rope", "fi_prompt_attention", "fi_tree_attention", "fi_q4_matmul", "fi_fp4_cache_write", "fi_fp4_tree_attention", "fi_beam_select",
+                     "fi_fork_pages", "fi_compact_pages"):   # structs: operators.py
             getattr(L, name).argtypes = [vp, vp]
-        for name in ("fi_tree_attention_workspace", "fi_q4_matmul_workspace"):
+        for name in ("fi_tree_attention_workspace", "fi_q4_matmul_workspace", "fi_fp4_tree_attention_workspace", "fi_beam_select_workspace", "fi_fork_pages_workspace",
+                     "fi_compact_pages_workspace"):
             getattr(L, name).argtypes = [vp, C.POINTER(u64)]
         L.fi_unload.argtypes = [vp]
         L.fi_destroy.argtypes = [vp]
