@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libfusedinf.so")
 TENSORS = os.path.join(HERE, "_tensors.so")   # the decoder operators on PyTorch tensors (argument marshalling; host code)
-SOURCES = ["fi_plan.cpp", "fi_api.cpp", "fi_sched.cpp", "fi_server.cpp", "fi_kernels.hip", "fi_chain.hip", "fi_stem.hip", "fi_kwave.hip", "fi_patch.hip", "fi_stream.hip", "fi_pool.hip", "fi_ops.cpp", "fi_rope.hip", "fi_attn.hip", "fi_q4.hip", "fi_fp4.hip", "fi_beam.hip", "fi_pages.hip"]
+SOURCES = ["fi_plan.cpp", "fi_api.cpp", "fi_sched.cpp", "fi_server.cpp", "fi_kernels.hip", "fi_chain.hip", "fi_stem.hip", "fi_kwave.hip", "fi_patch.hip", "fi_stream.hip", "fi_pool.hip", "fi_ops.cpp", "fi_rope.hip", "fi_attn.hip", "fi_q4.hip", "fi_fp4.hip", "fi_fp4_f32.hip", "fi_beam.hip", "fi_pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -22,7 +22,7 @@ def stale() -> bool:
     if not os.path.exists(OUT) or not os.path.exists(TENSORS):
         return True
     t = min(os.path.getmtime(OUT), os.path.getmtime(TENSORS))
-    headers = [os.path.join(CSRC, h) for h in ("fi_internal.h", "fi_device.h", "fi_ops.h", "fi_ops_device.h", "fi_tree_device.h", "fi_tensors.cpp")]
+    headers = [os.path.join(CSRC, h) for h in ("fi_internal.h", "fi_device.h", "fi_ops.h", "fi_ops_device.h", "fi_tree_device.h", "fi_fp4_device.h", "fi_tensors.cpp")]
     deps = sources() + headers + [os.path.join(HERE, "..", "include", "fusedinf.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
