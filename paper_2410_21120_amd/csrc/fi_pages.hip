@@ -12,8 +12,9 @@ namespace fi {
 namespace {
 
 constexpr int THREADS = 1024, PIECE = 16384;
-constexpr int SMALL_ROWS = 1024;           // rows, old and new, that one workgroup takes with its lists in LDS
-constexpr int64_t SMALL_TABLE = 1 << 16;   // and entries of their tables
+// What one workgroup takes with all counts in LDS: rows, old and new, pages, entries of the old table.
+constexpr int SMALL_ROWS = 1024, SMALL_PAGES = 24576;
+constexpr int64_t SMALL_TABLE = 1 << 17;
 
 // The caches of a call (kernel arguments are 4 KB at most, so a launch takes MOST of them).  start: where a cache's pieces of a page begin, last: of all.
 struct Copies {
@@ -23,8 +24,6 @@ struct Copies {
   uint8_t* base[MOST];
   int64_t stride[MOST], bytes[MOST];
 };
-
-__device__ __forceinline__ int agent_load(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }   // (counts change by atomics)
 
 // Sum over the threads before this one; total: over all.
 __device__ __forceinline__ int before(int x, int* lds, int& total) {
@@ -99,7 +98,10 @@ struct ForkRow {
   int parent, length, before, after;   // pages of the committed tokens, pages with the room
   bool fits;
 };
-__device__ __forceinline__ int pages_of(int tokens, int page) { return (int)(((int64_t)tokens + page - 1) / page); }
+__device__ __forceinline__ int pages_of(uint32_t tokens, int page) {   // (below 2^32)
+  const uint32_t q = tokens / (uint32_t)page;
+  return (int)(q + (q * (uint32_t)page != tokens));
+}
 __device__ __forceinline__ int held_pages(const fi_fork_pages_args& a, const int32_t* tokens, int row) {
   const int n = tokens[row], most = a.columns * a.page_size;
   return pages_of(n < 0 ? 0 : n > most ? most : n, a.page_size);
@@ -111,17 +113,19 @@ __device__ __forceinline__ ForkRow fork_row(const fi_fork_pages_args& a, int i) 
   const int most = a.columns * a.page_size, n = r.parent < 0 ? 0 : a.lengths[r.parent];
   r.length = n < 0 ? 0 : n > most ? most : n;
   r.before = pages_of(r.length, a.page_size);
-  const int64_t after = ((int64_t)r.length + a.room + a.page_size - 1) / a.page_size;
+  const int after = pages_of((uint32_t)r.length + (uint32_t)a.room, a.page_size);
   r.fits = r.parent >= 0 && after <= a.columns;
-  r.after = r.fits ? (int)after : r.before;
+  r.after = r.fits ? after : r.before;
   return r;
 }
 __device__ __forceinline__ bool is_page(const fi_fork_pages_args& a, int p) { return p >= 0 && p < a.n_pages; }
 
 // The page that a new row would write next to tokens that it has, or -1.
 __device__ __forceinline__ int fork_last(const fi_fork_pages_args& a, const ForkRow& r) {
-  if (!r.fits || a.room == 0 || r.length % a.page_size == 0) return -1;
-  const int p = a.block_table[r.parent * a.table_stride + r.length / a.page_size];
+  if (!r.fits || a.room == 0) return -1;
+  const uint32_t at = (uint32_t)r.length / (uint32_t)a.page_size;
+  if (at * (uint32_t)a.page_size == (uint32_t)r.length) return -1;
+  const int p = a.block_table[r.parent * a.table_stride + at];
   return is_page(a, p) ? p : -1;
 }
 // An old row's entry: children share it where it holds committed tokens; the row itself lets go.
@@ -156,7 +160,7 @@ __device__ __forceinline__ void fork_deal(const fi_fork_pages_args& a, const For
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int p = p0 + threadIdx.x * 4 + u;
-      free[u] = p < a.n_pages && agent_load(a.refs_out + p) == 0;
+      free[u] = p < a.n_pages && a.refs_out[p] == 0;
       n += free[u];
     }
     int all;
@@ -182,84 +186,135 @@ __device__ __forceinline__ void fork_deal(const fi_fork_pages_args& a, const For
   if (made) atomicAdd(w.head + 1, made);
 }
 
-// A new row's entries, by `lanes` threads.
-__device__ __forceinline__ void fork_write(const fi_fork_pages_args& a, const ForkSpace& w, int i, int lane, int lanes) {
+// What a new row gets is held (count(page, change)); its copy is noted.
+template <typename Count>
+__device__ __forceinline__ void fork_take(const ForkSpace& w, int need, int first, int copy, int last, const int* given, Count count) {
+  for (int n = 0; n < need; ++n) count(given[first + n], 1);
+  if (copy < 0) return;
+  w.source[copy] = last;
+  w.target[copy] = given[first];
+}
+// A new row's entries, by a wave.
+__device__ __forceinline__ void fork_write(const fi_fork_pages_args& a, const ForkSpace& w, int i) {
+  const int lane = threadIdx.x & 63;
+  const int need = w.need[i], first = w.first[i], there = w.head[0], asked = w.copy[i];
   const ForkRow r = fork_row(a, i);
-  const int need = w.need[i], first = w.first[i], there = agent_load(w.head);
-  const bool made = r.fits && (need == 0 || first + need <= there);
-  const bool copy = made && w.copy[i] >= 0;
+  const bool made = r.fits && (need == 0 || first + need <= there), copy = made && asked >= 0;
   const int at = r.length / a.page_size;
   auto entry = [&](int j) {
     if (copy && j == at) return w.given[first];
     if (j < r.before) return a.block_table[r.parent * a.table_stride + j];
     return made && j < r.after ? w.given[first + (copy ? 1 : 0) + j - r.before] : -1;
   };
-  for (int j = lane; j < a.columns; j += lanes) a.table_out[i * a.table_out_stride + j] = entry(j);
-  for (int t = lane; t < a.room; t += lanes) {
+  for (int j = lane; j < a.columns; j += 64) a.table_out[i * a.table_out_stride + j] = entry(j);
+  for (int t = lane; t < a.room; t += 64) {
     const int place = r.length + t, p = made ? entry(place / a.page_size) : -1;
     a.slots_out[(int64_t)i * a.room + t] = is_page(a, p) ? (int64_t)p * a.page_size + place % a.page_size : -1;
   }
-  if (made)
-    for (int n = lane; n < need; n += lanes) atomicAdd(a.refs_out + w.given[first + n], 1);
   if (lane == 0) {
     a.lengths_out[i] = r.length;
     a.held_out[i] = made ? r.length + a.room : r.length;
-    if (copy) {
-      atomicAdd(a.refs_out + w.last[i], -1);
-      w.source[w.copy[i]] = w.last[i];
-      w.target[w.copy[i]] = w.given[first];
-    }
   }
 }
 
-// Few rows: all of it by one workgroup.
+// Few rows: all that is counted by one workgroup, in LDS.  512 rows of up to 63 pages: 16.5 us; with the counts in memory (atomics, and loads past the
+// caches) 122, 4 rows 22 -> 6.  The rest is latency: 2 us until the rows are known, 8.5 for the old table, a few for running sums and what is written.
 __global__ void __launch_bounds__(THREADS) fork_small_kernel(fi_fork_pages_args a) {
-  __shared__ int children[SMALL_ROWS], committed[SMALL_ROWS], held[SMALL_ROWS], sums[THREADS / 64];
-  __shared__ __attribute__((aligned(16))) int last[SMALL_ROWS];
+  __shared__ int refs[SMALL_PAGES], children[SMALL_ROWS], committed[SMALL_ROWS], held[SMALL_ROWS], sums[THREADS / 64];
   const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
-  for (int p = threadIdx.x; p < a.n_pages; p += THREADS) a.refs_out[p] = a.refs[p];
-  for (int r = threadIdx.x; r < a.rows; r += THREADS) {
-    children[r] = 0;
-    committed[r] = held_pages(a, a.lengths, r);
-    held[r] = a.held ? held_pages(a, a.held, r) : committed[r];
-  }
-  for (int i = threadIdx.x; i < SMALL_ROWS; i += THREADS) last[i] = -1;
-  __threadfence();
-  __syncthreads();
+  const int me = threadIdx.x, lane = me & 63, wave = __builtin_amdgcn_readfirstlane(me >> 6);
   ForkRow row{-1, 0, 0, 0, false};
-  if ((int)threadIdx.x < a.new_rows) {
-    row = fork_row(a, threadIdx.x);
-    if (row.parent >= 0) atomicAdd(&children[row.parent], 1);
-    last[threadIdx.x] = fork_last(a, row);
+  if (me < a.new_rows) row = fork_row(a, me);
+  const int mine = me < a.new_rows ? fork_last(a, row) : -1;
+  children[me] = 0;
+  if (me < a.rows) {
+    committed[me] = held_pages(a, a.lengths, me);
+    held[me] = a.held ? held_pages(a, a.held, me) : committed[me];
   }
+  for (int p = me; p < a.n_pages; p += THREADS) refs[p] = a.refs[p];
   __syncthreads();
-  for (int i = threadIdx.x; i < a.rows * a.columns; i += THREADS) {
-    const int r = i / a.columns;
-    fork_count(a, r, i - r * a.columns, children[r], committed[r], held[r]);
-  }
-  __threadfence();
+  if (row.parent >= 0) atomicAdd(&children[row.parent], 1);
   __syncthreads();
-  if ((int)threadIdx.x < a.new_rows) {
-    const int mine = last[threadIdx.x];
-    bool copy = false;
-    if (mine >= 0) {
-      int sharers = 0;   // rows before this one that write the same page
-      for (int j = 0; j < (int)threadIdx.x; j += 4) {
-        const int4 o = *reinterpret_cast<const int4*>(last + j);
-        sharers += (o.x == mine) + (o.y == mine && j + 1 < (int)threadIdx.x) + (o.z == mine && j + 2 < (int)threadIdx.x) + (o.w == mine && j + 3 < (int)threadIdx.x);
+  // Entries that change: children share them where they are committed, the row itself lets go.  Lane l of wave x has row 16 l + x; rows and pieces of 64 of their entries
+  // are gone through by scalar registers (with vector ones, 512 rows of 64 entries take 12 us, so 8.5, which is what one unit has of lines on their way: 2, 8 or 32 loads
+  // at a time do not change it).
+  {
+    constexpr int WAVES = THREADS / 64, AT_ONCE = 4;
+    const int r = lane * WAVES + wave, c = r < a.rows ? children[r] : 0, kept = r < a.rows ? committed[r] : 0, all = r < a.rows ? held[r] : 0;
+    uint64_t left = __ballot(c == 1 ? kept != all : kept > 0 || all > 0);
+    int j0 = 0;
+    while (left) {
+      int p[AT_ONCE], change[AT_ONCE];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        p[u] = -1;
+        change[u] = 0;
+        if (!left) continue;
+        const int l = __ffsll((long long)left) - 1, times = __builtin_amdgcn_readlane(c, l), some = __builtin_amdgcn_readlane(kept, l), most = __builtin_amdgcn_readlane(all, l);
+        const int j = j0 + lane;
+        change[u] = (j < some ? times : 0) - (j < most ? 1 : 0);
+        if (change[u]) p[u] = a.block_table[(int64_t)(l * WAVES + wave) * a.table_stride + j];
+        j0 += 64;
+        if (j0 >= some && j0 >= most) {
+          j0 = 0;
+          left &= left - 1;
+        }
       }
-      copy = agent_load(a.refs_out + mine) - sharers > 1;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u)
+        if (is_page(a, p[u])) atomicAdd(&refs[p[u]], change[u]);
     }
-    w.last[threadIdx.x] = mine;
-    w.copy[threadIdx.x] = copy;
-    w.need[threadIdx.x] = row.fits ? (copy ? 1 : 0) + row.after - row.before : 0;
   }
-  __threadfence();
+  // Rows of a wave that write one page, those before this one; then the waves in order take their copies off the counts.
+  int sharers = 0;
+  for (uint64_t left = __ballot(mine >= 0); left;) {
+    const int page = __builtin_amdgcn_readlane(mine, __ffsll((long long)left) - 1);
+    const uint64_t same = __ballot(mine == page);
+    if (mine == page) sharers = __popcll(same & ((1ull << lane) - 1));
+    left &= ~same;
+  }
+  bool copy = false;
+  for (int x = 0; x < (a.new_rows + 63) / 64; ++x) {
+    __syncthreads();
+    if (x == wave && mine >= 0) {
+      copy = refs[mine] - sharers > 1;
+      if (copy) atomicAdd(&refs[mine], -1);   // (after all lanes have read: a wave's accesses to LDS keep their order)
+    }
+  }
+  const int need = row.fits ? (copy ? 1 : 0) + row.after - row.before : 0;
+  int wanted, copies;
+  const int first = before(need, sums, wanted), at = before(copy ? 1 : 0, sums, copies);   // (at most 1024 rows of 2^16 + 1)
+  int found = 0;
+  for (int p0 = 0; p0 < a.n_pages && found < wanted; p0 += THREADS * 4) {
+    const int p = p0 + me * 4;
+    int free = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) free |= (p + u < a.n_pages && refs[p + u] == 0) << u;
+    int all, to = found + before(__popc(free), sums, all);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (free >> u & 1) {
+        if (to < wanted) w.given[to] = p + u;
+        ++to;
+      }
+    found += all;
+  }
+  const int there = found < wanted ? found : wanted;
+  const bool made = row.fits && first + need <= there;
+  before(copy && made ? 1 : 0, sums, copies);   // (and what is given has been written)
+  if (me < a.new_rows) {
+    w.need[me] = need;
+    w.first[me] = first;
+    w.copy[me] = copy ? at : -1;
+    if (made) fork_take(w, need, first, copy ? at : -1, mine, w.given, [&](int p, int change) { atomicAdd(&refs[p], change); });
+    else if (copy) atomicAdd(&refs[mine], 1);
+  }
+  if (me == 0) {
+    w.head[0] = there;
+    w.head[1] = copies;
+  }
   __syncthreads();
-  fork_deal(a, w, sums);
-  __threadfence();
-  __syncthreads();
-  for (int i = threadIdx.x / 64; i < a.new_rows; i += THREADS / 64) fork_write(a, w, i, threadIdx.x & 63, 64);
+  for (int p = me; p < a.n_pages; p += THREADS) a.refs_out[p] = refs[p];
 }
 
 // Many rows: the same steps, a launch each.
@@ -303,15 +358,24 @@ __global__ void __launch_bounds__(THREADS) fork_deal_kernel(fi_fork_pages_args a
   __shared__ int sums[THREADS / 64];
   fork_deal(a, ForkSpace(a.workspace, a.rows, a.new_rows, a.n_pages), sums);
 }
-__global__ void __launch_bounds__(256) fork_write_kernel(fi_fork_pages_args a) {
+__global__ void __launch_bounds__(256) fork_take_kernel(fi_fork_pages_args a) {
   const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i < a.new_rows) fork_write(a, w, i, threadIdx.x & 63, 64);
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.new_rows || w.need[i] == 0 || w.first[i] + w.need[i] > w.head[0]) return;
+  if (w.copy[i] >= 0) atomicAdd(a.refs_out + w.last[i], -1);
+  fork_take(w, w.need[i], w.first[i], w.copy[i], w.last[i], w.given, [&](int p, int change) { atomicAdd(a.refs_out + p, change); });
 }
-__global__ void __launch_bounds__(256) fork_copy_kernel(const int* head, const int* source, const int* target, Copies c) {
-  copy_pages(c, blockIdx.x, gridDim.x, head[1], [&](int i, int& from, int& to) {
-    from = source[i];
-    to = target[i];
+// The rows, by the first `row_groups` workgroups, and the copies by the others.
+__global__ void __launch_bounds__(256) fork_write_kernel(fi_fork_pages_args a, Copies c, int row_groups) {
+  const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
+  if ((int)blockIdx.x < row_groups) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i < a.new_rows) fork_write(a, w, i);
+    return;
+  }
+  copy_pages(c, blockIdx.x - row_groups, gridDim.x - row_groups, w.head[1], [&](int i, int& from, int& to) {
+    from = w.source[i];
+    to = w.target[i];
   });
 }
 
@@ -400,7 +464,7 @@ uint64_t fork_workspace(const fi_fork_pages_args& a) {
 
 int launch_fork_pages(const fi_fork_pages_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a.rows <= SMALL_ROWS && a.new_rows <= SMALL_ROWS && (int64_t)a.rows * a.columns <= SMALL_TABLE && (int64_t)a.new_rows * a.columns <= SMALL_TABLE) {
+  if (a.rows <= SMALL_ROWS && a.new_rows <= SMALL_ROWS && a.n_pages <= SMALL_PAGES && (int64_t)a.rows * a.columns <= SMALL_TABLE) {
     fork_small_kernel<<<dim3(1), THREADS, 0, s>>>(a);
   } else {
     const int64_t widest = a.n_pages > a.new_rows ? a.n_pages : a.new_rows, begin = (widest + 255) / 256;
@@ -409,13 +473,16 @@ int launch_fork_pages(const fi_fork_pages_args& a, void* stream) {
     if (a.rows) fork_count_kernel<<<dim3(a.rows < 4096 ? a.rows : 4096), 256, 0, s>>>(a);
     if (a.new_rows) fork_need_kernel<<<dim3((a.new_rows + 3) / 4), 256, 0, s>>>(a);
     fork_deal_kernel<<<dim3(1), THREADS, 0, s>>>(a);
-    if (a.new_rows) fork_write_kernel<<<dim3((a.new_rows + 3) / 4), 256, 0, s>>>(a);
+    if (a.new_rows) fork_take_kernel<<<dim3((a.new_rows + 255) / 256), 256, 0, s>>>(a);
   }
-  if (a.room == 0 || a.new_rows == 0 || a.n_pages == 0) return (int)hipGetLastError();
-  const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
-  for (int at = 0; at < a.n_caches; at += Copies::MOST) {
-    const Copies c = copies_of(a.caches, a.n_caches, at);
-    if (c.n) fork_copy_kernel<<<dim3(copy_groups(c, a.new_rows)), 256, 0, s>>>(w.head, w.source, w.target, c);
+  if (!a.new_rows) return (int)hipGetLastError();
+  const bool copies = a.room > 0 && a.n_pages > 0;
+  int rows = (a.new_rows + 3) / 4;
+  for (int at = 0; at == 0 || (copies && at < a.n_caches); at += Copies::MOST) {
+    const Copies c = copies_of(a.caches, copies ? a.n_caches : 0, at);
+    const uint32_t groups = (uint32_t)rows + copy_groups(c, a.new_rows);
+    if (groups) fork_write_kernel<<<dim3(groups), 256, 0, s>>>(a, c, rows);
+    rows = 0;
   }
   return (int)hipGetLastError();
 }
