@@ -8,13 +8,13 @@ namespace {
 
 // What a lane does with its eight values, four lanes (fewer in a head's last block) a block.  The smallest e with max <= 6 * 2^e: of max = 2^p * (1 + f) it is
 // p - 2 where 1 + f <= 1.5, else p - 1.
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void write8(const T* from, bool there, uint8_t* codes, uint8_t* scale, T* held, int sub) {
   float x[8];
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-  if (there) load8<VEC>(from, x);
+  if (there) load8(from, x);
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);   // (of magnitudes; a NaN's is the largest)
   top = max(top, (uint32_t)__shfl_xor((int)top, 1));
@@ -37,20 +37,18 @@ __device__ __forceinline__ void write8(const T* from, bool there, uint8_t* codes
   if (held) {
     const float r = scale_of(b);
     const u32x4 y = {decode2<0>(w, r), decode2<1>(w, r), decode2<2>(w, r), decode2<3>(w, r)};
-    if constexpr (std::is_same<T, bf16_t>::value) {
-      if constexpr (VEC) *reinterpret_cast<u32x4*>(held) = y;
-      else
-#pragma unroll
-        for (int i = 0; i < 4; ++i) held[2 * i] = (bf16_t)(y[i] & 0xFFFFu), held[2 * i + 1] = (bf16_t)(y[i] >> 16);
+    typedef uint32_t piece __attribute__((ext_vector_type(4), aligned(sizeof(bf16_t))));
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<piece*>(held) = piece{y[0], y[1], y[2], y[3]};
     } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) held[2 * i] = __uint_as_float(y[i] << 16), held[2 * i + 1] = __uint_as_float(y[i] & 0xFFFF0000u);
+      reinterpret_cast<piece*>(held)[0] = piece{y[0] << 16, y[0] & 0xFFFF0000u, y[1] << 16, y[1] & 0xFFFF0000u};
+      reinterpret_cast<piece*>(held)[1] = piece{y[2] << 16, y[2] & 0xFFFF0000u, y[3] << 16, y[3] & 0xFFFF0000u};
     }
   }
 }
 
 // A thread keeps its place in a token (key or value, head, eight values) and goes through the tokens, so it divides once.  per: places of a token.
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __launch_bounds__(256) fp4_write_kernel(fi_fp4_cache_write_args a, int blocks, int per, int tokens_at_once) {
   const int at = blockIdx.y * 256 + threadIdx.x, ahead = at / per, place = at - ahead * per;
   if (ahead >= tokens_at_once) return;
@@ -71,14 +69,9 @@ __global__ void __launch_bounds__(256) fp4_write_kernel(fi_fp4_cache_write_args 
     const int64_t slot = a.slots[t];
     const bool kept = slot >= 0 && slot < a.n_slots;
     const int64_t page = kept ? slot / a.page_size : 0, r = kept ? slot - page * a.page_size : 0;
-    write8<T, VEC>(from + t * in_token, there, kept ? codes + page * c0 + r * c1 + code_at : nullptr, scales + page * s0 + r * s1 + scale_at,
+    write8<T>(from + t * in_token, there, kept ? codes + page * c0 + r * c1 + code_at : nullptr, scales + page * s0 + r * s1 + scale_at,
                    held ? held + t * held_token + held_at : nullptr, sub);
   }
-}
-
-// Whether every row of a tensor starts on 16 bytes (counts as they are: a dimension of one may have any stride).
-bool rows_on_16(const void* p, const int64_t* strides, int es) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && strides[0] * es % 16 == 0 && strides[1] * es % 16 == 0;
 }
 
 }  // namespace
@@ -100,7 +93,7 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   int64_t splits;
   if (p.counted) {
     p.least = 256;
-    splits = (511 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
+    splits = (1023 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
   } else {
     splits = units > 0 ? (1023 + units) / units : 1;
   }
@@ -118,19 +111,12 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
 
 int launch_fp4_cache_write(const fi_fp4_cache_write_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const int es = elem_size(a.dtype), blocks = (a.head_dim + BLOCK - 1) / BLOCK, per = (a.v ? 2 : 1) * a.kv_heads * blocks * 4;
-  const bool vec = rows_on_16(a.k, a.k_strides, es) && (!a.v || rows_on_16(a.v, a.v_strides, es)) && (!a.k_held || rows_on_16(a.k_held, a.k_held_strides, es)) &&
-                   (!a.v_held || rows_on_16(a.v_held, a.v_held_strides, es));
+  const int blocks = (a.head_dim + BLOCK - 1) / BLOCK, per = (a.v ? 2 : 1) * a.kv_heads * blocks * 4;
   const int at_once = per < 256 ? 256 / per : 1, ys = per < 256 ? 1 : (per + 255) / 256;
   const int64_t xs = ((int64_t)a.tokens + at_once - 1) / at_once, most = ys < 4096 ? (4096 + ys - 1) / ys : 1;
   const dim3 grid((uint32_t)(xs < most ? xs : most), (uint32_t)ys);
-  if (a.dtype == FI_F32) {
-    if (vec) fp4_write_kernel<float, true><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
-    else fp4_write_kernel<float, false><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
-  } else {
-    if (vec) fp4_write_kernel<bf16_t, true><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
-    else fp4_write_kernel<bf16_t, false><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
-  }
+  if (a.dtype == FI_F32) fp4_write_kernel<float><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
+  else fp4_write_kernel<bf16_t><<<grid, 256, 0, s>>>(a, blocks, per, at_once);
   return (int)hipGetLastError();
 }
 

@@ -20,30 +20,30 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int BLOCK = FI_FP4_BLOCK, NAN_SCALE = 255, MOST_SCALE = 252;
 
-// Eight values of a head as fp32, from any start (VEC: rows start on 16 bytes).
-template <bool VEC>
+// Eight values of a head as fp32, from any start (the hardware takes loads that are aligned to two bytes).
 __device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
-  if constexpr (VEC) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+  typedef uint32_t piece __attribute__((ext_vector_type(4), aligned(2)));
+  const piece a = *reinterpret_cast<const piece*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(a[i] << 16);
-      x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = bf2f(p[i]);
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
   }
 }
-template <bool VEC>
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  if constexpr (VEC) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-  } else {
+  typedef float piece __attribute__((ext_vector_type(4), aligned(4)));
+  const piece a = reinterpret_cast<const piece*>(p)[0], b = reinterpret_cast<const piece*>(p)[1];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i];
-  }
+  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+// Four results, to any start.
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+  typedef float piece __attribute__((ext_vector_type(4), aligned(4)));
+  *reinterpret_cast<piece*>(p) = piece{a, b, c, d};
+}
+__device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
+  typedef uint32_t piece __attribute__((ext_vector_type(2), aligned(2)));
+  *reinterpret_cast<piece*>(p) = piece{pack_bf16x2(a, b), pack_bf16x2(c, d)};
 }
 // Byte B of a dword of codes: two values as bf16, the low half's in the low half.
 template <int B>
@@ -56,10 +56,12 @@ __device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b
 // Lane l holds scores of query l & 15, of the keys 4 (l >> 4) + i and 16 + 4 (l >> 4) + i, i < 4, of a tile, and these registers are the operand of the second product
 // as they stand: its lane l has to bring values of just these eight keys.  The reduction over a head's values may run in any order, so lane l brings the KD dwords
 // of codes from KD (l >> 4) on, of key l & 15.  Values: DT of a head's, from DT (l & 15) on, of each of the eight keys; two keys' are paired by a byte permute.
-// All loads go to registers, a tile ahead: lanes of a key read 64 bytes and more that follow each other.
-// MODE: how the lanes find their keys.  WHOLE pages hold a multiple of 16 keys, so the 16 keys of half a tile lie in one page, whose number and address are the wave's (scalar registers), and
-// a lane's offsets are the same in every tile; FULL heads beside that have 32 KD values, so a lane's codes of a key are one load.  Else every lane looks up its own ten keys.
-enum Fp4Mode { ANY, WHOLE, FULL };
+// MODE: how keys come to the lanes.  In pages that hold a multiple of 16 keys, the 16 keys of half a tile lie in one page, whose number and address are the wave's (scalar registers), and a
+// lane's offsets are the same in every tile: direct loads bring a tile to LDS, a wave's own, while the one before it is worked on.  RING: heads of 64, 128 and 256, by 16
+// bytes; WORDS: others, by 4.  ANY: other pages, or strides that the offsets do not hold; every lane looks up its own ten keys and loads to registers, a tile ahead.
+// 4 tokens over 131071 keys: 119 us with 16 waves on a unit, of which the loads alone take 108 (5.5 TB/s) and all that is computed alone 78; loaded to registers, which leaves room for 12
+// waves, 128, and 196 with addresses by vector instructions.  Three tiles on their way, and half the waves, are no faster.
+enum Fp4Mode { ANY, WORDS, RING };
 template <typename T, int KD_, int NB_, Fp4Mode MODE_>
 struct Fp4 {
   static constexpr int KD = KD_, NB = NB_;                                             // dwords of codes of a key per lane; columns of queries
@@ -69,7 +71,11 @@ struct Fp4 {
   static constexpr int VW = KD == 8 ? 2 : 1, DT = KD == 2 ? 4 : 8 * VW;                // words of codes of a value row per lane; values in them
   static constexpr int KS = KD == 8 ? 2 : KD == 3 ? 3 : 1;                             // scales of a key per lane
   static constexpr int WAVES = 4;
-  static constexpr int LDS = WAVES * (NB * DT * 1024 + NB * 512);
+  // a tile in LDS: codes of keys, codes of values, scales of either (SB bytes a key; WORDS: four bytes a scale, PS times 64 of them a half); what a wave issues for it
+  static constexpr int PS = KD == 8 ? 2 : 1, SB = KD == 8 ? 8 : 4, CODES = 512 * KD, SCALES = MODE == RING ? 32 * SB : 512 * PS, TILE = 2 * CODES + 2 * SCALES;
+  static constexpr int LOADS = MODE == RING ? (KD == 8 ? 12 : 8) : 4 * (KD + PS), DEPTH = 2;
+  static constexpr int JOIN = NB * DT * 1024 + NB * 512;   // a wave's sums
+  static constexpr int LDS = WAVES * (MODE != ANY && DEPTH * TILE > JOIN ? DEPTH * TILE : JOIN);
 };
 template <typename F>
 struct Fp4Tile {
@@ -93,47 +99,21 @@ struct Fp4Lane {
       vs[c] = most(F::DT == 4 ? m >> 3 : 4 * c + (m >> 2), blocks);
     }
   }
-  __device__ __forceinline__ void ahead(uint32_t codes, uint32_t scales, uint32_t value_codes, uint32_t value_scales) {
-#pragma unroll
-    for (int c = 0; c < F::KD; ++c) k[c] += codes;
-#pragma unroll
-    for (int c = 0; c < F::KS; ++c) ks[c] += scales;
-#pragma unroll
-    for (int c = 0; c < F::VW; ++c) v[c] += value_codes, vs[c] += value_scales;
-  }
 };
-// A lane's address: `base` is the wave's (in WHOLE and FULL), so that a load takes it from scalar registers with the lane's offset as it stands.  (The empty asm keeps the
-// compiler from adding the two ahead of the loop, which leaves an addition of 64 bits and two registers for every load in it.)
-__device__ __forceinline__ const uint8_t* lane_at(const uint8_t* base, uint32_t off) {
-  asm("" : "+v"(off));
-  return base + off;
-}
 template <typename F>
 __device__ __forceinline__ void fp4_load_key(Fp4Tile<F>& t, int h, const Fp4Lane<F>& at, const uint8_t* codes, const uint8_t* scales) {
-  if constexpr (F::MODE == FULL) {
-    const uint8_t* const p = lane_at(codes, at.k[0]);
 #pragma unroll
-    for (int c = 0; c < F::KD; c += 4) {
-      constexpr int N = F::KD < 4 ? F::KD : 4;
-      typedef uint32_t vec __attribute__((ext_vector_type(N), aligned(4)));
-      const vec x = *reinterpret_cast<const vec*>(p + 4 * c);
+  for (int c = 0; c < F::KD; ++c) t.k[h][c] = *reinterpret_cast<const uint32_t*>(codes + at.k[c]);
 #pragma unroll
-      for (int i = 0; i < N; ++i) t.k[h][c + i] = x[i];
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < F::KD; ++c) t.k[h][c] = *reinterpret_cast<const uint32_t*>(lane_at(codes, at.k[c]));
-  }
-#pragma unroll
-  for (int c = 0; c < F::KS; ++c) t.ks[h][c] = *lane_at(scales, at.ks[c]);
+  for (int c = 0; c < F::KS; ++c) t.ks[h][c] = scales[at.ks[c]];
 }
 template <typename F>
 __device__ __forceinline__ void fp4_load_value(Fp4Tile<F>& t, int j, const Fp4Lane<F>& at, const uint8_t* codes, const uint8_t* scales) {
 #pragma unroll
   for (int c = 0; c < F::VW; ++c) {
-    const uint8_t* const p = lane_at(codes, at.v[c]);
+    const uint8_t* const p = codes + at.v[c];
     t.v[j][c] = F::DT == 4 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint32_t*>(p);
-    t.vs[j][c] = *lane_at(scales, at.vs[c]);
+    t.vs[j][c] = scales[at.vs[c]];
   }
 }
 
@@ -278,7 +258,7 @@ struct Fp4Walk {
   Fp4Lane<F> at;
   uint32_t inv;                     // floor(2^32 / page size): a quotient by it is right or one too small
   int keys, last_column, page[2];   // page: of the tile that is loaded next
-  // where a row of a page begins: in WHOLE and FULL by two scalar products of 32 bits (strides are below 2^31 there: checked on the host)
+  // where a row of a page begins: in WHOLE pages by two scalar products of 32 bits (strides are below 2^31 there: checked on the host)
   static __device__ __forceinline__ uint64_t row_at(const int64_t* strides, int p, int row) {
     if constexpr (F::MODE != ANY) return (uint64_t)(uint32_t)p * (uint32_t)strides[0] + (uint64_t)(uint32_t)row * (uint32_t)strides[1];
     else return (uint64_t)((int64_t)p * strides[0] + (int64_t)row * strides[1]);
@@ -289,10 +269,6 @@ struct Fp4Walk {
         inv(args.page_size == 1 ? ~0u : (uint32_t)((1ull << 32) / (uint32_t)args.page_size)), keys(w.keys) {
     int row;
     last_column = place(keys - 1, row);
-    if constexpr (F::MODE != ANY) {   // (offsets of 16 rows are below 2^31: checked on the host)
-      const int lane = threadIdx.x & 63, r = lane & 15, first = 4 * (lane >> 4);
-      at.ahead((uint32_t)(r * a.k_codes_strides[1]), (uint32_t)(r * a.k_scales_strides[1]), (uint32_t)(first * a.v_codes_strides[1]), (uint32_t)(first * a.v_scales_strides[1]));
-    }
   }
   __device__ __forceinline__ int place(int key, int& row) const {
     uint32_t c = __umulhi((uint32_t)key, inv), r = (uint32_t)key - c * (uint32_t)a.page_size;
@@ -312,29 +288,30 @@ struct Fp4Walk {
       }
     }
   }
+  // For both halves of a tile in whole pages: where their rows of codes and scales begin.
+  template <typename Half>
+  __device__ __forceinline__ void halves(int tile, Half half) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      int row;
+      place(tile * 32 + 16 * h, row);
+      const int p = clamp_int(page[h], 0, a.n_pages - 1);
+      half(h, k + row_at(a.k_codes_strides, p, row), ks + row_at(a.k_scales_strides, p, row), v + row_at(a.v_codes_strides, p, row), vs + row_at(a.v_scales_strides, p, row));
+    }
+  }
   __device__ __forceinline__ void load(Fp4Tile<F>& t, int tile) {
     const int lane = threadIdx.x & 63, kq = lane >> 4, r = lane & 15;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int first = tile * 32 + 16 * h;
-      if constexpr (F::MODE != ANY) {
-        int row;
-        place(first, row);
-        const int p = clamp_int(page[h], 0, a.n_pages - 1);
-        fp4_load_key<F>(t, h, at, k + row_at(a.k_codes_strides, p, row), ks + row_at(a.k_scales_strides, p, row));
-        const uint8_t *from = v + row_at(a.v_codes_strides, p, row), *scales = vs + row_at(a.v_scales_strides, p, row);
+      auto find = [&](int key, int& p, int& row) { p = page_at(place(key < keys ? key : keys - 1, row)); };
+      int p, row;
+      find(first + r, p, row);
+      fp4_load_key<F>(t, h, at, k + row_at(a.k_codes_strides, p, row), ks + row_at(a.k_scales_strides, p, row));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) fp4_load_value<F>(t, 4 * h + i, at, from + i * (uint32_t)a.v_codes_strides[1], scales + i * (uint32_t)a.v_scales_strides[1]);
-      } else {
-        auto find = [&](int key, int& p, int& row) { p = page_at(place(key < keys ? key : keys - 1, row)); };
-        int p, row;
-        find(first + r, p, row);
-        fp4_load_key<F>(t, h, at, k + row_at(a.k_codes_strides, p, row), ks + row_at(a.k_scales_strides, p, row));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          find(first + 4 * kq + i, p, row);
-          fp4_load_value<F>(t, 4 * h + i, at, v + row_at(a.v_codes_strides, p, row), vs + row_at(a.v_scales_strides, p, row));
-        }
+      for (int i = 0; i < 4; ++i) {
+        find(first + 4 * kq + i, p, row);
+        fp4_load_value<F>(t, 4 * h + i, at, v + row_at(a.v_codes_strides, p, row), vs + row_at(a.v_scales_strides, p, row));
       }
     }
   }
@@ -342,6 +319,168 @@ struct Fp4Walk {
     int row;
     const int p = page_at(place(key, row));
     return vs + row_at(a.v_scales_strides, p, row);
+  }
+};
+
+// A wave's ring.  RING: rows of a head are KD pieces of 16 bytes; keys lie in their order, values so that the four rows that lanes read at a time follow each other (row
+// 4 k + i of a half at place 4 i + k): reads of 64 and 128 values meet no bank twice; of 256 pieces change places with the row, which leaves two at most.  WORDS: rows of codes, and of
+// scales as words, one behind the other; lanes past the half's end bring its last words again, so that every tile is as many loads.
+template <typename F>
+struct Fp4Ring {
+  static constexpr int KD = F::KD, PARTS = F::MODE == WORDS ? KD : KD == 8 ? 2 : 1;   // load instructions of half a tile's codes
+  uint8_t* const base;
+  uint32_t k[PARTS], v[PARTS], ks[F::PS], vs[F::PS];   // a lane's bytes from half a tile's first row: its pieces, its scales
+  uint32_t key_at, value_at, key_scale, value_scale;   // where the lane reads
+  uint32_t row_bytes, row_scales;                      // (WORDS) of a row in LDS
+  static __device__ __forceinline__ int turn_k(int row) { return KD == 8 ? row & 7 : 0; }
+  static __device__ __forceinline__ int turn_v(int place) { return KD == 8 ? (place >> 1 & 1) << 2 : 0; }
+  __device__ __forceinline__ Fp4Ring(uint8_t* b, const fi_fp4_tree_attention_args& a) : base(b) {
+    const int lane = threadIdx.x & 63, kq = lane >> 4, r = lane & 15;
+    const uint32_t kt = (uint32_t)a.k_codes_strides[1], vt = (uint32_t)a.v_codes_strides[1], kst = (uint32_t)a.k_scales_strides[1], vst = (uint32_t)a.v_scales_strides[1];
+    if constexpr (F::MODE == WORDS) {
+      const int words = a.head_dim / 8, blocks = (a.head_dim + BLOCK - 1) / BLOCK;
+      auto most = [](int x, int n) { return (uint32_t)(x < n ? x : n - 1); };
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int piece = j * 64 + lane;
+        const uint32_t row = most(piece / words, 16), c = 4 * most(piece - (int)row * words, words);
+        k[j] = row * kt + c;
+        v[j] = row * vt + c;
+      }
+#pragma unroll
+      for (int j = 0; j < F::PS; ++j) {
+        const int piece = j * 64 + lane;
+        const uint32_t row = most(piece / blocks, 16), c = most(piece - (int)row * blocks, blocks);
+        ks[j] = row * kst + c;
+        vs[j] = row * vst + c;
+      }
+      row_bytes = 4 * words;
+      row_scales = 4 * blocks;
+      key_at = r * row_bytes;
+      value_at = F::CODES + 4 * kq * row_bytes;
+      key_scale = 2 * F::CODES + r * row_scales;
+      value_scale = 2 * F::CODES + F::SCALES + 4 * kq * row_scales;
+    } else {
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int piece = j * 64 + lane, place = piece / KD & 15, c = piece % KD, row = 4 * (place & 3) + (place >> 2);
+        k[j] = (uint32_t)place * kt + 16 * (c ^ turn_k(place));
+        v[j] = (uint32_t)row * vt + 16 * (c ^ turn_v(place));
+      }
+      const int key = KD == 8 ? lane >> 1 & 15 : r, part = KD == 8 ? 4 * (lane & 1) : 0;
+      ks[0] = (uint32_t)key * kst + part;
+      vs[0] = (uint32_t)key * vst + part;
+      key_at = KD == 8 ? r * 128 : r * 16 * KD + kq * 4 * KD;
+      value_at = F::CODES + 16 * KD * kq;   // of place kq, the first of four
+      key_scale = 2 * F::CODES + r * F::SB + (KD == 2 ? kq >> 1 : KD == 4 ? kq : 2 * kq);
+      value_scale = 2 * F::CODES + 32 * F::SB + 4 * kq * F::SB;
+    }
+  }
+  // Half h of tile number `slot` of the ring: rows from these addresses on.
+  __device__ __forceinline__ void load(int slot, int h, const uint8_t* kc, const uint8_t* kss, const uint8_t* vc, const uint8_t* vss) const {
+    const int lane = threadIdx.x & 63;
+    uint8_t* const tile = base + slot * F::TILE;
+    uint8_t *const codes = tile + h * (F::CODES / 2), *const scales = tile + 2 * F::CODES + h * (F::SCALES / 2);
+    if constexpr (F::MODE == WORDS) {
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        load_lds_off<4>(kc, k[j], codes + j * 256);
+        load_lds_off<4>(vc, v[j], codes + F::CODES + j * 256);
+      }
+#pragma unroll
+      for (int j = 0; j < F::PS; ++j) {
+        load_lds_off<1>(kss, ks[j], scales + j * 256);
+        load_lds_off<1>(vss, vs[j], scales + F::SCALES + j * 256);
+      }
+    } else {
+      if (KD != 2 || lane < 32) {
+#pragma unroll
+        for (int j = 0; j < PARTS; ++j) {
+          load_lds_off<16>(kc, k[j], codes + j * 1024);
+          load_lds_off<16>(vc, v[j], codes + F::CODES + j * 1024);
+        }
+      }
+      if (lane < (KD == 8 ? 32 : 16)) {
+        load_lds_off<(KD == 2 ? 2 : 4)>(kss, ks[0], scales);
+        load_lds_off<(KD == 2 ? 2 : 4)>(vss, vs[0], scales + F::SCALES);
+      }
+    }
+  }
+  __device__ __forceinline__ void read(Fp4Tile<F>& t, int slot, const Fp4Lane<F>& at) const {
+    const int lane = threadIdx.x & 63, kq = lane >> 4, m = lane & 15, r = lane & 15;
+    const uint8_t* const tile = base + slot * F::TILE;
+    if constexpr (F::MODE == WORDS) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t *const codes = tile + h * (F::CODES / 2), *const scales = tile + h * (F::SCALES / 2);
+#pragma unroll
+        for (int c = 0; c < KD; ++c) t.k[h][c] = *reinterpret_cast<const uint32_t*>(codes + key_at + at.k[c]);
+#pragma unroll
+        for (int c = 0; c < F::KS; ++c) t.ks[h][c] = scales[key_scale + 4 * at.ks[c]];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t *const codes = tile + h * (F::CODES / 2), *const scales = tile + h * (F::SCALES / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int w = 0; w < F::VW; ++w) {
+            const uint8_t* const row = codes + value_at + i * row_bytes + at.v[w];
+            t.v[4 * h + i][w] = F::DT == 4 ? (uint32_t)*reinterpret_cast<const uint16_t*>(row) : *reinterpret_cast<const uint32_t*>(row);
+            t.vs[4 * h + i][w] = scales[value_scale + i * row_scales + 4 * at.vs[w]];
+          }
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* const row = tile + h * (F::CODES / 2) + key_at;
+        if constexpr (KD == 2) {
+          const uint2 x = *reinterpret_cast<const uint2*>(row);
+          t.k[h][0] = x.x, t.k[h][1] = x.y;
+        } else {
+#pragma unroll
+          for (int c = 0; c < KD / 4; ++c) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(KD == 8 ? row + 16 * ((2 * kq + c) ^ turn_k(r)) : row);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.k[h][4 * c + i] = x[i];
+          }
+        }
+        const uint8_t* const scales = tile + h * 16 * F::SB + key_scale;
+        if constexpr (KD == 8) {
+          const uint32_t x = *reinterpret_cast<const uint16_t*>(scales);
+          t.ks[h][0] = x & 255, t.ks[h][1] = x >> 8;
+        } else {
+          t.ks[h][0] = *scales;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint8_t* const row = tile + h * (F::CODES / 2) + value_at + i * 4 * 16 * KD;   // place 4 i + kq
+#pragma unroll
+          for (int w = 0; w < F::VW; ++w) {
+            const int c = 4 * w + (m >> 2);
+            if constexpr (KD == 2) t.v[4 * h + i][w] = *reinterpret_cast<const uint16_t*>(row + 2 * m);
+            else t.v[4 * h + i][w] = *reinterpret_cast<const uint32_t*>(row + 16 * (c ^ turn_v(kq)) + 4 * (m & 3));
+          }
+        }
+        u32x4 x[F::SB / 4];
+#pragma unroll
+        for (int w = 0; w < F::SB / 4; ++w) x[w] = reinterpret_cast<const u32x4*>(tile + h * 16 * F::SB + value_scale)[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int w = 0; w < F::VW; ++w)
+            t.vs[4 * h + i][w] = KD == 8 ? x[i >> 1][2 * (i & 1) + w] >> (8 * (m >> 2)) & 255 : x[0][i] >> (8 * (KD == 2 ? m >> 3 : m >> 2)) & 255;
+      }
+    }
+  }
+  // This wave's loads have arrived but for those of the `later` tiles asked for since (DEPTH - 1 at most).
+  static __device__ __forceinline__ void wait(int later) {
+    static_assert(F::DEPTH == 2, "a tile is on its way while one is worked on");
+    if (later >= 1) arrived_but<F::LOADS>();
+    else arrived_but<0>();
   }
 };
 
@@ -355,6 +494,20 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
   const int t0 = share(wave), t1 = share(wave + 1);
   auto row_of = [&](int nb) { return first + 16 * nb + (lane & 15); };
   auto mine = [&](int nb) { return row_of(nb) < rows ? row_of(nb) : rows - 1; };
+  // The first tile is on its way before the queries are asked for: loads come back in order, so who has waited for those has this.
+  Fp4Walk<F> walk(a, w);
+  const Fp4Ring<F> ring(smem + wave * F::DEPTH * F::TILE, a);
+  int into = 0, from = 0;   // slots of the ring
+  auto load_ring = [&](int t) {
+    walk.halves(t, [&](int h, const uint8_t* kc, const uint8_t* kss, const uint8_t* vc, const uint8_t* vss) { ring.load(into, h, kc, kss, vc, vss); });
+    into = into + 1 < F::DEPTH ? into + 1 : 0;
+    if (t + 1 < t1) walk.ask(t + 1);
+  };
+  if constexpr (F::MODE != ANY)
+    if (t0 < t1) {
+      walk.ask(t0);
+      load_ring(t0);
+    }
   // the queries: values 8 (KD kq + c) .. of the lane's row of every column, as they are or in three terms; zeros past the head's end
   u32x4 q[NB][F::QT][F::KD];
 #pragma unroll
@@ -365,7 +518,7 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
     for (int c = 0; c < F::KD; ++c) {
       const int d = 8 * (F::KD * kq + c);
       float x[8] = {};
-      if (d < D) load8<false>(from + d, x);
+      if (d < D) load8(from + d, x);
       u32x4 terms[F::QT];
       terms8<F::QT>(x, terms);
 #pragma unroll
@@ -386,25 +539,41 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
     return tree_visible(a, w, node, a.mask ? a.mask + (int64_t)(w.n0 + node) * a.mask_words : nullptr, key);
   };
   if (t0 < t1) {
-    Fp4Walk<F> walk(a, w);
-    Fp4Tile<F> x, y;
+    Fp4Tile<F> x;
     bool strange = false;
-    auto load = [&](Fp4Tile<F>& tile, int t) {
-      walk.load(tile, t);
-      if (t + 1 < t1) walk.ask(t + 1);
-      __builtin_amdgcn_sched_barrier(0);   // (they are on their way before the tile at hand is worked on)
-    };
     auto attend = [&](Fp4Tile<F>& tile, int t) {
       strange |= fp4_attend<F>(st, q, tile, c, (t + 1) * 32 > w.cached, [&](int nb) { return visible(nb, t * 32); });
     };
-    walk.ask(t0);
-    load(x, t0);
-    for (int t = t0; t < t1; t += 2) {
-      if (t + 1 < t1) load(y, t + 1);
-      attend(x, t);
-      if (t + 1 >= t1) break;
-      if (t + 2 < t1) load(x, t + 2);
-      attend(y, t + 1);
+    if constexpr (F::MODE != ANY) {
+      // (a wait that the compiler puts before the queries' first use would wait for the ring's loads, too)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int term = 0; term < F::QT; ++term)
+#pragma unroll
+          for (int i = 0; i < F::KD; ++i) asm volatile("" : "+v"(q[nb][term][i]));
+      for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) load_ring(t + 1);   // (where the tile before this one was: it has been read)
+        Fp4Ring<F>::wait(t1 - 1 - t);
+        ring.read(x, from, walk.at);
+        from = from + 1 < F::DEPTH ? from + 1 : 0;
+        attend(x, t);
+        arrived_but<63>();   // (reads of LDS only)
+      }
+    } else {
+      Fp4Tile<F> y;
+      auto load = [&](Fp4Tile<F>& tile, int t) {
+        walk.load(tile, t);
+        __builtin_amdgcn_sched_barrier(0);   // (they are on their way before the tile at hand is worked on)
+      };
+      load(x, t0);
+      for (int t = t0; t < t1; t += 2) {
+        if (t + 1 < t1) load(y, t + 1);
+        attend(x, t);
+        if (t + 1 >= t1) break;
+        if (t + 2 < t1) load(x, t + 2);
+        attend(y, t + 1);
+      }
     }
     if (__any(strange)) {   // blocks of NaN in masked tiles: for the queries that see the key
       const int masked = w.cached / 32 * 32, blocks = (D + BLOCK - 1) / BLOCK;
@@ -423,13 +592,16 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       }
     }
   }
-  // the waves' sums against the largest maximum, added in the order of the waves: wave x adds the values d with d % WAVES == x
-  f32x4* const sums = reinterpret_cast<f32x4*>(smem) + lane;
+  // the waves' sums against the largest maximum, added in the order of the waves: wave x adds its share of the values
+  if constexpr (F::MODE != ANY) __syncthreads();   // (they lie where other waves' tiles were)
+  float* const sums = reinterpret_cast<float*>(smem) + lane;   // (element by element, so that reads of one element meet no bank twice)
   float2* const stats = reinterpret_cast<float2*>(smem + WAVES * NB * DT * 1024) + lane;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) sums[((wave * NB + nb) * DT + d) * 64] = st.o[nb][d];
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[(((wave * NB + nb) * DT + d) * 4 + i) * 64] = st.o[nb][d][i];
     stats[(wave * NB + nb) * 64] = make_float2(st.top[nb], over_keys_sum(st.total[nb]));
   }
   __syncthreads();
@@ -446,28 +618,30 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       total += other.y * factor[x];
     }
     const float inv = w.splits > 1 ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
+    constexpr int N = DT < 8 ? DT : 8;
     const bool there = row_of(nb) < rows;
     const int node = mine(nb) / group, head = w.hk * group + mine(nb) % group;
     const int64_t row = (int64_t)(w.n0 + node) * a.q_heads + head;
     T* const out = static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1];
     float* const part = part_sums(a, p, row, w.split);
-    // DT values from DT (4 kq + i) on (of KD 8: 8 of each half) are the lane's; a wave takes DT / WAVES that follow each other
-    constexpr int N = DT / WAVES;
+    // 4 DT values are the lane's: DT from DT (4 kq + i) on for each i < 4 (of KD 8: 8 of each half).  Wave i takes those.
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int e = 0; e < DT; e += N) {
       float v[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) v[n] = 0.0f;
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int x = 0; x < WAVES; ++x) v[n] += reinterpret_cast<const float*>(&sums[((x * NB + nb) * DT + wave * N + n) * 64])[i] * factor[x];
-      const int e = wave * N, d = F::VW == 2 ? (e >> 3) * 128 + 8 * (4 * kq + i) + (e & 7) : DT * (4 * kq + i) + e;
+        for (int x = 0; x < WAVES; ++x) v[n] += sums[(((x * NB + nb) * DT + e + n) * 4 + wave) * 64] * factor[x];
+      const int d = (e >> 3) * 128 + (DT < 8 ? DT : 8) * (4 * kq + wave);
       if (!there || d >= D) continue;
+      if (w.splits > 1) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        if (w.splits > 1) part[d + n] = v[n];
-        else fi::st(out + d + n, v[n] * inv);
+        for (int n = 0; n < N; n += 4) *reinterpret_cast<float4*>(part + d + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
+      } else {
+#pragma unroll
+        for (int n = 0; n < N; n += 4) store4(out + d + n, v[n] * inv, v[n + 1] * inv, v[n + 2] * inv, v[n + 3] * inv);
       }
     }
     if (w.splits > 1 && there && wave == 0 && kq == 0) *reinterpret_cast<float2*>(part_stats(a, p, row, w.split)) = make_float2(top, total);
@@ -475,7 +649,8 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
 }
 
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
-__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 ? (NB == 1 ? 3 : NB == 2 ? 2 : 1) : 1)) fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
+__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : KD <= 4 && sizeof(T) == 2 && NB <= 2 ? 2 : 1))
+    fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
   using F = Fp4<T, KD, NB, MODE>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
   if constexpr (COUNTED) {
@@ -490,15 +665,21 @@ __global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 ? (NB == 1 ? 3
     if (tree_direct(a, p, w)) fp4_work<T, F>(a, w, p, smem);
   }
 }
-
 template <typename T, int KD, int NB, Fp4Mode MODE>
 int launch_fp4_tree(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipStream_t s) {
   const TreeSplit t = {p.splits, p.least / 32, 32, 8, 16 * NB, p.packed ? 0 : p.blocks, p.header};
   const int64_t direct = p.packed ? p.packed : (int64_t)a.n_seqs * p.blocks, all_rows = a.nodes * a.q_heads;
   if (!p.counted && !one_launch(direct, 256)) return kTooLarge;
   if (p.splits > 1 && !one_launch((all_rows + 3) / 4, 256)) return kTooLarge;
-  if (p.counted) fp4_tree_kernel<T, KD, NB, MODE, true><<<dim3(KD <= 4 && NB == 1 && sizeof(T) == 2 ? 768 : 512), 256, 0, s>>>(a, t);
-  else fp4_tree_kernel<T, KD, NB, MODE, false><<<dim3((uint32_t)direct, (uint32_t)a.kv_heads, (uint32_t)p.splits), 256, 0, s>>>(a, t);
+  const dim3 grid((uint32_t)direct, (uint32_t)a.kv_heads, (uint32_t)p.splits);
+  if (p.counted) {   // as many workgroups as run at a time: two rounds of them take twice as long (12 fp32 trees up to 37 nodes over up to 2003 keys: 36 us, 29)
+    static const int on_unit = [] {
+      int n = 0;
+      return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fp4_tree_kernel<T, KD, NB, MODE, true>, 256, 0) != hipSuccess || n < 1 ? 1 : n < 4 ? n : 4;
+    }();
+    fp4_tree_kernel<T, KD, NB, MODE, true><<<dim3(256 * on_unit), 256, 0, s>>>(a, t);
+  }
+  if (!p.counted) fp4_tree_kernel<T, KD, NB, MODE, false><<<grid, 256, 0, s>>>(a, t);
   constexpr int PER = KD <= 2 ? 1 : KD <= 4 ? 2 : 4;
   if (p.splits > 16 && all_rows <= 1024) tree_join_kernel<fi_fp4_tree_attention_args, T, PER, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, t, p.counted);
   else if (p.splits > 1) tree_join_kernel<fi_fp4_tree_attention_args, T, PER, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, t, p.counted);
@@ -507,9 +688,18 @@ int launch_fp4_tree(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipSt
 template <typename T, int KD, int NB>
 int launch_fp4_mode(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipStream_t s) {
   const int64_t far = (1ll << 31) / 16 - 1024;
-  bool whole = a.page_size % 16 == 0;
-  for (const int64_t* strides : {a.k_codes_strides, a.k_scales_strides, a.v_codes_strides, a.v_scales_strides}) whole = whole && strides[0] < 1ll << 31 && strides[1] < far;
-  return !whole ? launch_fp4_tree<T, KD, NB, ANY>(a, p, s) : a.head_dim == 32 * KD ? launch_fp4_tree<T, KD, NB, FULL>(a, p, s) : launch_fp4_tree<T, KD, NB, WHOLE>(a, p, s);
+  bool whole = a.page_size % 16 == 0, ring = a.head_dim == 32 * KD;
+  auto look = [&](const void* p, const int64_t* strides, int align) {
+    whole = whole && strides[0] < 1ll << 31 && strides[1] < far;
+    ring = ring && reinterpret_cast<uintptr_t>(p) % align == 0 && strides[0] % align == 0 && strides[1] % align == 0 && strides[2] % align == 0;
+  };
+  look(a.k_codes, a.k_codes_strides, 16);
+  look(a.v_codes, a.v_codes_strides, 16);
+  look(a.k_scales, a.k_scales_strides, KD == 2 ? 2 : 4);
+  look(a.v_scales, a.v_scales_strides, KD == 2 ? 2 : 4);
+  if constexpr (KD != 3)
+    if (whole && ring) return launch_fp4_tree<T, KD, NB, RING>(a, p, s);
+  return whole ? launch_fp4_tree<T, KD, NB, WORDS>(a, p, s) : launch_fp4_tree<T, KD, NB, ANY>(a, p, s);
 }
 template <typename T, int KD>
 int launch_fp4_columns(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipStream_t s) {

@@ -5,7 +5,7 @@
 
 namespace fi {
 
-// One direct load: the active lanes' N bytes (1: a byte, as a dword) at `from` go to at + max(N, 4) * lane (at: the same for the wave).  In assembler, which has
+// One direct load: the active lanes' N bytes (1 and 2: as a dword) at `from` go to at + max(N, 4) * lane (at: the same for the wave).  In assembler, which has
 // no output register: the compiler knows nothing of the load, so it puts no wait of its own before other reads of LDS (it does before transposed ones,
 // whose tile it cannot tell from the one under way); every wait is written out in the kernels.
 // (The low word of a pointer into LDS is its offset there.  m0 is the compiler's for such instructions only, and it sets it before each of its own.)
@@ -26,6 +26,7 @@ __device__ __forceinline__ void load_lds_off(const void* base, uint32_t off, uin
   const uint64_t shared = (uint64_t)high << 32 | low;
   if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(shared) : "memory");
   else if constexpr (N == 4) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(m0), "v"(off), "s"(shared) : "memory");
+  else if constexpr (N == 2) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_ushort %1, %2" ::"s"(m0), "v"(off), "s"(shared) : "memory");
   else asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_ubyte %1, %2" ::"s"(m0), "v"(off), "s"(shared) : "memory");
 }
 
