@@ -85,17 +85,29 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   const int per_block = 16 * p.nb;
   p.blocks = (int)((rows + per_block - 1) / per_block);
   const int64_t streams = (int64_t)a.n_seqs * a.kv_heads, units = streams * p.blocks;
+  // workgroups that run on a unit at a time, by their registers
+  p.on_unit = p.kd == 8 || p.nb == 4 ? 1 : a.dtype == FI_F32 ? (p.nb == 1 || p.kd == 2 ? 2 : 1) : p.nb == 1 ? 4 : 2;
+  const int64_t at_once = 256 * p.on_unit;
   auto some = [](int64_t n) { return n < 1 << 20 ? n : 1 << 20; };   // (products of two stay in 64 bits)
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
-  p.least = 128;
+  // Short histories: a wave for each, nothing to join (us, four waves / one; 8 heads of 128 in bf16, lengths up to 60: 4 sequences 7.4 / 6.1, 256 of them 14.6 / 8.6; 250: 10.5 / 11.8
+  // and 22.4 / 18.7; 256 sequences of 32 heads of 72, 500: 113 / 92).
+  p.small = p.nb <= 2 && (a.max_length <= 64 || (int64_t)a.max_length * 8 <= units);
+  // Counted, where there is much to share out for what runs at a time and histories are long beside their number: where they are all as long that loses some microseconds, where they are
+  // ragged it gains more (us, direct / counted, all as long and, r, spread over their logarithm. 8 heads of 128, a node each: 4 sequences of 32000 keys 33.4 / 37.3, r 30.4 / 24.3; 16 of 8000
+  // 32.7 / 38.7, r 29.0 / 21.2; 256 of 2000 121 / 121, r 45.4 / 49.3. Eight nodes: 12 of 2000 28.7 / 29.3, r 18.2 / 19.4; of 4000 37.1 / 35.7, r 23.5 / 21.9; 100 of 1000 46.9 / 71.2,
+  // r 27.6 / 42.2. 37 nodes: 2 of 1000 23.1 / 26.4, r 20.9 / 24.4; of 2000 38.5 / 33.5, r 24.1 / 26.1; 12 of 2000 93 / 83, r 46 / 47).
+  const int64_t much = p.on_unit == 1 ? 80 * 1024 : p.on_unit == 2 ? 320 * 1024 : 960 * 1024;
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
-  p.counted = a.n_seqs > 1 && a.n_seqs <= SEQS && parts(p.least) > 1 && some(units) * parts(p.least) > 256 && line < 2147483648.0;
+  p.counted = !p.small && a.n_seqs > 1 && a.n_seqs <= SEQS && some(units) * a.max_length >= much && a.max_length >= 2 * units && line < 2147483648.0;
   int64_t splits;
   if (p.counted) {
     p.least = 256;
-    splits = (1023 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
+    splits = (at_once - 1 + (int64_t)a.kv_heads * p.blocks) / ((int64_t)a.kv_heads * p.blocks);
   } else {
-    splits = units > 0 ? (1023 + units) / units : 1;
+    // Parts of fewer keys where parts are few (2 sequences of 2000 keys, parts of 128 / 256: 10.2 us / 11.7; of 8000 14.5 / 12.7); below 384 keys a second launch costs more than it saves (250: 10.5, 8.5).
+    p.least = some(units) * parts(128) > 256 ? 256 : 128;
+    splits = a.max_length <= 384 || p.small || units == 0 ? 1 : (at_once - 1 + units) / units;
   }
   if (splits > parts(p.least)) splits = parts(p.least);
   const int64_t room = (64ll << 20) / ((int64_t)a.nodes * a.q_heads * (a.head_dim + 2) * 4 + 1);   // the workspace stays below 64 MB as far as the chip is full

@@ -11,7 +11,7 @@ namespace fi {
 
 // How a call is shared out, from its sizes alone (the workspace goes by it): dwords of codes of a key that a lane has, columns of 16 queries a wave has, blocks of
 // rows of a sequence, parts of its keys and the least keys of one, floats before the parts in the workspace, blocks of all sequences together where they are so dealt out.
-struct Fp4Plan { int kd, nb, blocks, splits, least, header; bool counted; int64_t packed; };
+struct Fp4Plan { int kd, nb, on_unit, blocks, splits, least, header; bool counted, small; int64_t packed; };   // small: a wave a workgroup, and parts are none
 Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a);
 int launch_fp4_tree_f32(const fi_fp4_tree_attention_args& a, void* stream);
 
@@ -62,7 +62,7 @@ __device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b
 // 4 tokens over 131071 keys: 119 us with 16 waves on a unit, of which the loads alone take 108 (5.5 TB/s) and all that is computed alone 78; loaded to registers, which leaves room for 12
 // waves, 128, and 196 with addresses by vector instructions.  Three tiles on their way, and half the waves, are no faster.
 enum Fp4Mode { ANY, WORDS, RING };
-template <typename T, int KD_, int NB_, Fp4Mode MODE_>
+template <typename T, int KD_, int NB_, Fp4Mode MODE_, int WAVES_>
 struct Fp4 {
   static constexpr int KD = KD_, NB = NB_;                                             // dwords of codes of a key per lane; columns of queries
   static constexpr Fp4Mode MODE = MODE_;
@@ -70,11 +70,11 @@ struct Fp4 {
   static constexpr int QT = F32 ? 3 : 1, PT = F32 ? 3 : NB <= 2 ? 2 : 1;               // bf16 terms of a query's value, of a weight
   static constexpr int VW = KD == 8 ? 2 : 1, DT = KD == 2 ? 4 : 8 * VW;                // words of codes of a value row per lane; values in them
   static constexpr int KS = KD == 8 ? 2 : KD == 3 ? 3 : 1;                             // scales of a key per lane
-  static constexpr int WAVES = 4;
+  static constexpr int WAVES = WAVES_;
   // a tile in LDS: codes of keys, codes of values, scales of either (SB bytes a key; WORDS: four bytes a scale, PS times 64 of them a half); what a wave issues for it
   static constexpr int PS = KD == 8 ? 2 : 1, SB = KD == 8 ? 8 : 4, CODES = 512 * KD, SCALES = MODE == RING ? 32 * SB : 512 * PS, TILE = 2 * CODES + 2 * SCALES;
   static constexpr int LOADS = MODE == RING ? (KD == 8 ? 12 : 8) : 4 * (KD + PS), DEPTH = 2;
-  static constexpr int JOIN = NB * DT * 1024 + NB * 512;   // a wave's sums
+  static constexpr int JOIN = WAVES == 1 ? 16 : NB * DT * 1024 + NB * 512;   // a wave's sums
   static constexpr int LDS = WAVES * (MODE != ANY && DEPTH * TILE > JOIN ? DEPTH * TILE : JOIN);
 };
 template <typename F>
@@ -592,30 +592,38 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       }
     }
   }
-  // the waves' sums against the largest maximum, added in the order of the waves: wave x adds its share of the values
-  if constexpr (F::MODE != ANY) __syncthreads();   // (they lie where other waves' tiles were)
+  // The waves' sums against the largest maximum, added in the order of the waves.  4 DT values of a row are the lane's: DT from DT (4 kq + i) on for each i < 4 (of KD 8: 8
+  // of each half).  Wave i takes those; a wave alone takes all of its own.
   float* const sums = reinterpret_cast<float*>(smem) + lane;   // (element by element, so that reads of one element meet no bank twice)
   float2* const stats = reinterpret_cast<float2*>(smem + WAVES * NB * DT * 1024) + lane;
+  if constexpr (WAVES > 1) {
+    if constexpr (F::MODE != ANY) __syncthreads();   // (they lie where other waves' tiles were)
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
+    for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sums[(((wave * NB + nb) * DT + d) * 4 + i) * 64] = st.o[nb][d][i];
-    stats[(wave * NB + nb) * 64] = make_float2(st.top[nb], over_keys_sum(st.total[nb]));
+        for (int i = 0; i < 4; ++i) sums[(((wave * NB + nb) * DT + d) * 4 + i) * 64] = st.o[nb][d][i];
+      stats[(wave * NB + nb) * 64] = make_float2(st.top[nb], over_keys_sum(st.total[nb]));
+    }
+    __syncthreads();
   }
-  __syncthreads();
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    float top = stats[nb * 64].x, total = 0.0f, factor[WAVES];
+    float top = st.top[nb], total = 0.0f, factor[WAVES];
+    if constexpr (WAVES > 1) {
+      top = stats[nb * 64].x;
 #pragma unroll
-    for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[(x * NB + nb) * 64].x);
-    const float base = top == -INFINITY ? 0.0f : top;
+      for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[(x * NB + nb) * 64].x);
+      const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-    for (int x = 0; x < WAVES; ++x) {
-      const float2 other = stats[(x * NB + nb) * 64];
-      factor[x] = __builtin_amdgcn_exp2f((other.x - base) * c);
-      total += other.y * factor[x];
+      for (int x = 0; x < WAVES; ++x) {
+        const float2 other = stats[(x * NB + nb) * 64];
+        factor[x] = __builtin_amdgcn_exp2f((other.x - base) * c);
+        total += other.y * factor[x];
+      }
+    } else {
+      total = over_keys_sum(st.total[nb]);
     }
     const float inv = w.splits > 1 ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
     constexpr int N = DT < 8 ? DT : 8;
@@ -624,24 +632,30 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
     const int64_t row = (int64_t)(w.n0 + node) * a.q_heads + head;
     T* const out = static_cast<T*>(a.out) + (int64_t)(w.n0 + node) * a.out_strides[0] + head * a.out_strides[1];
     float* const part = part_sums(a, p, row, w.split);
-    // 4 DT values are the lane's: DT from DT (4 kq + i) on for each i < 4 (of KD 8: 8 of each half).  Wave i takes those.
 #pragma unroll
-    for (int e = 0; e < DT; e += N) {
-      float v[N];
+    for (int i0 = 0; i0 < (WAVES > 1 ? 1 : 4); ++i0) {
+      const int i = WAVES > 1 ? wave : i0;
 #pragma unroll
-      for (int n = 0; n < N; ++n) v[n] = 0.0f;
+      for (int e = 0; e < DT; e += N) {
+        float v[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) v[n] = 0.0f;
 #pragma unroll
-        for (int x = 0; x < WAVES; ++x) v[n] += sums[(((x * NB + nb) * DT + e + n) * 4 + wave) * 64] * factor[x];
-      const int d = (e >> 3) * 128 + (DT < 8 ? DT : 8) * (4 * kq + wave);
-      if (!there || d >= D) continue;
-      if (w.splits > 1) {
+        for (int n = 0; n < N; ++n) {
+          if constexpr (WAVES == 1) v[n] = st.o[nb][e + n][i0];
+          else
 #pragma unroll
-        for (int n = 0; n < N; n += 4) *reinterpret_cast<float4*>(part + d + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
-      } else {
+            for (int x = 0; x < WAVES; ++x) v[n] += sums[(((x * NB + nb) * DT + e + n) * 4 + i) * 64] * factor[x];
+        }
+        const int d = (e >> 3) * 128 + (DT < 8 ? DT : 8) * (4 * kq + i);
+        if (!there || d >= D) continue;
+        if (w.splits > 1) {
 #pragma unroll
-        for (int n = 0; n < N; n += 4) store4(out + d + n, v[n] * inv, v[n + 1] * inv, v[n + 2] * inv, v[n + 3] * inv);
+          for (int n = 0; n < N; n += 4) *reinterpret_cast<float4*>(part + d + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
+        } else {
+#pragma unroll
+          for (int n = 0; n < N; n += 4) store4(out + d + n, v[n] * inv, v[n + 1] * inv, v[n + 2] * inv, v[n + 3] * inv);
+        }
       }
     }
     if (w.splits > 1 && there && wave == 0 && kq == 0) *reinterpret_cast<float2*>(part_stats(a, p, row, w.split)) = make_float2(top, total);
@@ -649,9 +663,9 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
 }
 
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
-__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : KD <= 4 && sizeof(T) == 2 && NB <= 2 ? 2 : 1))
+__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : sizeof(T) == 2 && (KD <= 4 ? NB <= 2 : NB == 1) && MODE != ANY ? 2 : 1))
     fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
-  using F = Fp4<T, KD, NB, MODE>;
+  using F = Fp4<T, KD, NB, MODE, 4>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
   if constexpr (COUNTED) {
     __shared__ TreeLine line;
@@ -665,21 +679,30 @@ __global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY
     if (tree_direct(a, p, w)) fp4_work<T, F>(a, w, p, smem);
   }
 }
+// A wave a workgroup, which has the whole history: many short ones.
+template <typename T, int KD, int NB, Fp4Mode MODE>
+__global__ void __launch_bounds__(64, (KD <= 4 && sizeof(T) == 2 && MODE != ANY && NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : 1)) fp4_small_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
+  using F = Fp4<T, KD, NB, MODE, 1>;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
+  TreeWork w;
+  if (tree_direct(a, p, w)) fp4_work<T, F>(a, w, p, smem);
+}
+
 template <typename T, int KD, int NB, Fp4Mode MODE>
 int launch_fp4_tree(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipStream_t s) {
   const TreeSplit t = {p.splits, p.least / 32, 32, 8, 16 * NB, p.packed ? 0 : p.blocks, p.header};
   const int64_t direct = p.packed ? p.packed : (int64_t)a.n_seqs * p.blocks, all_rows = a.nodes * a.q_heads;
-  if (!p.counted && !one_launch(direct, 256)) return kTooLarge;
+  if (!p.counted && !one_launch(direct, p.small ? 64 : 256)) return kTooLarge;
   if (p.splits > 1 && !one_launch((all_rows + 3) / 4, 256)) return kTooLarge;
   const dim3 grid((uint32_t)direct, (uint32_t)a.kv_heads, (uint32_t)p.splits);
-  if (p.counted) {   // as many workgroups as run at a time: two rounds of them take twice as long (12 fp32 trees up to 37 nodes over up to 2003 keys: 36 us, 29)
-    static const int on_unit = [] {
-      int n = 0;
-      return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fp4_tree_kernel<T, KD, NB, MODE, true>, 256, 0) != hipSuccess || n < 1 ? 1 : n < 4 ? n : 4;
-    }();
-    fp4_tree_kernel<T, KD, NB, MODE, true><<<dim3(256 * on_unit), 256, 0, s>>>(a, t);
-  }
-  if (!p.counted) fp4_tree_kernel<T, KD, NB, MODE, false><<<grid, 256, 0, s>>>(a, t);
+  if constexpr (NB <= 2)
+    if (p.small) {
+      fp4_small_kernel<T, KD, NB, MODE><<<grid, 64, 0, s>>>(a, t);
+      return (int)hipGetLastError();
+    }
+  // (counted: as many workgroups as run at a time; two rounds of them take twice as long: 12 fp32 trees up to 37 nodes over up to 2003 keys 36 us, 29)
+  if (p.counted) fp4_tree_kernel<T, KD, NB, MODE, true><<<dim3(256 * p.on_unit), 256, 0, s>>>(a, t);
+  else fp4_tree_kernel<T, KD, NB, MODE, false><<<grid, 256, 0, s>>>(a, t);
   constexpr int PER = KD <= 2 ? 1 : KD <= 4 ? 2 : 4;
   if (p.splits > 16 && all_rows <= 1024) tree_join_kernel<fi_fp4_tree_attention_args, T, PER, true><<<dim3((uint32_t)all_rows), 256, 0, s>>>(a, t, p.counted);
   else if (p.splits > 1) tree_join_kernel<fi_fp4_tree_attention_args, T, PER, false><<<dim3((uint32_t)((all_rows + 3) / 4)), 256, 0, s>>>(a, t, p.counted);
