@@ -663,7 +663,7 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
 }
 
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
-__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : sizeof(T) == 2 && (KD <= 4 ? NB <= 2 : NB == 1) && MODE != ANY ? 2 : 1))
+__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : sizeof(T) == 2 && KD == 8 && NB == 1 && MODE == RING ? 2 : 1))
     fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
   using F = Fp4<T, KD, NB, MODE, 4>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];

@@ -165,8 +165,15 @@ LINES = [
 ]
 
 
+# much to share out for a call of one column of queries, of two and of heads of 256, by every way of loading a tile
+SHARED = [
+    ([60000, 3, 9000, 0, 700], [1] * 5, 16, 16, 4, 64), ([70000, 12, 20000], [2, 5, 1], 64, 5, 5, 72), ([50000, 300, 4000, 31], [2] * 4, 16, 24, 6, 128),
+    ([60000, 3, 800, 9, 65], [1, 2, 1, 1, 3], 3, 12, 4, 128), ([20000, 40, 900], [6, 1, 8], 32, 12, 2, 256), ([21000, 7, 500, 2100], [12, 3, 9, 1], 16, 8, 4, 64),
+]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("cached,counts,page,hq,hk,d", LINES)
+@pytest.mark.parametrize("cached,counts,page,hq,hk,d", LINES + SHARED)
 def test_attention_of_ragged_histories(torch, fi, dtype, cached, counts, page, hq, hk, d):  # noqa: F811
     """Histories that are cut and joined, and such that all workgroups share."""
     g, kind = torch.Generator().manual_seed(3), _kind(torch, dtype)
