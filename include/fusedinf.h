@@ -651,8 +651,8 @@ fi_status fi_fp4_tree_attention(const fi_fp4_tree_attention_args* args, void* hi
 
 /* The `keep` best continuations of every sequence over its beams and the vocabulary.  Row s * beams + b of logits is beam b of sequence s, whose score is
  * scores[s][b]; a continuation with token t scores scores[s][b] + logits[row][t] - log(sum over u of exp(logits[row][u])), and one that is NaN or minus infinity is none (so a
- * beam with score minus infinity has none, and a row with a NaN or an infinity of logits neither).  Best first; equal scores by beam, then by logit, then by token: the
- * lowest first.  Where there are fewer than `keep`, the rest is token -1, parent -1, score minus infinity.
+ * beam with score minus infinity has none, nor a row of logits with a NaN or plus infinity; minus infinity is a masked token).  Best first; of equal scores the lowest beam's first, of
+ * one beam's the higher logit's, then the lower token's.  Where there are fewer than `keep`, the rest is token -1, parent -1, score minus infinity.
  * end >= 0: the token that ends a sequence.  A beam with ended[s][b] != 0 has one continuation, itself: token `end`, its score unchanged; its logits are not looked at. ended_out
  * tells for each continuation whether it has ended. */
 #define FI_MAX_BEAMS 64
@@ -684,10 +684,10 @@ typedef struct {
  * made for; refs[p] counts how often page p is held (by these rows or anyone else), 0: it is free.
  *  1. All rows let go of what they hold.  New row i continues row parents[i]: it shares the pages of that row's committed tokens.  A parent
  *     outside [0, rows) is none: the new row is empty, length 0, and holds nothing.
- *  2. With room > 0 every continuing row gets pages for `room` tokens behind the committed ones, in the order of the rows, the lowest free page first.  Its last page, if
- *     it is partly filled and still held by another (counting rows after this one, rows before it that copied no more), is replaced by a copy, whose
- *     page is the first that the row gets.  A row whose tokens do not fit the table's columns, or for which, counting what all rows before it need, pages are
- *     lacking, gets nothing and copies nothing.
+ *  2. With room > 0 every continuing row gets pages for `room` tokens behind the committed ones, the lowest free page first, in the order of the rows.  A row whose last
+ *     page is partly filled and held more than once gets a copy of it in its place, whose page is the first that the row gets.  Rows are looked at in order: one that
+ *     copies has given the old page up for those after it, so the last of those that share a page keeps it.  A row whose tokens do not fit the table's columns gets
+ *     nothing and copies nothing.  Nor does one for which, counting what all rows before it need, pages are lacking; rows after it were counted as if it had copied.
  * Written are the new rows (-1 behind the pages that a row holds), lengths, held (lengths + room for the rows that got it, else lengths), refs, and the slots of the
  * `room` tokens, page * page_size + place (-1 where there is no room: what writes to a cache leaves such tokens out).  A copy is of the whole page, in every one of
  * `caches`; nothing else in them changes.  Entries that are no pages are kept, count nowhere and are no slots. */

@@ -1,10 +1,11 @@
 """The decoder operators on tensors: argument marshalling for the fi_* entry points of the same names.
 
-qk_norm_rope, prompt_attention, tree_attention, q4_matmul, and for beams over a 4-bit cache fp4_cache_write, fp4_tree_attention, beam_select, fork_pages
-and compact_pages take PyTorch tensors (device memory with a shape and strides), check that they fit together, fill the argument struct of include/fusedinf.h and make the call on the tensors' device and on
-`stream` (a hipStream_t as an integer; by default torch's current stream of that device).  Nothing here computes; the checks
-and the structs are done in csrc/fi_tensors.cpp (a call of fi_qk_norm_rope or fi_q4_matmul takes the host 3 to 4 us that way, in
-Python 11 and 8, more than the kernels of a decoding step).
+qk_norm_rope, prompt_attention, tree_attention, q4_matmul, and for beams over a 4-bit cache fp4_cache_write,
+fp4_tree_attention, beam_select, fork_pages and compact_pages take PyTorch tensors (device memory with a shape and
+strides), check that they fit together, fill the argument struct of include/fusedinf.h and make the call on the tensors'
+device and on `stream` (a hipStream_t as an integer; by default torch's current stream of that device).  Nothing here
+computes; the checks and the structs are done in csrc/fi_tensors.cpp (a call of fi_qk_norm_rope or fi_q4_matmul takes the
+host 3 to 4 us that way, in Python 11 and 8, more than the kernels of a decoding step).
 
 A tensor that is used on another stream than the one it was made on is the caller's to order, as for any launch.  What a call makes
 itself (outputs that are None, workspaces) comes from the memory that torch keeps for the call's stream, so `stream` has nothing to wait
@@ -251,8 +252,9 @@ def fp4_tree_attention(q, k_codes, k_scales, v_codes, v_scales, block_table, cac
 
 def beam_select(logits, scores, *, keep=None, end=None, ended=None, tokens_out=None, parents_out=None, scores_out=None, ended_out=None, workspace=None, stream=None):
     """The `keep` (default: beams) best continuations of every sequence: logits [sequences * beams, vocabulary], bf16 or fp32; scores fp32 [sequences, beams], to which the
-    log-softmax of the logits is added.  Best first; equal scores by beam, then the larger logit, then the lower token first.  Beams with score
-    minus infinity, and rows with a NaN or an infinity, have no continuations; where there are fewer than `keep`, token and parent are -1.
+    log-softmax of the logits is added.  Best first; equal scores by beam, then the larger logit, then the lower token first.  A logit of minus
+    infinity masks its token; beams with score minus infinity, and rows with a NaN or plus infinity, have no continuations; where there are fewer than `keep`, token and
+    parent are -1.
     end: the token that ends a sequence; ended bool [sequences, beams]: beams that have, and go on as themselves (token `end`, score unchanged).
     Returns tokens and parents (rows of logits) int32, scores fp32, and with end bool ended, else None, all [sequences, keep]."""
     return (_ext or _load()).beam_select(logits, scores, keep, end, ended, tokens_out, parents_out, scores_out, ended_out, workspace, stream)
