@@ -687,7 +687,8 @@ typedef struct {
  *  2. With room > 0 every continuing row gets pages for `room` tokens behind the committed ones, the lowest free page first, in the order of the rows.  A row whose last
  *     page is partly filled and held more than once gets a copy of it in its place, whose page is the first that the row gets.  Rows are looked at in order: one that
  *     copies has given the old page up for those after it, so the last of those that share a page keeps it.  A row whose tokens do not fit the table's columns gets
- *     nothing and copies nothing.  Nor does one for which, counting what all rows before it need, pages are lacking; rows after it were counted as if it had copied.
+ *     nothing and copies nothing.  Nor does one for which, counting what all rows before it need, pages are lacking, or one that would go on in a page of which such a row
+ *     holds more (it would write over that row's tokens).
  * Written are the new rows (-1 behind the pages that a row holds), lengths, held (lengths + room for the rows that got it, else lengths), refs, and the slots of the
  * `room` tokens, page * page_size + place (-1 where there is no room: what writes to a cache leaves such tokens out).  A copy is of the whole page, in every one of
  * `caches`; nothing else in them changes.  Entries that are no pages are kept, count nowhere and are no slots. */

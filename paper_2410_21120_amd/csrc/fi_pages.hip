@@ -136,6 +136,9 @@ __device__ __forceinline__ void fork_count(const fi_fork_pages_args& a, int row,
   if (is_page(a, p)) atomicAdd(a.refs_out + p, change);
 }
 
+// Whether the pages that are there suffice for a row, of which rows before it need the `first` first ones.
+__device__ __forceinline__ bool suffices(int first, int need, int there) { return first <= there - need; }
+
 // What every row needs, in order, and the free pages for it: by one workgroup.
 __device__ __forceinline__ void fork_deal(const fi_fork_pages_args& a, const ForkSpace& w, int* lds) {
   int64_t wanted = 0;   // (needs of all rows may pass 32 bits; more than there are pages is as good as one more)
@@ -182,7 +185,7 @@ __device__ __forceinline__ void fork_deal(const fi_fork_pages_args& a, const For
   int made = 0;
   const int there = w.head[0];
   for (int i = threadIdx.x; i < a.new_rows; i += THREADS)
-    if (w.copy[i] >= 0 && w.first[i] + w.need[i] <= there) ++made;
+    if (w.copy[i] >= 0 && suffices(w.first[i], w.need[i], there)) ++made;
   if (made) atomicAdd(w.head + 1, made);
 }
 
@@ -199,7 +202,21 @@ __device__ __forceinline__ void fork_write(const fi_fork_pages_args& a, const Fo
   const int lane = threadIdx.x & 63;
   const int need = w.need[i], first = w.first[i], there = w.head[0], asked = w.copy[i];
   const ForkRow r = fork_row(a, i);
-  const bool made = r.fits && (need == 0 || first + need <= there), copy = made && asked >= 0;
+  bool made = r.fits && (need == 0 || suffices(first, need, there));
+  const bool copy = made && asked >= 0;
+  if (made && need == 0 && !suffices(w.first[a.new_rows - 1], w.need[a.new_rows - 1], there)) {   // rows before this one may hold more of the page that it would write, and have got no copy
+    const int mine = fork_last(a, r);
+    if (mine >= 0)
+      for (int j0 = 0; j0 < i && made; j0 += 64) {
+        const int j = j0 + lane;
+        bool over = false;
+        if (j < i && w.copy[j] >= 0 && !suffices(w.first[j], w.need[j], there)) {
+          const ForkRow other = fork_row(a, j);
+          over = other.length > r.length && fork_last(a, other) == mine;
+        }
+        made = !__any(over);
+      }
+  }
   const int at = r.length / a.page_size;
   auto entry = [&](int j) {
     if (copy && j == at) return w.given[first];
@@ -300,7 +317,7 @@ __global__ void __launch_bounds__(THREADS) fork_small_kernel(fi_fork_pages_args 
     found += all;
   }
   const int there = found < wanted ? found : wanted;
-  const bool made = row.fits && first + need <= there;
+  const bool made = row.fits && suffices(first, need, there);
   before(copy && made ? 1 : 0, sums, copies);   // (and what is given has been written)
   if (me < a.new_rows) {
     w.need[me] = need;
@@ -361,7 +378,7 @@ __global__ void __launch_bounds__(THREADS) fork_deal_kernel(fi_fork_pages_args a
 __global__ void __launch_bounds__(256) fork_take_kernel(fi_fork_pages_args a) {
   const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
   const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.new_rows || w.need[i] == 0 || w.first[i] + w.need[i] > w.head[0]) return;
+  if (i >= a.new_rows || w.need[i] == 0 || !suffices(w.first[i], w.need[i], w.head[0])) return;
   if (w.copy[i] >= 0) atomicAdd(a.refs_out + w.last[i], -1);
   fork_take(w, w.need[i], w.first[i], w.copy[i], w.last[i], w.given, [&](int p, int change) { atomicAdd(a.refs_out + p, change); });
 }

@@ -266,7 +266,7 @@ def fork_pages(block_table, lengths, refs, parents=None, *, page_size, held=None
     row has pages for (default: lengths); refs int32 [pages]: how often a page is held, 0: free.  New row i continues row parents[i] (int32; -1: it is empty; None: row i
     itself), whose pages of committed tokens it shares; everything else that rows held is let go.  With room every continuing row gets pages for so many
     tokens more, the lowest free ones, in the order of the rows; a partly filled last page that others hold is copied first, in every tensor of `caches` [pages, ...].
-    Where pages run out, a row gets nothing: its held is its length, its slots are -1.  No output may overlap an input.
+    Where pages run out, a row gets nothing, as does one that would write over what such a row holds: its held is its length, its slots are -1.  No output may overlap an input.
     Returns table int32 [new rows, columns] (-1 behind a row's pages), lengths, held, refs, and slots int64 [new rows, room] of the tokens to come."""
     return (_ext or _load()).fork_pages(block_table, lengths, refs, parents, page_size, held, room, caches, table_out, lengths_out, held_out, refs_out, slots_out, workspace, stream)
 

@@ -85,7 +85,7 @@ def fork(table, lengths, refs, parents, page, held=None, room=0, caches=()):
         counts.append(n)
         for p in filter(there, rows[-1]):
             refs[p] += 1
-    free, taken, sharers = [p for p, n in enumerate(refs) if n == 0], 0, list(refs)
+    free, taken, sharers, longest = [p for p, n in enumerate(refs) if n == 0], 0, list(refs), {}   # longest: of the rows that got no copy of a page
     out_held, slots = list(counts), []
     for i, (parent, n) in enumerate(zip(parents, counts)):
         slots.append([-1] * room)
@@ -98,6 +98,10 @@ def fork(table, lengths, refs, parents, page, held=None, room=0, caches=()):
         wanted = copy + need(n + room) - need(n)
         taken += wanted
         if wanted and taken > len(free):
+            if copy:
+                longest[last] = max(longest.get(last, 0), n)
+            continue
+        if not wanted and longest.get(last, 0) > n:   # (it would write over what they hold)
             continue
         mine = free[taken - wanted:taken]
         for p in mine:

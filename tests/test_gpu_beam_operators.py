@@ -102,6 +102,19 @@ def test_selection_of_large_logits(torch, fi):  # noqa: F811
     _same(fi.beam_select(logits.cuda(), scores.cuda(), keep=4), oracle.select(logits, scores, 4))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_selection_beyond_32_bits(torch, fi, dtype):  # noqa: F811
+    """Rows whose offsets pass 2^32 bytes, and 2^31 values."""
+    g, kind, vocab = torch.Generator().manual_seed(47), _kind(torch, dtype), 5003
+    gap = (1 << 33) // 5 // torch.finfo(kind).bits * 8 + 3
+    wide = torch.empty(5 * gap + vocab, dtype=kind, device="cuda")
+    logits = torch.as_strided(wide, (6, vocab), (gap, 1))
+    logits.copy_(torch.randn((6, vocab), generator=g))
+    scores = -torch.rand((2, 3), generator=g)
+    plain = fi.beam_select(logits.contiguous(), scores.cuda())
+    assert all(x is None or torch.equal(x, y) for x, y in zip(fi.beam_select(logits, scores.cuda()), plain))
+
+
 def test_first_step_of_a_search(torch, fi):  # noqa: F811
     """All beams hold the same prompt and only the first is alive."""
     g = torch.Generator().manual_seed(34)
@@ -217,6 +230,41 @@ def test_forks_go_on(torch, fi):  # noqa: F811
         if step % 7 == 6:
             parents[:3] = -1
     assert lacking > 0
+
+
+@pytest.mark.parametrize("pages,rows,steps,seed", [(7, 6, 60, 0), (9, 6, 60, 3), (9, 6, 60, 6), (12, 6, 60, 1), (700, 1100, 12, 2)])
+def test_rows_keep_their_tokens_where_pages_are_lacking(torch, fi, pages, rows, steps, seed):  # noqa: F811
+    """Rows that got no copy of a page share it with one that went on in it; later steps, in any order of the rows, write over nobody's tokens."""
+    g, page, room = torch.Generator().manual_seed(seed), 4, 2
+    table, refs, lengths = torch.full((rows, 12), -1, dtype=torch.int32), torch.zeros(pages, dtype=torch.int32), torch.zeros(rows, dtype=torch.int32)
+    table[0, 0], refs[3], lengths[0] = 3, 1, 2
+    cache, truth, parents, stamp, without = torch.zeros((pages, page), dtype=torch.int64), [[1, 2]] + [[]] * (rows - 1), torch.zeros(rows, dtype=torch.int32), 3, 0
+    cache[3, :2] = torch.tensor([1, 2])
+    held, theirs = lengths.clone(), cache.cuda()
+    for step in range(steps):
+        want = oracle.fork(table, lengths, refs, parents, page, held, room, [cache])
+        got = fi.fork_pages(table.cuda(), lengths.cuda(), refs.cuda(), parents.cuda(), page_size=page, held=held.cuda(), room=room, caches=[theirs])
+        assert all(torch.equal(x.cpu(), y) for x, y in zip(got, want)) and torch.equal(theirs.cpu(), cache), step
+        table, lengths, held, refs, slots = want
+        truth = [list(truth[p]) if p >= 0 else [] for p in parents.tolist()]
+        for i in range(rows):
+            if slots[i, 0] >= 0:
+                values = torch.arange(stamp, stamp + room)
+                cache.view(-1)[slots[i]] = values
+                stamp += room
+                truth[i] += values[:int(torch.randint(1, room + 1, (1,), generator=g))].tolist()
+            else:
+                without += int(parents[i] >= 0)
+        lengths = torch.tensor([len(x) for x in truth], dtype=torch.int32)
+        theirs.copy_(cache)
+        numbers, values = table.tolist(), cache.tolist()
+        for i, tokens in enumerate(truth):
+            assert [values[numbers[i][j // page]][j % page] for j in range(len(tokens))] == tokens, (step, i)
+        parents = torch.arange(rows, dtype=torch.int32)
+        parents[torch.randperm(rows, generator=g)[:rows // 2]] = torch.randint(-1, rows, (rows // 2,), generator=g).int()
+        if step % 3 == 0:
+            parents = parents[torch.randperm(rows, generator=g)]
+    assert without > 0
 
 
 def test_forks_of_damaged_tables(torch, fi):  # noqa: F811

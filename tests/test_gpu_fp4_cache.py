@@ -316,3 +316,37 @@ def test_damaged_tables_stay_inside_the_cache(torch, fi):  # noqa: F811
         assert torch.equal(fi.fp4_tree_attention(q, *k, *v, t, c, cu)[:4], want[:4])
     fi.fp4_tree_attention(q, *k, *v, table, lengths, torch.tensor([3, 1 << 30, -2], dtype=torch.int32).cuda())
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cached,counts", [([40, 3], [1, 2]), ([900, 33], [1, 2]), ([30000, 5, 9000], [9, 0, 7])])
+def test_rows_behind_the_last_sequence_stay_as_they_were(torch, fi, dtype, cached, counts):  # noqa: F811
+    """A padded batch: a wave for each history, parts that are joined, stretches that all workgroups share."""
+    g, kind, all_rows = torch.Generator().manual_seed(10), _kind(torch, dtype), sum(counts) + 21
+    (k, v), table, dense = _held(torch, g, cached, counts, 16, 2, 128, "head")
+    q = _rows(torch, g, (all_rows, 16, 128), kind, "plain")
+    q[sum(counts):] = math.nan
+    out = torch.full((all_rows, 16, 128), 7.0, dtype=kind).cuda()
+    want, bound = _ref(torch, q[:sum(counts)], dense, cached, counts, None, 128 ** -0.5, dtype)
+    args = (table, torch.tensor(cached, dtype=torch.int32).cuda(), _cu(torch, counts))
+    for hint in (dict(), dict(max_nodes=max(counts), max_length=max(c + n for c, n in zip(cached, counts)))):
+        fi.fp4_tree_attention(q, *k, *v, *args, out=out, **hint)
+        _inside(out[:sum(counts)].double().cpu(), want, bound)
+        assert (out[sum(counts):] == 7).all()
+
+
+def test_calls_on_two_streams_at_once(torch, fi):  # noqa: F811
+    """Each call has a workspace of its own, so neither sees the other."""
+    g, cached, counts = torch.Generator().manual_seed(11), [30000, 5, 9000], [9, 0, 7]
+    (k, v), table, _ = _held(torch, g, cached, counts, 16, 2, 128, "head")
+    q = [_rows(torch, g, (16, 16, 128), torch.bfloat16, "plain") for _ in range(2)]
+    args = (table, torch.tensor(cached, dtype=torch.int32).cuda(), _cu(torch, counts))
+    want = [fi.fp4_tree_attention(x, *k, *v, *args, max_nodes=9, max_length=30009) for x in q]
+    streams, got = [torch.cuda.Stream() for _ in q], [[], []]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, s, into in zip(q, streams, got):
+            with torch.cuda.stream(s):
+                into.append(fi.fp4_tree_attention(x, *k, *v, *args, max_nodes=9, max_length=30009))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, w) for into, w in zip(got, want) for x in into)
