@@ -2,7 +2,7 @@
 // holds what; and the move of the pages in use to the lowest numbers.
 //
 // What has to be counted over rows or pages in order (who copies, who gets which free page) is done by one workgroup with running sums; what is left is copying, for which
-// workgroups take pieces of 16 KB in turn, however many there turn out to be.
+// waves take pieces of 4 KB in turn, however many there turn out to be.
 #include <hip/hip_runtime.h>
 
 #include "fi_device.h"
@@ -11,7 +11,7 @@
 namespace fi {
 namespace {
 
-constexpr int THREADS = 1024, PIECE = 16384;
+constexpr int THREADS = 1024, PIECE = 4096;
 // What one workgroup takes with all counts in LDS: rows, old and new, pages, entries of the old table.
 constexpr int SMALL_ROWS = 1024, SMALL_PAGES = 24576;
 constexpr int64_t SMALL_TABLE = 1 << 17;
@@ -45,11 +45,11 @@ __device__ __forceinline__ int before(int x, int* lds, int& total) {
   return first + upto - x;
 }
 
-// Copies page from to page to of every cache, pieces `first`, first + step, ... of pairs x pieces of a page.
+// Copies page from to page to of every cache: workgroup `group` of `groups` (of 256 threads).
 template <typename Pair>
-__device__ __forceinline__ void copy_pages(const Copies& c, int64_t first, int64_t step, int pairs, Pair pair) {
-  const int per = c.start[c.n];
-  for (int64_t at = first; at < (int64_t)pairs * per; at += step) {
+__device__ __forceinline__ void copy_pages(const Copies& c, int group, int groups, int pairs, Pair pair) {
+  const int per = c.start[c.n], lane = threadIdx.x & 63;
+  for (int64_t at = (int64_t)group * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); at < (int64_t)pairs * per; at += (int64_t)groups * 4) {
     const int i = (int)(at / per), piece = (int)(at - (int64_t)i * per);
     int k = 0;
     while (k + 1 < c.n && c.start[k + 1] <= piece) ++k;
@@ -62,14 +62,14 @@ __device__ __forceinline__ void copy_pages(const Copies& c, int64_t first, int64
       u32x4 w[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if ((u * 256 + threadIdx.x) * 16 < n) w[u] = reinterpret_cast<const u32x4*>(x)[u * 256 + threadIdx.x];
+        if ((u * 64 + lane) * 16 < n) w[u] = reinterpret_cast<const u32x4*>(x)[u * 64 + lane];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if ((u * 256 + threadIdx.x) * 16 < n) reinterpret_cast<u32x4*>(y)[u * 256 + threadIdx.x] = w[u];
+        if ((u * 64 + lane) * 16 < n) reinterpret_cast<u32x4*>(y)[u * 64 + lane] = w[u];
     } else if (((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | (uintptr_t)n) & 3) == 0) {
-      for (int b = threadIdx.x * 4; b < n; b += 1024) *reinterpret_cast<uint32_t*>(y + b) = *reinterpret_cast<const uint32_t*>(x + b);
+      for (int b = lane * 4; b < n; b += 256) *reinterpret_cast<uint32_t*>(y + b) = *reinterpret_cast<const uint32_t*>(x + b);
     } else {
-      for (int b = threadIdx.x; b < n; b += 256) y[b] = x[b];
+      for (int b = lane; b < n; b += 64) y[b] = x[b];
     }
   }
 }
@@ -462,7 +462,8 @@ __global__ void __launch_bounds__(THREADS) compact_plan_kernel(fi_compact_pages_
     w.head[1] = movers;
   }
 }
-// Bound by memory: 1.0 GB read and written in 212 us, 4.75 TB/s, a large copy's rate is 4.96.
+// Bound by memory: 1.0 GB read and written in 211 us, 4.8 TB/s, a large copy's rate is 4.96.  Pieces of a workgroup's, 16 KB, took 215; 4715 pages of 20 KB in 6 caches 52.9 us, so 46.0;
+// 6730 of 288 bytes 20.5 and 15.3.
 __global__ void __launch_bounds__(256) compact_move_kernel(fi_compact_pages_args a, Copies c, int table_groups) {
   const CompactSpace w(a.workspace, a.n_pages);
   if ((int)blockIdx.x < table_groups) {
@@ -494,8 +495,8 @@ Copies copies_of(const fi_page_cache* caches, int n, int at) {
 }
 // Workgroups for at most `pairs` pages: what fills the chip (eight on a unit), or what there can be to do.
 uint32_t copy_groups(const Copies& c, int64_t pairs) {
-  const int64_t pieces = pairs * c.start[c.n];
-  return (uint32_t)(pieces < 2048 ? pieces : 2048);
+  const int64_t groups = (pairs * c.start[c.n] + 3) / 4;
+  return (uint32_t)(groups < 2048 ? groups : 2048);
 }
 
 }  // namespace
