@@ -304,6 +304,21 @@ def test_cache_offsets_beyond_32_bits(torch, fi):  # noqa: F811
     assert torch.equal(got, want)
 
 
+def test_more_slots_than_32_bits_count(torch, fi):  # noqa: F811
+    page, g = 4099, torch.Generator().manual_seed(12)
+    pages = (1 << 32) // page + 3
+    codes, scales = (torch.empty((pages, page, 1, n), dtype=torch.uint8, device="cuda") for n in (4, 1))
+    slots = torch.tensor([pages * page - 1, 5, -1, (1 << 32) + 7, 1 << 32, pages * page, (1 << 32) - 1])
+    for t in (codes, scales):
+        t.view(pages * page, -1)[slots[[0, 1, 3, 4, 6]].cuda()] = 77
+    x = torch.randn((7, 1, 8), generator=g).bfloat16().cuda()
+    fi.fp4_cache_write(x, None, slots.cuda(), codes, scales)
+    want = oracle.write(x)
+    kept = [0, 1, 3, 4, 6]
+    at = slots[kept].cuda()
+    assert torch.equal(codes.view(pages * page, 4)[at].cpu(), want[0][kept][:, 0]) and torch.equal(scales.view(-1)[at].cpu(), want[1][kept].view(-1))
+
+
 def test_damaged_tables_stay_inside_the_cache(torch, fi):  # noqa: F811
     g, cached, counts = torch.Generator().manual_seed(9), [100, 60], [4, 4]
     (k, v), table, _ = _held(torch, g, cached, counts, 16, 2, 64, "head")
