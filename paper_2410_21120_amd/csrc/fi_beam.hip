@@ -13,7 +13,7 @@
 namespace fi {
 namespace {
 
-constexpr int WAVES = 4, JOIN_WAVES = 8, LIST = 64;   // waves of a workgroup of the first launch, of the second
+constexpr int WAVES = 4, LIST = 64;   // waves of a workgroup of the first launch
 // A logit and its token as a number that orders them: larger logits first, then smaller tokens.  0: none.
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) {
   const uint32_t b = __float_as_uint(x + 0.0f);   // (-0 is 0)
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(64 * WAVES) beam_scan_kernel(fi_beam_select_ar
 }
 
 // log of the sum of exp over a row, by its definition in 64 bits: for rows whose sum left the range of 32.
-template <typename T>
+template <typename T, int JOIN_WAVES>
 __device__ double log_sum(const T* row, int vocab, double* lds) {
   double top = -INFINITY, sum = 0.0;
   bool nan = false;
@@ -373,7 +373,7 @@ __device__ double log_sum(const T* row, int vocab, double* lds) {
 }
 
 // A candidate's place: better scores first, then by beam, then by place in its row's list.
-template <typename T>
+template <typename T, int JOIN_WAVES>
 __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_select_args a, BeamSplit p) {
   extern __shared__ double scores[];                                              // [beams][keep], of every row the best first
   uint64_t* const found = reinterpret_cast<uint64_t*>(scores);                    // (before its scores are known: a row's keys, in the same places)
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
         sums[b] = ((double)highest + log2(sum)) * LN2;
         if (!(sum > 0.0 && sum < INFINITY && fabsf(highest) < 1e38f)) sums[b] = NAN, odd = 1;
       }
-      best = sort64(best);
+      if (p.strips > 1) best = sort64(best);   // (one stretch's list is sorted)
       if (n > 64) best = best64(best, sort64(second));
       if (n > 128) {
         Best all(lists[wave], a.keep);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
   if (odd)
     for (int b = 0; b < a.beams; ++b) {
       if (counts[b] >= 0 || sums[b] == sums[b]) continue;   // (the same for the workgroup: sums are written below by all of it)
-      const double exact = log_sum<T>(static_cast<const T*>(a.logits) + (int64_t)(s * a.beams + b) * a.logits_stride, a.vocab, lds);
+      const double exact = log_sum<T, JOIN_WAVES>(static_cast<const T*>(a.logits) + (int64_t)(s * a.beams + b) * a.logits_stride, a.vocab, lds);
       __syncthreads();
       if (threadIdx.x == 0) sums[b] = exact, counts[b] = -2;
       __syncthreads();
@@ -459,30 +459,41 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
   __syncthreads();
   int total = 0;
   for (int b = 0; b < a.beams; ++b) total += counts[b];
-  // `sharing` threads look a candidate up in some of the rows each
-  const int candidates = a.beams * a.keep;
+  // `sharing` threads look a candidate up in some of the rows each, four rows at a time, until `keep` others are known to come first.  Those that are as far down their rows'
+  // lists are looked up together: the further down, the sooner they are done.
+  const int candidates = a.beams * a.keep, half = 1 << (31 - __clz(a.keep));
   int sharing = 1;
   while (sharing < 8 && sharing * 2 <= a.beams && sharing * 2 * candidates <= 64 * JOIN_WAVES) sharing *= 2;
   for (int i0 = 0; i0 < candidates; i0 += 64 * JOIN_WAVES / sharing) {
+    constexpr int AT_ONCE = 4;
     const int i = i0 + (int)threadIdx.x / sharing, part = (int)threadIdx.x & (sharing - 1);
-    const int b = i < candidates ? i / a.keep : 0, at = i - b * a.keep;
+    const int at = i < candidates ? i / a.beams : 0, b = i < candidates ? i - at * a.beams : 0;
     const bool there = i < candidates && at < counts[b];
-    const double value = there ? scores[i] : 0.0;
+    const double value = there ? scores[b * a.keep + at] : 0.0;
     int place = part == 0 ? at : 0;
-    for (int o = part; there && o < a.beams; o += sharing) {
-      if (o == b) continue;
-      int lo = 0, hi = counts[o];   // how many of row o come first: those that are larger, or as large in a row before
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const double other = scores[o * a.keep + mid];
-        if (other > value || (other == value && o < b)) lo = mid + 1;
-        else hi = mid;
+    for (int o0 = part; o0 < a.beams && __any(there && place < a.keep); o0 += AT_ONCE * sharing) {
+      int row[AT_ONCE], rows[AT_ONCE], most[AT_ONCE], first[AT_ONCE];   // first: how many of the row come first: those that are larger, or as large in a row before
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        row[u] = o0 + u * sharing;
+        const bool other = row[u] < a.beams && row[u] != b;
+        rows[u] = other ? row[u] * a.keep : 0;
+        most[u] = other ? counts[row[u]] : 0;
+        first[u] = 0;
       }
-      place += lo;
+      for (int step = half; step; step >>= 1)
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          const int to = first[u] + step;
+          const double other = scores[rows[u] + (to <= most[u] ? to : 1) - 1];
+          if (to <= most[u] && (other > value || (other == value && row[u] < b))) first[u] = to;
+        }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) place += first[u];
     }
     for (int o = 1; o < sharing; o <<= 1) place += __shfl_xor(place, o);
     if (!there || part || place >= a.keep) continue;
-    const int row = s * a.beams + b, to = s * a.keep + place, token = tokens[i];
+    const int row = s * a.beams + b, to = s * a.keep + place, token = tokens[b * a.keep + at];
     a.tokens_out[to] = token;
     a.parents_out[to] = row;
     a.scores_out[to] = (float)value;
@@ -497,12 +508,13 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
   }
 }
 
-// Stretches as short as the chip has workgroups for.
+// Stretches as short as the chip has workgroups for and the join has registers for lists (3 sequences of 5 beams, 126434 tokens, 10 kept: 17.4 us with the shortest, 15.3; one of
+// 16 beams, 131072 tokens, 32 kept: 56 and 33).
 BeamSplit plan_beams(const fi_beam_select_args& a) {
   const int64_t rows = (int64_t)a.n_seqs * a.beams;
   auto strips = [&](int64_t stretch) { return a.vocab ? (a.vocab + WAVES * stretch - 1) / (WAVES * stretch) : 1; };
   int stretch = 512;
-  while (stretch < 4096 && a.vocab > WAVES * stretch && rows * strips(stretch) > 1024) stretch *= stretch == 512 ? 4 : 2;
+  while (stretch < 4096 && a.vocab > WAVES * stretch && (rows * strips(stretch) > 1024 || strips(stretch) * a.keep > 128)) stretch *= stretch == 512 ? 4 : 2;
   return BeamSplit{(int)strips(stretch), stretch};
 }
 template <typename T>
@@ -510,6 +522,13 @@ void launch_beam_scan(const fi_beam_select_args& a, const BeamSplit& p, uint32_t
   if (p.stretch == 512) beam_scan_kernel<T, 1><<<dim3(groups), 64 * WAVES, 0, s>>>(a, p);
   else if (p.stretch == 2048) beam_scan_kernel<T, 4><<<dim3(groups), 64 * WAVES, 0, s>>>(a, p);
   else beam_scan_kernel<T, 8><<<dim3(groups), 64 * WAVES, 0, s>>>(a, p);
+}
+// A wave a row, up to 16 (6 sequences of 16 beams, 32 kept, 669 tokens, 8 waves / 16: 14.0 us / 9.8).
+template <typename T>
+void launch_beam_join(const fi_beam_select_args& a, const BeamSplit& p, hipStream_t s) {
+  const uint32_t lds = (uint32_t)(a.beams * a.keep * 12);
+  if (a.beams <= 8) beam_join_kernel<T, 8><<<dim3((uint32_t)a.n_seqs), 64 * 8, lds, s>>>(a, p);
+  else beam_join_kernel<T, 16><<<dim3((uint32_t)a.n_seqs), 64 * 16, lds, s>>>(a, p);
 }
 
 }  // namespace
@@ -523,14 +542,13 @@ int launch_beam_select(const fi_beam_select_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const BeamSplit p = plan_beams(a);
   const int64_t groups = (int64_t)a.n_seqs * a.beams * p.strips;
-  if (!one_launch(groups, 64 * WAVES) || !one_launch(a.n_seqs, 64 * JOIN_WAVES)) return kTooLarge;
-  const uint32_t lds = (uint32_t)(a.beams * a.keep * 12);
+  if (!one_launch(groups, 64 * WAVES) || !one_launch(a.n_seqs, 64 * 16)) return kTooLarge;
   if (a.dtype == FI_F32) {
     launch_beam_scan<float>(a, p, (uint32_t)groups, s);
-    beam_join_kernel<float><<<dim3((uint32_t)a.n_seqs), 64 * JOIN_WAVES, lds, s>>>(a, p);
+    launch_beam_join<float>(a, p, s);
   } else {
     launch_beam_scan<bf16_t>(a, p, (uint32_t)groups, s);
-    beam_join_kernel<bf16_t><<<dim3((uint32_t)a.n_seqs), 64 * JOIN_WAVES, lds, s>>>(a, p);
+    launch_beam_join<bf16_t>(a, p, s);
   }
   return (int)hipGetLastError();
 }

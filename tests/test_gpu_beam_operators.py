@@ -28,7 +28,7 @@ def _same(got, want, end=None):
 SELECTIONS = [
     # sequences, beams, keep, vocabulary, gap behind a row, end
     (1, 1, 1, 1, 0, None), (1, 4, 4, 32000, 0, None), (3, 5, 10, 777, 3, 5), (2, 1, 64, 50, 0, 0), (7, 3, 2, 2047, 1, None), (1, 64, 64, 4099, 0, 17), (2, 2, 64, 131071, 0, None),
-    (5, 8, 16, 20000, 8, 19999), (1, 2, 3, 300000, 5, None), (40, 4, 8, 513, 0, 1), (2, 64, 1, 100, 0, None), (64, 8, 8, 8193, 0, None),
+    (5, 8, 16, 20000, 8, 19999), (1, 2, 3, 300000, 5, None), (40, 4, 8, 513, 0, 1), (2, 64, 1, 100, 0, None), (64, 8, 8, 8193, 0, None), (2, 16, 32, 130001, 0, None),
 ]
 
 
