@@ -459,13 +459,13 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
   __syncthreads();
   int total = 0;
   for (int b = 0; b < a.beams; ++b) total += counts[b];
-  // `sharing` threads look a candidate up in some of the rows each, four rows at a time, until `keep` others are known to come first.  Those that are as far down their rows'
+  // `sharing` threads look a candidate up in some of the rows each, AT_ONCE rows at a time, until `keep` others are known to come first.  Those that are as far down their rows'
   // lists are looked up together: the further down, the sooner they are done.
   const int candidates = a.beams * a.keep, half = 1 << (31 - __clz(a.keep));
   int sharing = 1;
   while (sharing < 8 && sharing * 2 <= a.beams && sharing * 2 * candidates <= 64 * JOIN_WAVES) sharing *= 2;
   for (int i0 = 0; i0 < candidates; i0 += 64 * JOIN_WAVES / sharing) {
-    constexpr int AT_ONCE = 4;
+    constexpr int AT_ONCE = JOIN_WAVES == 8 ? 2 : 4;   // (up to 8 beams, 4 at once: 4.6 us for 4.3, what is not there is looked up, too)
     const int i = i0 + (int)threadIdx.x / sharing, part = (int)threadIdx.x & (sharing - 1);
     const int at = i < candidates ? i / a.beams : 0, b = i < candidates ? i - at * a.beams : 0;
     const bool there = i < candidates && at < counts[b];
