@@ -234,10 +234,22 @@ __device__ __forceinline__ void fork_write(const fi_fork_pages_args& a, const Fo
   }
 }
 
-// Few rows: all that is counted by one workgroup, in LDS.  512 rows of up to 63 pages: 16.5 us; with the counts in memory (atomics, and loads past the
+// Few rows: all that is counted by one workgroup, in LDS.  512 rows of up to 63 pages: 16.0 us; with the counts in memory (atomics, and loads past the
 // caches) 122, 4 rows 22 -> 6.  The rest is latency: 2 us until the rows are known, 8.5 for the old table, a few for running sums and what is written.
 __global__ void __launch_bounds__(THREADS) fork_small_kernel(fi_fork_pages_args a) {
   __shared__ int refs[SMALL_PAGES], children[SMALL_ROWS], committed[SMALL_ROWS], held[SMALL_ROWS], sums[THREADS / 64];
+  if (blockIdx.x) {   // large tables: the one on the first one's XCD brings what that will read to their cache (512 rows of 64 entries: 17.6 us, so 16.0)
+    if (blockIdx.x % NXCD) return;
+    constexpr int LINE = 32;   // entries
+    int x = 0;
+    for (int i = threadIdx.x * LINE; i < a.rows * a.columns; i += THREADS * LINE) {   // (at most 2^17)
+      const int r = i / a.columns;
+      x ^= a.block_table[r * a.table_stride + i - r * a.columns];
+    }
+    for (int p = threadIdx.x * LINE; p < a.n_pages; p += THREADS * LINE) x ^= a.refs[p];
+    asm volatile("" ::"v"(x));
+    return;
+  }
   const ForkSpace w(a.workspace, a.rows, a.new_rows, a.n_pages);
   const int me = threadIdx.x, lane = me & 63, wave = __builtin_amdgcn_readfirstlane(me >> 6);
   ForkRow row{-1, 0, 0, 0, false};
@@ -509,7 +521,7 @@ uint64_t fork_workspace(const fi_fork_pages_args& a) {
 int launch_fork_pages(const fi_fork_pages_args& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.rows <= SMALL_ROWS && a.new_rows <= SMALL_ROWS && a.n_pages <= SMALL_PAGES && (int64_t)a.rows * a.columns <= SMALL_TABLE) {
-    fork_small_kernel<<<dim3(1), THREADS, 0, s>>>(a);
+    fork_small_kernel<<<dim3((int64_t)a.rows * a.columns > 8192 ? 1 + NXCD : 1), THREADS, 0, s>>>(a);
   } else {
     const int64_t widest = a.n_pages > a.new_rows ? a.n_pages : a.new_rows, begin = (widest + 255) / 256;
     fork_begin_kernel<<<dim3((uint32_t)(begin < 1 ? 1 : begin < 2048 ? begin : 2048)), 256, 0, s>>>(a);
