@@ -96,7 +96,7 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   p.blocks = (int)((rows + per_block - 1) / per_block);
   const int64_t streams = (int64_t)a.n_seqs * a.kv_heads, units = streams * p.blocks;
   // workgroups that run on a unit at a time, by their registers
-  p.on_unit = p.kd == 8 || p.nb == 4 ? 1 : a.dtype == FI_F32 ? (p.nb == 1 || p.kd == 2 ? 2 : 1) : p.nb == 1 ? 4 : 2;
+  p.on_unit = p.kd == 8 ? 1 : a.dtype == FI_F32 || p.nb > 1 ? 2 : 4;
   const int64_t at_once = 256 * p.on_unit;
   auto some = [](int64_t n) { return n < 1 << 20 ? n : 1 << 20; };   // (products of two stay in 64 bits)
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
@@ -106,8 +106,9 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   // Counted, where there is much to share out for what runs at a time and histories are long beside their number: where they are all as long that loses some microseconds, where they are
   // ragged it gains more (us, direct / counted, all as long and, r, spread over their logarithm. 8 heads of 128, a node each: 4 sequences of 32000 keys 33.4 / 37.3, r 30.4 / 24.3; 16 of 8000
   // 32.7 / 38.7, r 29.0 / 21.2; 256 of 2000 121 / 121, r 45.4 / 49.3. Eight nodes: 12 of 2000 28.7 / 29.3, r 18.2 / 19.4; of 4000 37.1 / 35.7, r 23.5 / 21.9; 100 of 1000 46.9 / 71.2,
-  // r 27.6 / 42.2. 37 nodes: 2 of 1000 23.1 / 26.4, r 20.9 / 24.4; of 2000 38.5 / 33.5, r 24.1 / 26.1; 12 of 2000 93 / 83, r 46 / 47).
-  const int64_t much = p.on_unit == 1 ? 80 * 1024 : p.on_unit == 2 ? 320 * 1024 : 960 * 1024;
+  // r 27.6 / 42.2. 37 nodes: 2 of 2000 25.7 / 28.8, r 20.8 / 22.9; 12 of 2000 59 / 62, r 33 / 34; of 4000
+  // 91 / 88, r 48 / 40.  Heads of 256, 4 nodes, 16 heads on 2: 12 of 4000 39 / 33, r 21 / 22).
+  const int64_t much = p.on_unit == 1 ? 80 * 1024 : p.on_unit == 2 ? 360 * 1024 : 960 * 1024;
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
   p.counted = !p.small && a.n_seqs > 1 && a.n_seqs <= SEQS && some(units) * a.max_length >= much && a.max_length >= 2 * units && line < 2147483648.0;
   int64_t splits;

@@ -74,8 +74,13 @@ struct Fp4 {
   // a tile in LDS: codes of keys, codes of values, scales of either (SB bytes a key; WORDS: four bytes a scale, PS times 64 of them a half); what a wave issues for it
   static constexpr int PS = KD == 8 ? 2 : 1, SB = KD == 8 ? 8 : 4, CODES = 512 * KD, SCALES = MODE == RING ? 32 * SB : 512 * PS, TILE = 2 * CODES + 2 * SCALES;
   static constexpr int LOADS = MODE == RING ? (KD == 8 ? 12 : 8) : 4 * (KD + PS), DEPTH = 2;
-  static constexpr int JOIN = WAVES == 1 ? 16 : NB * DT * 1024 + NB * 512;   // a wave's sums
-  static constexpr int LDS = WAVES * (MODE != ANY && DEPTH * TILE > JOIN ? DEPTH * TILE : JOIN);
+  // Queries of many columns are read from LDS, where all waves of a workgroup share them, and sums are joined by one column at a time: two workgroups find room on a unit then, and
+  // with 256 registers the matrix instructions' sums stay where the vector unit reads them (one workgroup with 460 moved them back and forth, 290 of 960 instructions a tile; 100 trees of
+  // 37 nodes, 32 heads on 8 of 128, over 500 keys 217 us, so 105; 12 over 8000 207 and 135; fp32, 16 on 4 of 72, 100 over 1000 201 and 108).
+  static constexpr bool SHARED = WAVES > 1 && KD <= 4 && NB == (F32 ? 2 : 4);
+  static constexpr int COLUMNS = SHARED ? 1 : NB;                             // joined at a time
+  static constexpr int JOIN = WAVES == 1 ? 16 : COLUMNS * (DT * 1024 + 512);   // a wave's sums
+  static constexpr int TILES = WAVES * (MODE != ANY && DEPTH * TILE > JOIN ? DEPTH * TILE : JOIN), LDS = TILES + (SHARED ? NB * QT * KD * 1024 : 0);
 };
 template <typename F>
 struct Fp4Tile {
@@ -161,24 +166,41 @@ __device__ __forceinline__ uint32_t decode_pair(int u, uint32_t codes, float sca
 
 // One tile.  masked: some query does not see some key; visible(nb): bit k tells whether the lane's query of column nb sees key k of the tile.  Returns whether a value's
 // scale was put aside (masked tiles: NaN times a weight of zero would be NaN for queries that do not see the key).
-template <typename F, typename Visible>
-__device__ __forceinline__ bool fp4_attend(Fp4State<F>& st, const u32x4 (&q)[F::NB][F::QT][F::KD], Fp4Tile<F>& t, float c, bool masked, Visible visible) {
+template <typename F, typename Query, typename Visible>
+__device__ __forceinline__ bool fp4_attend(Fp4State<F>& st, Query query, Fp4Tile<F>& t, float c, bool masked, Visible visible) {
   const int kq = (threadIdx.x & 63) >> 4;
   f32x4 s[F::NB][2];
+  auto key_of = [&](int h, int w) {
+    const float scale = scale_of(t.ks[h][F::KD == 8 ? w >> 2 : F::KD == 3 ? w : 0]);
+    const uint32_t x = t.k[h][w];
+    return u32x4{decode2<0>(x, scale), decode2<1>(x, scale), decode2<2>(x, scale), decode2<3>(x, scale)};
+  };
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-#pragma unroll
-    for (int nb = 0; nb < F::NB; ++nb) s[nb][h] = f32x4{0, 0, 0, 0};
+  for (int nb = 0; nb < F::NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0, 0, 0, 0};
+  if constexpr (F::SHARED) {   // (a query's words are read once for both halves)
 #pragma unroll
     for (int w = 0; w < F::KD; ++w) {
-      const float scale = scale_of(t.ks[h][F::KD == 8 ? w >> 2 : F::KD == 3 ? w : 0]);
-      const uint32_t x = t.k[h][w];
-      const u32x4 key = {decode2<0>(x, scale), decode2<1>(x, scale), decode2<2>(x, scale), decode2<3>(x, scale)};
+      const u32x4 key[2] = {key_of(0, w), key_of(1, w)};
 #pragma unroll
       for (int nb = 0; nb < F::NB; ++nb)
 #pragma unroll
-        for (int term = F::QT - 1; term >= 0; --term) s[nb][h] = product16(key, q[nb][term][w], s[nb][h]);
+        for (int term = F::QT - 1; term >= 0; --term) {
+          const u32x4 q = query(nb, term, w);
+          s[nb][0] = product16(key[0], q, s[nb][0]);
+          s[nb][1] = product16(key[1], q, s[nb][1]);
+        }
     }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int w = 0; w < F::KD; ++w) {
+        const u32x4 key = key_of(h, w);
+#pragma unroll
+        for (int nb = 0; nb < F::NB; ++nb)
+#pragma unroll
+          for (int term = F::QT - 1; term >= 0; --term) s[nb][h] = product16(key, query(nb, term, w), s[nb][h]);
+      }
   }
   bool strange = false;
   if (masked) {
@@ -509,9 +531,7 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       load_ring(t0);
     }
   // the queries: values 8 (KD kq + c) .. of the lane's row of every column, as they are or in three terms; zeros past the head's end
-  u32x4 q[NB][F::QT][F::KD];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
+  auto load_query = [&](int nb, u32x4 (&q)[F::QT][F::KD]) {
     const int node = mine(nb) / group, head = w.hk * group + mine(nb) % group;
     const T* const from = static_cast<const T*>(a.q) + (int64_t)(w.n0 + node) * a.q_strides[0] + head * a.q_strides[1];
 #pragma unroll
@@ -522,9 +542,28 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       u32x4 terms[F::QT];
       terms8<F::QT>(x, terms);
 #pragma unroll
-      for (int term = 0; term < F::QT; ++term) q[nb][term][c] = terms[term];
+      for (int term = 0; term < F::QT; ++term) q[term][c] = terms[term];
     }
+  };
+  u32x4 q[F::SHARED ? 1 : NB][F::QT][F::KD];
+  u32x4* const shared = reinterpret_cast<u32x4*>(smem + F::TILES) + lane;
+  if constexpr (F::SHARED) {
+    if (wave < NB) {
+      load_query(wave, q[0]);
+#pragma unroll
+      for (int term = 0; term < F::QT; ++term)
+#pragma unroll
+        for (int c = 0; c < F::KD; ++c) shared[((wave * F::QT + term) * F::KD + c) * 64] = q[0][term][c];
+    }
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) load_query(nb, q[nb]);
   }
+  auto query = [&](int nb, int term, int w) {
+    if constexpr (F::SHARED) return shared[((nb * F::QT + term) * F::KD + w) * 64];
+    else return q[nb][term][w];
+  };
   Fp4State<F> st;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
@@ -542,16 +581,17 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
     Fp4Tile<F> x;
     bool strange = false;
     auto attend = [&](Fp4Tile<F>& tile, int t) {
-      strange |= fp4_attend<F>(st, q, tile, c, (t + 1) * 32 > w.cached, [&](int nb) { return visible(nb, t * 32); });
+      strange |= fp4_attend<F>(st, query, tile, c, (t + 1) * 32 > w.cached, [&](int nb) { return visible(nb, t * 32); });
     };
     if constexpr (F::MODE != ANY) {
       // (a wait that the compiler puts before the queries' first use would wait for the ring's loads, too)
+      if constexpr (!F::SHARED)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int term = 0; term < F::QT; ++term)
+          for (int term = 0; term < F::QT; ++term)
 #pragma unroll
-          for (int i = 0; i < F::KD; ++i) asm volatile("" : "+v"(q[nb][term][i]));
+            for (int i = 0; i < F::KD; ++i) asm volatile("" : "+v"(q[nb][term][i]));
       for (int t = t0; t < t1; ++t) {
         if (t + 1 < t1) load_ring(t + 1);   // (where the tile before this one was: it has been read)
         Fp4Ring<F>::wait(t1 - 1 - t);
@@ -595,30 +635,38 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
   // The waves' sums against the largest maximum, added in the order of the waves.  4 DT values of a row are the lane's: DT from DT (4 kq + i) on for each i < 4 (of KD 8: 8
   // of each half).  Wave i takes those; a wave alone takes all of its own.
   float* const sums = reinterpret_cast<float*>(smem) + lane;   // (element by element, so that reads of one element meet no bank twice)
-  float2* const stats = reinterpret_cast<float2*>(smem + WAVES * NB * DT * 1024) + lane;
-  if constexpr (WAVES > 1) {
+  constexpr int COLUMNS = F::COLUMNS;
+  float2* const stats = reinterpret_cast<float2*>(smem + WAVES * COLUMNS * DT * 1024) + lane;
+  auto put = [&](int nb) {
+    const int at = wave * COLUMNS + nb % COLUMNS;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[((at * DT + d) * 4 + i) * 64] = st.o[nb][d][i];
+    stats[at * 64] = make_float2(st.top[nb], over_keys_sum(st.total[nb]));
+  };
+  if constexpr (WAVES > 1 && COLUMNS == NB) {
     if constexpr (F::MODE != ANY) __syncthreads();   // (they lie where other waves' tiles were)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sums[(((wave * NB + nb) * DT + d) * 4 + i) * 64] = st.o[nb][d][i];
-      stats[(wave * NB + nb) * 64] = make_float2(st.top[nb], over_keys_sum(st.total[nb]));
-    }
+    for (int nb = 0; nb < NB; ++nb) put(nb);
     __syncthreads();
   }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
+    if constexpr (WAVES > 1 && COLUMNS < NB) {
+      __syncthreads();   // (where other waves' tiles were, or the column before)
+      put(nb);
+      __syncthreads();
+    }
     float top = st.top[nb], total = 0.0f, factor[WAVES];
     if constexpr (WAVES > 1) {
-      top = stats[nb * 64].x;
+      top = stats[nb % COLUMNS * 64].x;
 #pragma unroll
-      for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[(x * NB + nb) * 64].x);
+      for (int x = 1; x < WAVES; ++x) top = fmaxf(top, stats[(x * COLUMNS + nb % COLUMNS) * 64].x);
       const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
       for (int x = 0; x < WAVES; ++x) {
-        const float2 other = stats[(x * NB + nb) * 64];
+        const float2 other = stats[(x * COLUMNS + nb % COLUMNS) * 64];
         factor[x] = __builtin_amdgcn_exp2f((other.x - base) * c);
         total += other.y * factor[x];
       }
@@ -645,7 +693,7 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
           if constexpr (WAVES == 1) v[n] = st.o[nb][e + n][i0];
           else
 #pragma unroll
-            for (int x = 0; x < WAVES; ++x) v[n] += sums[(((x * NB + nb) * DT + e + n) * 4 + i) * 64] * factor[x];
+            for (int x = 0; x < WAVES; ++x) v[n] += sums[(((x * COLUMNS + nb % COLUMNS) * DT + e + n) * 4 + i) * 64] * factor[x];
         }
         const int d = (e >> 3) * 128 + (DT < 8 ? DT : 8) * (4 * kq + i);
         if (!there || d >= D) continue;
@@ -663,7 +711,7 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
 }
 
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
-__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : NB == 2 ? 2 : 1) : sizeof(T) == 2 && KD == 8 && NB == 1 && MODE == RING ? 2 : 1))
+__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : 2) : MODE != ANY && (sizeof(T) == 2 ? KD == 8 && NB == 1 && MODE == RING : KD <= 4 && NB == 2) ? 2 : 1))
     fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
   using F = Fp4<T, KD, NB, MODE, 4>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
@@ -700,7 +748,7 @@ int launch_fp4_tree(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipSt
       fp4_small_kernel<T, KD, NB, MODE><<<grid, 64, 0, s>>>(a, t);
       return (int)hipGetLastError();
     }
-  // (counted: as many workgroups as run at a time; two rounds of them take twice as long: 12 fp32 trees up to 37 nodes over up to 2003 keys 36 us, 29)
+  // (counted: as many workgroups as run at a time: 32 beams over up to 5001 keys, 1024 workgroups 20.3 us, 512 of them 21.1, 640, which share units unevenly, 22.7)
   if (p.counted) fp4_tree_kernel<T, KD, NB, MODE, true><<<dim3(256 * p.on_unit), 256, 0, s>>>(a, t);
   else fp4_tree_kernel<T, KD, NB, MODE, false><<<grid, 256, 0, s>>>(a, t);
   constexpr int PER = KD <= 2 ? 1 : KD <= 4 ? 2 : 4;

@@ -165,10 +165,11 @@ LINES = [
 ]
 
 
-# much to share out for a call of one column of queries, of two and of heads of 256, by every way of loading a tile
+# much to share out for a call of one column of queries, of two, of four and of heads of 256, by every way of loading a tile
 SHARED = [
     ([60000, 3, 9000, 0, 700], [1] * 5, 16, 16, 4, 64), ([70000, 12, 20000], [2, 5, 1], 64, 5, 5, 72), ([50000, 300, 4000, 31], [2] * 4, 16, 24, 6, 128),
-    ([60000, 3, 800, 9, 65], [1, 2, 1, 1, 3], 3, 12, 4, 128), ([20000, 40, 900], [6, 1, 8], 32, 12, 2, 256), ([21000, 7, 500, 2100], [12, 3, 9, 1], 16, 8, 4, 64),
+    ([60000, 3, 800, 9, 65], [1, 2, 1, 1, 3], 3, 12, 4, 128), ([20000, 40, 900], [6, 1, 8], 32, 12, 2, 256), ([24000, 7, 500, 2100], [12, 3, 9, 1], 16, 8, 4, 64),
+    ([30000, 10, 800], [37, 5, 20], 64, 16, 4, 72), ([30000, 3, 700], [64, 9, 30], 16, 8, 2, 128), ([30000, 40], [64, 33], 48, 8, 4, 64), ([16000, 40], [64, 33], 5, 8, 4, 64),
 ]
 
 
