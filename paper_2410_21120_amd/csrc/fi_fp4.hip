@@ -90,13 +90,14 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   Fp4Plan p;
   const int64_t nodes = a.max_nodes < a.nodes ? a.max_nodes : a.nodes, rows = nodes * (a.q_heads / a.kv_heads);
   p.kd = a.head_dim <= 64 ? 2 : a.head_dim <= 96 ? 3 : a.head_dim <= 128 ? 4 : 8;
-  const int most = a.dtype == FI_F32 ? (p.kd == 8 ? 1 : 2) : p.kd == 8 ? 2 : 4;
-  p.nb = rows <= 16 ? 1 : rows <= 32 || most < 4 ? (most < 2 ? most : 2) : 4;
+  // (heads of 256: two columns leave room for one workgroup on a unit, one for two; 16 heads on 2, 16 nodes, 12 histories of 2000 keys 44.0 us and 37.2, 4 nodes, 100 of 2000 66.0 and 58.1)
+  const int most = p.kd == 8 ? 1 : a.dtype == FI_F32 ? 2 : 4;
+  p.nb = rows <= 16 ? 1 : rows <= 32 && most > 2 ? 2 : most;
   const int per_block = 16 * p.nb;
   p.blocks = (int)((rows + per_block - 1) / per_block);
   const int64_t streams = (int64_t)a.n_seqs * a.kv_heads, units = streams * p.blocks;
   // workgroups that run on a unit at a time, by their registers
-  p.on_unit = p.kd == 8 ? 1 : a.dtype == FI_F32 || p.nb > 1 ? 2 : 4;
+  p.on_unit = p.kd == 8 ? (a.dtype == FI_F32 ? 1 : 2) : a.dtype == FI_F32 ? (p.nb == 1 ? 3 : 2) : p.nb > 1 ? 2 : 4;
   const int64_t at_once = 256 * p.on_unit;
   auto some = [](int64_t n) { return n < 1 << 20 ? n : 1 << 20; };   // (products of two stay in 64 bits)
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
@@ -107,8 +108,9 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   // ragged it gains more (us, direct / counted, all as long and, r, spread over their logarithm. 8 heads of 128, a node each: 4 sequences of 32000 keys 33.4 / 37.3, r 30.4 / 24.3; 16 of 8000
   // 32.7 / 38.7, r 29.0 / 21.2; 256 of 2000 121 / 121, r 45.4 / 49.3. Eight nodes: 12 of 2000 28.7 / 29.3, r 18.2 / 19.4; of 4000 37.1 / 35.7, r 23.5 / 21.9; 100 of 1000 46.9 / 71.2,
   // r 27.6 / 42.2. 37 nodes: 2 of 2000 25.7 / 28.8, r 20.8 / 22.9; 12 of 2000 59 / 62, r 33 / 34; of 4000
-  // 91 / 88, r 48 / 40.  Heads of 256, 4 nodes, 16 heads on 2: 12 of 4000 39 / 33, r 21 / 22).
-  const int64_t much = p.on_unit == 1 ? 80 * 1024 : p.on_unit == 2 ? 360 * 1024 : 960 * 1024;
+  // 91 / 88, r 48 / 40.  Heads of 256, 4 nodes, 16 heads on 2: 12 of 4000 30.3 / 29.4,
+  // r 18.1 / 17.5.  fp32, a node each, 32 heads on 8 of 128: 12 of 8000 31.8 / 36.9, r 23.1 / 23.1; 32 of 4000 39.1 / 45.7, r 33.8 / 24.2).
+  const int64_t much = 1024ll * (p.kd == 8 ? (p.on_unit == 1 ? 80 : 180) : p.on_unit == 2 ? 360 : p.on_unit == 3 ? 640 : 960);
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
   p.counted = !p.small && a.n_seqs > 1 && a.n_seqs <= SEQS && some(units) * a.max_length >= much && a.max_length >= 2 * units && line < 2147483648.0;
   int64_t splits;

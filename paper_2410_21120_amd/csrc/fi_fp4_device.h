@@ -710,8 +710,10 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
   }
 }
 
+// Workgroups on a unit that registers leave room for.  (ANY: two tiles are in registers.)
+template <typename T, int KD, int NB, Fp4Mode MODE> constexpr int ON_UNIT = MODE == ANY ? 1 : KD == 8 ? (sizeof(T) == 2 && MODE == RING ? 2 : 1) : NB > 1 ? 2 : sizeof(T) == 4 || (MODE == WORDS && KD == 4) ? 3 : 4;
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
-__global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY ? (NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : 2) : MODE != ANY && (sizeof(T) == 2 ? KD == 8 && NB == 1 && MODE == RING : KD <= 4 && NB == 2) ? 2 : 1))
+__global__ void __launch_bounds__(256, (ON_UNIT<T, KD, NB, MODE>))
     fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
   using F = Fp4<T, KD, NB, MODE, 4>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
@@ -729,7 +731,7 @@ __global__ void __launch_bounds__(256, (KD <= 4 && sizeof(T) == 2 && MODE != ANY
 }
 // A wave a workgroup, which has the whole history: many short ones.
 template <typename T, int KD, int NB, Fp4Mode MODE>
-__global__ void __launch_bounds__(64, (KD <= 4 && sizeof(T) == 2 && MODE != ANY && NB == 1 ? (MODE == WORDS && KD == 4 ? 3 : 4) : 1)) fp4_small_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
+__global__ void __launch_bounds__(64, (sizeof(T) == 2 && KD <= 4 && NB == 1 ? ON_UNIT<T, KD, NB, MODE> : 1)) fp4_small_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
   using F = Fp4<T, KD, NB, MODE, 1>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS];
   TreeWork w;
@@ -775,7 +777,7 @@ int launch_fp4_mode(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipSt
 template <typename T, int KD>
 int launch_fp4_columns(const fi_fp4_tree_attention_args& a, const Fp4Plan& p, hipStream_t s) {
   if (p.nb == 1) return launch_fp4_mode<T, KD, 1>(a, p, s);
-  if constexpr (sizeof(T) == 2 || KD < 8)
+  if constexpr (KD < 8)
     if (p.nb == 2) return launch_fp4_mode<T, KD, 2>(a, p, s);
   if constexpr (sizeof(T) == 2 && KD < 8)
     if (p.nb == 4) return launch_fp4_mode<T, KD, 4>(a, p, s);
