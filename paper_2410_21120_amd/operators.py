@@ -245,7 +245,7 @@ def fp4_cache_write(k, v, slots, k_codes, k_scales, v_codes=None, v_scales=None,
 
 def fp4_tree_attention(q, k_codes, k_scales, v_codes, v_scales, block_table, cached, cu_nodes, mask=None, *, scale=None, max_nodes=None, max_length=None, out=None,
                        workspace=None, stream=None):
-    """tree_attention over a 4-bit cache, whose values enter the products exactly.  The other arguments are those of tree_attention.  workspace: uint8,
+    """tree_attention over a 4-bit cache, whose values enter the products exactly; fastest with pages of multiples of 16 tokens.  The other arguments are those of tree_attention.  workspace: uint8,
     fi_fp4_tree_attention_workspace bytes; made here if None.  Returns out [nodes, q heads, head dim]."""
     return (_ext or _load()).fp4_tree_attention(q, k_codes, k_scales, v_codes, v_scales, block_table, cached, cu_nodes, mask, scale, max_nodes, max_length, out, workspace, stream)
 
