@@ -229,33 +229,34 @@ __global__ void __launch_bounds__(64 * WAVES) beam_scan_kernel(fi_beam_select_ar
   static_assert(WAVES == 4, "");
   const int row = blockIdx.x / p.strips, strip = blockIdx.x - row * p.strips, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t begin = ((int64_t)strip * WAVES + wave) * (STEPS * 512);
-  const int from = (int)(begin < a.vocab ? begin : a.vocab), to = (int)(begin + STEPS * 512 < a.vocab ? begin + STEPS * 512 : a.vocab);
+  // A lane's places count from the stretch's beginning: sums of a place in the row and a stretch may pass 2^31.
+  const int from = (int)(begin < a.vocab ? begin : a.vocab), size = a.vocab - from < STEPS * 512 ? a.vocab - from : STEPS * 512;
   const T* const logits = static_cast<const T*>(a.logits) + row * a.logits_stride;
   Eight<T> x[STEPS];
-  const bool whole = from + STEPS * 512 <= to;
-  auto place = [&](int u) {   // where piece u of this lane lies
-    const int at = from + u * 512 + lane * 8;
-    return at + 8 <= to ? at : to - 8;
+  const bool whole = size == STEPS * 512;
+  auto place = [&](int u) {   // where piece u of this lane lies: before the stretch, where that is shorter than a piece
+    const int at = u * 512 + lane * 8;
+    return from + (at + 8 <= size ? at : size - 8);
   };
   if (a.vocab >= 8) {
 #pragma unroll
     for (int u = 0; u < STEPS; ++u)
-      if (from + u * 512 < to) x[u].load(logits + place(u));
+      if (u * 512 < size) x[u].load(logits + place(u));
   }
   if (!beam_counts(a, row)) return;
   if (!whole) {
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
-      const int at = from + u * 512 + lane * 8;
-      if (from + u * 512 + 512 <= to) continue;
+      const int at = u * 512 + lane * 8;
+      if (u * 512 + 512 <= size) continue;
       if (a.vocab >= 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (from + u * 512 >= to || place(u) + i < at) x[u].hide(i);
+          if (u * 512 >= size || place(u) - from + i < at) x[u].hide(i);
       } else {   // (a row shorter than a piece)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float y = u == 0 && at + i < to ? ld(logits + at + i) : -INFINITY;
+          const float y = u == 0 && at + i < size ? ld(logits + from + at + i) : -INFINITY;
           if constexpr (sizeof(T) == 4) x[u].w[i >> 2][i & 3] = __float_as_uint(y);
           else x[u].w[0][i >> 1] = i & 1 ? (x[u].w[0][i >> 1] & 0xFFFFu) | (__float_as_uint(y) & 0xFFFF0000u) : __float_as_uint(y) >> 16;
         }
