@@ -158,7 +158,8 @@ __device__ __forceinline__ void fork_deal(const fi_fork_pages_args& a, const For
     copies += all_copies;
   }
   int found = 0;
-  for (int p0 = 0; p0 < a.n_pages && found < wanted; p0 += THREADS * 4) {
+  for (int64_t begin = 0; begin < a.n_pages && found < wanted; begin += THREADS * 4) {   // (n_pages and a round of the loop may pass 2^31)
+    const int p0 = (int)begin;
     int free[4], n = 0;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {

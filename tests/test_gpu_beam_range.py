@@ -28,3 +28,16 @@ def test_selection_from_the_largest_vocabulary(torch, fi, dtype):  # noqa: F811
     want = torch.tensor([-2.0 + (x - log_sum) for x in planted.values()]).double()
     assert tokens.tolist() == [list(planted)] and not parents.any()
     assert ((scores[0].double().cpu() - want).abs() <= LOG_SUM + 1.01 * U * want.abs()).all()
+
+
+def test_forks_in_the_largest_pool(torch, fi):  # noqa: F811
+    """One page is free, the last one, and two rows need one: the pages are gone through to their end and no further."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    refs = torch.ones(MOST, **i32)
+    refs[MOST - 1] = 0
+    table, lengths = torch.tensor([[0, -1], [1, -1]], **i32), torch.tensor([16, 16], **i32)
+    table, lengths, held, after, slots = fi.fork_pages(table, lengths, refs, page_size=16, room=1)
+    assert table.tolist() == [[0, MOST - 1], [1, -1]] and lengths.tolist() == [16, 16] and held.tolist() == [17, 16]
+    assert slots.tolist() == [[(MOST - 1) * 16], [-1]]
+    refs[MOST - 1] = 1
+    assert torch.equal(after, refs)
