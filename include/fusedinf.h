@@ -627,7 +627,7 @@ typedef struct {
 fi_status fi_fp4_cache_write(const fi_fp4_cache_write_args* args, void* hip_stream);
 
 /* fi_tree_attention over such a cache; the values of the cache enter the products exactly.  Pages of 16 tokens, or a multiple, take the fast kernels; others two to three
- * times as long over long histories. */
+ * times as long over long histories.  Queries enter exactly, too, up to the largest number of their type; scores before `scale`, and their differences, have to be in fp32's range. */
 typedef struct {
   int32_t dtype;                 /* of q and out */
   int32_t n_seqs, q_heads, kv_heads, head_dim;

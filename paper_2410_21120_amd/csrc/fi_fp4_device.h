@@ -137,6 +137,19 @@ __device__ __forceinline__ void terms8(float (&x)[8], u32x4 (&w)[TERMS]) {
     }
 }
 
+// The same for fp32 queries, cut off where rounding would make an infinity of the largest numbers: fp32's 24 bits are three times eight, so the terms' sum is exact and none is
+// larger than the value.
+__device__ __forceinline__ void cut8(float (&x)[8], u32x4 (&w)[3]) {
+#pragma unroll
+  for (int t = 0; t < 3; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[t][i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
+      x[2 * i] -= __uint_as_float(w[t][i] << 16);
+      x[2 * i + 1] -= __uint_as_float(w[t][i] & 0xFFFF0000u);
+    }
+}
+
 template <typename F>
 struct Fp4State {
   f32x4 o[F::NB][F::DT];
@@ -540,7 +553,8 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
       float x[8] = {};
       if (d < D) load8(from + d, x);
       u32x4 terms[F::QT];
-      terms8<F::QT>(x, terms);
+      if constexpr (F::F32) cut8(x, terms);
+      else terms8<F::QT>(x, terms);
 #pragma unroll
       for (int term = 0; term < F::QT; ++term) q[term][c] = terms[term];
     }
