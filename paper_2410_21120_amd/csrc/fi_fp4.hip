@@ -96,9 +96,9 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   const int per_block = 16 * p.nb;
   p.blocks = (int)((rows + per_block - 1) / per_block);
   const int64_t streams = (int64_t)a.n_seqs * a.kv_heads, units = streams * p.blocks;
-  // workgroups that run on a unit at a time, by their registers
-  p.on_unit = p.kd == 8 ? (a.dtype == FI_F32 ? 1 : 2) : a.dtype == FI_F32 ? (p.nb == 1 ? 3 : 2) : p.nb > 1 ? 2 : 4;
-  const int64_t at_once = 256 * p.on_unit;
+  // How tiles will be loaded, as sizes have it (strides and addresses may make words of pieces, or any of whole pages: the workspace is asked for before they are known).
+  const Fp4Mode mode = a.page_size % 16 ? ANY : p.kd != 3 && a.head_dim == 32 * p.kd ? RING : WORDS;
+  p.on_unit = on_unit(a.dtype == FI_F32, p.kd, p.nb, mode);
   auto some = [](int64_t n) { return n < 1 << 20 ? n : 1 << 20; };   // (products of two stay in 64 bits)
   auto parts = [&](int least) { return ((int64_t)a.max_length + least - 1) / least; };
   // Short histories: a wave for each, nothing to join (us, four waves / one; 8 heads of 128 in bf16, lengths up to 60: 4 sequences 7.4 / 6.1, 256 of them 14.6 / 8.6; 250: 10.5 / 11.8
@@ -110,9 +110,15 @@ Fp4Plan plan_fp4(const fi_fp4_tree_attention_args& a) {
   // r 27.6 / 42.2. 37 nodes: 2 of 2000 25.7 / 28.8, r 20.8 / 22.9; 12 of 2000 59 / 62, r 33 / 34; of 4000
   // 91 / 88, r 48 / 40.  Heads of 256, 4 nodes, 16 heads on 2: 12 of 4000 30.3 / 29.4,
   // r 18.1 / 17.5.  fp32, a node each, 32 heads on 8 of 128: 12 of 8000 31.8 / 36.9, r 23.1 / 23.1; 32 of 4000 39.1 / 45.7, r 33.8 / 24.2).
-  const int64_t much = 1024ll * (p.kd == 8 ? (p.on_unit == 1 ? 80 : 180) : p.on_unit == 2 ? 360 : p.on_unit == 3 ? 640 : 960);
+  // Pages of 8, 32 heads on 8 of 128: a node each, 12 of 2000 22.5 / 24.7, r 16.4 / 15.4; of 4000 37.6 / 34.4, r 24.3 / 19.2.  Eight nodes: 12 of 2000 45.0 / 49.9, r 27.5 / 20.5; 2 of 16000
+  // 38.7 / 55.3, r 38.4 / 36.9; 4 of 32000 98 / 225, r 93 / 59.  37 nodes: 12 of 2000 163 / 146, r 56 / 48.  fp32, a node each: 12 of 4000 34 / 42, r 24 / 20; 4 of 32000 89 / 89, r 82 / 32.
+  // Heads of 64, pages of 1, 37 nodes, 16 heads on 4: 2 of 2000 17.6 / 20.4, r 16.7 / 19.2; 4 of 4000 44.6 / 36.3, r 21.1 / 20.8.
+  const int64_t much = 1024ll * (p.kd == 8 ? (p.on_unit == 1 ? 80 : 180) : p.on_unit == 4 ? 960 : p.on_unit == 3 || (p.on_unit == 1 && p.nb == 1) ? 640 : p.on_unit == 2 || p.nb < most ? 360 : 180);
   const double line = (double)units * ((double)a.page_size * a.table_columns / 32 + 64);   // (tiles, beginnings)
   p.counted = !p.small && a.n_seqs > 1 && a.n_seqs <= SEQS && some(units) * a.max_length >= much && a.max_length >= 2 * units && line < 2147483648.0;
+  // Stretches: as many as run at a time.  Parts: as many as would with pieces of 16 bytes (for what does run they are fewer, and their last round is as likely to be a short one. Pages of 8, 32
+  // heads on 8 of 128, so / for what runs: a node each, 12 of 2000 22.5 / 26.4, of 4000 37.6 / 39.1; eight nodes, 4 of 4000 29.3 / 23.4; fp32, a node each, 12 of 2000 23.2 / 28.1).
+  const int64_t at_once = 256 * (p.counted ? p.on_unit : on_unit(a.dtype == FI_F32, p.kd, p.nb, RING));
   int64_t splits;
   if (p.counted) {
     p.least = 256;

@@ -62,6 +62,12 @@ __device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b
 // 4 tokens over 131071 keys: 119 us with 16 waves on a unit, of which the loads alone take 108 (5.5 TB/s) and all that is computed alone 78; loaded to registers, which leaves room for 12
 // waves, 128, and 196 with addresses by vector instructions.  Three tiles on their way, and half the waves, are no faster.
 enum Fp4Mode { ANY, WORDS, RING };
+// Workgroups of four waves that run on a unit at a time, by the registers of a wave.  (ANY: two tiles are in registers.)
+constexpr int on_unit(bool f32, int kd, int nb, Fp4Mode mode) {
+  if (mode == ANY) return kd == 2 ? (nb == 1 && !f32 ? 3 : nb <= 2 ? 2 : 1) : kd < 8 && nb == 1 && !f32 ? 2 : 1;
+  if (kd == 8) return mode == RING && !f32 ? 2 : 1;
+  return nb > 1 ? 2 : f32 || (mode == WORDS && kd == 4) ? 3 : 4;
+}
 template <typename T, int KD_, int NB_, Fp4Mode MODE_, int WAVES_>
 struct Fp4 {
   static constexpr int KD = KD_, NB = NB_;                                             // dwords of codes of a key per lane; columns of queries
@@ -724,8 +730,8 @@ __device__ __forceinline__ void fp4_work(const fi_fp4_tree_attention_args& a, co
   }
 }
 
-// Workgroups on a unit that registers leave room for.  (ANY: two tiles are in registers.)
-template <typename T, int KD, int NB, Fp4Mode MODE> constexpr int ON_UNIT = MODE == ANY ? 1 : KD == 8 ? (sizeof(T) == 2 && MODE == RING ? 2 : 1) : NB > 1 ? 2 : sizeof(T) == 4 || (MODE == WORDS && KD == 4) ? 3 : 4;
+// What the kernels are compiled for.  (ANY: for two on a unit the compiler finds pages one after the other; 4 tokens over 32000 keys, 8 heads of 128, pages of 8: 93 us, so 70.)
+template <typename T, int KD, int NB, Fp4Mode MODE> constexpr int ON_UNIT = MODE == ANY ? 1 : on_unit(sizeof(T) == 4, KD, NB, MODE);
 template <typename T, int KD, int NB, Fp4Mode MODE, bool COUNTED>
 __global__ void __launch_bounds__(256, (ON_UNIT<T, KD, NB, MODE>))
     fp4_tree_kernel(fi_fp4_tree_attention_args a, TreeSplit p) {
