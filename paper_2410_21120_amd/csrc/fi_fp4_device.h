@@ -73,7 +73,10 @@ struct Fp4 {
   static constexpr int KD = KD_, NB = NB_;                                             // dwords of codes of a key per lane; columns of queries
   static constexpr Fp4Mode MODE = MODE_;
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int QT = F32 ? 3 : 1, PT = F32 ? 3 : NB <= 2 ? 2 : 1;               // bf16 terms of a query's value, of a weight
+  // bf16 terms of a query's value, of a weight (the weights' sum takes them as they are, in fp32).  With a second term of the weights the error is that of rounding the result: heads of 128,
+  // 1000 keys 2.0e-3 to 2.1e-3 with one, 1.65e-3 with two and for the exact result rounded.  It costs 1 to 9 % in up to two columns (one / two: a node each, 16 histories of 8000 keys 38.0 us / 38.6;
+  // 8 nodes, 12 of 8000 42.7 / 46.6); in four, which its products bound, up to 15 (37 nodes, 12 of 8000 133.5 / 153.5, 100 of 500 100 / 113), and one is left there as in fi_tree_attention.
+  static constexpr int QT = F32 ? 3 : 1, PT = F32 ? 3 : NB <= 2 ? 2 : 1;
   static constexpr int VW = KD == 8 ? 2 : 1, DT = KD == 2 ? 4 : 8 * VW;                // words of codes of a value row per lane; values in them
   static constexpr int KS = KD == 8 ? 2 : KD == 3 ? 3 : 1;                             // scales of a key per lane
   static constexpr int WAVES = WAVES_;

@@ -1,8 +1,8 @@
-"""Attention over a 4-bit cache by queries that fill the range of their type.  Bounds as in test_gpu_fp4_cache.py."""
+"""Attention over a 4-bit cache by queries that fill the range of their type, and how many bits its softmax weights have.  Bounds as in test_gpu_fp4_cache.py."""
 import pytest
 
 from tests.test_gpu_fp4_cache import _held, _ref
-from tests.test_gpu_operators import _cu, _inside, _kind, _tree_mask, fi, torch  # noqa: F401
+from tests.test_gpu_operators import H, U, _cu, _inside, _kind, _rows, _tree_mask, fi, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,31 @@ def test_queries_up_to_the_largest_number(torch, fi, dtype, cached, counts, page
     want, bound = _ref(torch, q, dense, cached, counts, bits, scale, dtype)
     assert want.isfinite().all() and want.abs().max() > 0.1
     _inside(got.double().cpu(), want, bound)
+
+
+# up to 32 rows a key head (any number in heads of more than 128), a wave a workgroup and four, by every way of loading a tile: nodes, cached, page, query heads, key heads, head dim
+WEIGHTS = [(1, 30, 16, 32, 8, 128), (8, 40, 16, 32, 8, 128), (1, 150, 16, 32, 8, 128), (8, 190, 64, 32, 8, 128), (5, 100, 48, 8, 2, 72), (3, 120, 5, 8, 2, 64), (6, 30, 16, 8, 2, 64),
+           (1, 90, 1, 8, 8, 96), (9, 100, 16, 6, 2, 112), (40, 20, 16, 4, 2, 256), (4, 100, 7, 16, 2, 192)]
+
+
+@pytest.mark.parametrize("nodes,cached,page,hq,hk,d", WEIGHTS)
+def test_weights_have_16_bits(torch, fi, nodes, cached, page, hq, hk, d):  # noqa: F811
+    """Of n keys, with e the error of a score as in test_gpu_operators.py: 2 (e + 68 u) + 2 (n + 8) u and, for weights of two bf16 terms, h^2, relative to sum of weight times |value|, and the result's
+    rounding.  Small queries make e small and the weights alike.  Weights of one term (done here in 64 bits) are outside of that bound."""
+    g = torch.Generator().manual_seed(22)
+    (k, v), table, dense = _held(torch, g, [cached], [nodes], page, hk, d, "head")
+    q = (0.1 * _rows(torch, g, (nodes, hq, d), torch.bfloat16, "plain")).contiguous()
+    got = fi.fp4_tree_attention(q, *k, *v, table, torch.tensor([cached], dtype=torch.int32).cuda(), _cu(torch, [nodes]), max_nodes=nodes, max_length=cached + nodes)
+    x, n, scale, coarse = q.double().cpu(), cached + nodes, d ** -0.5, 0
+    seen = torch.ones((nodes, n), dtype=torch.bool).tril(cached)
+    for h in range(hq):
+        keys, values = dense[0][:, :, h // (hq // hk)]
+        s = (x[:, h] @ keys.t() * scale).masked_fill(~seen, float("-inf"))
+        e = ((d + 2) * U * (x[:, h].abs() @ keys.abs().t()) * scale).amax(1, keepdim=True)
+        w = (s - s.amax(1, keepdim=True)).exp()
+        total = w.sum(1, keepdim=True)
+        want, size = w @ values / total, w @ values.abs() / total
+        bound = size * (2 * (e + 68 * U) + 2 * (n + 8) * U + 1.01 * H * H) + 1.01 * H * want.abs() + 1e-30
+        _inside(got[:, h].double().cpu(), want, bound)
+        coarse += int(((w.bfloat16().double() @ values / total - want).abs() > bound).sum())
+    assert coarse > 0
