@@ -41,3 +41,35 @@ def test_forks_in_the_largest_pool(torch, fi):  # noqa: F811
     assert slots.tolist() == [[(MOST - 1) * 16], [-1]]
     refs[MOST - 1] = 1
     assert torch.equal(after, refs)
+
+
+TAILS = [512 + 1, 512 + 7, 3 * 512 + 4, 2048 + 5, 16384 + 1, 16384 + 7, 2 * 16384 + 3, 8 * 16384 - 1, 13, 8, 7, 1]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", TAILS)
+def test_the_last_logits_of_a_row_count_once(torch, fi, dtype, vocab):  # noqa: F811
+    """The last few logits, which a piece that was moved forward brings, hold most of the softmax's mass: one left out, or taken twice, would be seen in every score."""
+    g, kind = torch.Generator().manual_seed(51), _kind(torch, dtype)
+    logits = torch.randn((6, vocab), generator=g) - 10
+    for row, n in enumerate((1, 2, 5, 7, 8, 9)):   # of logits at the end
+        logits[row, -n:] = 4 + torch.rand(min(n, vocab), generator=g)
+    logits = logits.to(kind)
+    scores = -torch.rand((3, 2), generator=g)
+    for keep in (1, 9, 64):
+        tokens, parents, best, _ = fi.beam_select(logits.cuda(), scores.cuda(), keep=keep)
+        want = oracle.select(logits, scores, keep)
+        assert torch.equal(tokens.cpu(), want[0]) and torch.equal(parents.cpu(), want[1])
+        there = want[0] >= 0
+        assert ((best.double().cpu() - want[2]).abs() <= LOG_SUM + 1.01 * U * want[2].abs())[there].all() and (best.cpu()[~there] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,beams,keep,vocab", [(1, 4, 4, 32000), (3, 5, 10, 777), (1, 64, 64, 4099), (2, 2, 64, 131071), (5, 8, 16, 20000), (1, 16, 32, 131072), (64, 8, 16, 32000)])
+def test_scores_are_as_exact_as_terms_of_32_bits(torch, fi, dtype, seqs, beams, keep, vocab):  # noqa: F811
+    g, kind = torch.Generator().manual_seed(52), _kind(torch, dtype)
+    logits, scores = (3 * torch.randn((seqs * beams, vocab), generator=g)).to(kind), -10 * torch.rand((seqs, beams), generator=g)
+    tokens, parents, best, _ = fi.beam_select(logits.cuda(), scores.cuda(), keep=keep)
+    want = oracle.select(logits, scores, keep)
+    assert torch.equal(tokens.cpu(), want[0]) and torch.equal(parents.cpu(), want[1])
+    assert ((best.double().cpu() - want[2]).abs() <= LOG_SUM + 1.01 * U * want[2].abs()).all()
