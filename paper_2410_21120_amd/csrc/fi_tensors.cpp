@@ -473,18 +473,19 @@ PyObject* beam_select(PyObject* const* arg) {
   return Py_BuildValue("(NNNN)", returned(arg[5], tokens), returned(arg[6], parents), returned(arg[7], best), ends ? returned(arg[8], ended) : (Py_INCREF(Py_None), Py_None));
 }
 
-// The caches of a call: tensors [pages, ...] whose pages are without gaps, in any order of their dimensions.
+// The caches of a call: tensors [pages, ...] whose pages are without gaps, in any order of their dimensions.  A tuple of them: a caller's list may change while Python runs something else
+// (allocations, other threads during the launch).
 struct Caches {
   fi_page_cache list[FI_MAX_PAGE_CACHES];
-  PyObject* sequence;
+  PyObject* tensors;
   int32_t n;
-  Caches(const Call& c, PyObject* o, int64_t pages) : sequence(PySequence_Fast(o, "caches: tensors")), n(0) {
-    if (!sequence) throw Raised{};
+  Caches(const Call& c, PyObject* o, int64_t pages) : tensors(PySequence_Tuple(o)), n(0) {
+    if (!tensors) throw Raised{};
     try {
-      const Py_ssize_t count = PySequence_Fast_GET_SIZE(sequence);
+      const Py_ssize_t count = PyTuple_GET_SIZE(tensors);
       if (count > FI_MAX_PAGE_CACHES) refuse(PyExc_ValueError, "%zd caches, at most %d", count, FI_MAX_PAGE_CACHES);
       for (; n < (int32_t)count; ++n) {
-        const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(sequence, n), "a cache");
+        const at::Tensor& t = tensor(PyTuple_GET_ITEM(tensors, n), "a cache");
         if (t.dim() < 1 || t.size(0) != pages) refuse(PyExc_ValueError, "cache %d: its first dimension is the %lld pages", n, (long long)pages);
         if (!t.is_cuda() || t.get_device() != c.index) refuse(PyExc_ValueError, "cache %d is not on device %d", n, c.index);
         int64_t values = 1, span = 1;
@@ -501,14 +502,14 @@ struct Caches {
         list[n] = fi_page_cache{t.data_ptr(), t.stride(0) * size, values * size};
       }
     } catch (...) {
-      Py_DECREF(sequence);
+      Py_DECREF(tensors);
       throw;
     }
   }
   Caches(const Caches&) = delete;
-  ~Caches() { Py_DECREF(sequence); }
+  ~Caches() { Py_DECREF(tensors); }
   void written() const {
-    for (int32_t i = 0; i < n; ++i) changed(THPVariable_Unpack(PySequence_Fast_GET_ITEM(sequence, i)));
+    for (int32_t i = 0; i < n; ++i) changed(THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i)));
   }
 };
 

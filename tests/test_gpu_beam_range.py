@@ -1,4 +1,4 @@
-"""Selection and forks where their sizes end: the largest vocabulary, the last few logits of a row, the largest pool of pages.
+"""Selection and forks where their sizes end: the largest vocabulary, the last few logits of a row, the largest pool of pages; and a list of caches that changes during the call.
 
 A score is a sum in 64 bits, rounded once to fp32, whose log-sum comes from fp32 terms: each exp2 has a few u, its argument one rounding of at most 64 u for what
 counts, a lane adds at most 64 of them in fp32 (u each), lanes and waves are added in 64 bits: bound (64 * 1.1 + 80) u absolutely, and u |score|."""
@@ -73,3 +73,24 @@ def test_scores_are_as_exact_as_terms_of_32_bits(torch, fi, dtype, seqs, beams, 
     want = oracle.select(logits, scores, keep)
     assert torch.equal(tokens.cpu(), want[0]) and torch.equal(parents.cpu(), want[1])
     assert ((best.double().cpu() - want[2]).abs() <= LOG_SUM + 1.01 * U * want[2].abs()).all()
+
+
+def test_caches_are_those_of_the_call_whatever_becomes_of_their_list(torch, fi, monkeypatch):  # noqa: F811
+    """A caller's list that changes while the call allocates its outputs."""
+    i32, made = dict(dtype=torch.int32, device="cuda"), torch.empty
+    cache, caches = torch.arange(24.0).cuda().view(3, 8), []
+    table, refs, one = torch.zeros((1, 2), **i32), torch.tensor([1, 0, 0], **i32), torch.tensor([3], **i32)
+    now = torch.cuda.current_stream().cuda_stream
+
+    def empty(*args, **kw):
+        caches.clear()
+        return made(*args, **kw)
+    caches.append(cache)
+    before = cache._version
+    monkeypatch.setattr(torch, "empty", empty)
+    got = fi.fork_pages(table, one, refs, torch.tensor([0, 0], **i32), page_size=4, room=1, caches=caches, stream=now)
+    assert not caches and cache._version == before + 1 and got[0].tolist() == [[1, -1], [0, -1]]
+    assert torch.equal(cache[1], cache[0]) and cache[2, 0] == 16
+    caches.append(cache)
+    fi.compact_pages(table + 2, torch.tensor([0, 0, 1], **i32), caches=caches, stream=now)
+    assert not caches and cache._version == before + 2 and cache[0, 0] == 16
