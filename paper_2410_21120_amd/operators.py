@@ -225,7 +225,7 @@ def q4_matmul(x, w, scales, zeros=None, *, group=None, out=None, workspace=None,
     return (_ext or _load()).q4_matmul(x, w, scales, zeros, group, out, workspace, stream)
 
 
-FP4_BLOCK, MAX_BEAMS = 32, 64
+FP4_BLOCK = 32
 
 
 def fp4_cache(pages, page_size, kv_heads, head_dim, device="cuda"):
