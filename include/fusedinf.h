@@ -627,7 +627,8 @@ typedef struct {
 fi_status fi_fp4_cache_write(const fi_fp4_cache_write_args* args, void* hip_stream);
 
 /* fi_tree_attention over such a cache; the values of the cache enter the products exactly.  Pages of 16 tokens, or a multiple, take the fast kernels; others two to three
- * times as long over long histories.  Queries enter exactly, too, up to the largest number of their type; scores before `scale`, and their differences, have to be in fp32's range.
+ * times as long over long histories.  Queries enter exactly, too, up to the largest number of their type; scores before `scale`, their differences, and sums over the keys of 2^8 times their
+ * values have to be in fp32's range.
  * Softmax weights are fp32 in their sum; before they multiply a value they are rounded to 24 bits for fp32, for bf16 to 16, or to 8 in heads of up to 128 where a key head has more than 32 rows
  * (the smaller of max_nodes and nodes, times the query heads that share it): relative errors of 1.65e-3, what rounding the result to bf16 makes, and 2.1e-3. */
 typedef struct {

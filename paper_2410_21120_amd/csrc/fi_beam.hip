@@ -4,7 +4,8 @@
 // maxima, which give a border that hardly more than `keep` of the workgroup's values reach; the softmax's sum; the values that reach the border, which are
 // sorted over the lanes of one wave.  The second has a workgroup a sequence: it joins the waves' sums and lists row by row, and finds a candidate's place among all rows' by
 // looking it up in each of their sorted lists.
-// Scores of different beams lie close and their order must be right, so sums of waves are joined and scores made in 64 bits.
+// Scores of different beams lie close, so sums of waves are joined and scores made in 64 bits; terms, and the sums of at most 64 of them by a lane, are fp32.  A log-sum is off by less than 1e-5 by
+// that (scores by 2.6e-8 of their size as measured), and beams that lie closer may change places.
 #include <hip/hip_runtime.h>
 
 #include "fi_device.h"
@@ -509,8 +510,8 @@ __global__ void __launch_bounds__(64 * JOIN_WAVES) beam_join_kernel(fi_beam_sele
   }
 }
 
-// Stretches as short as the chip has workgroups for and the join has registers for lists (3 sequences of 5 beams, 126434 tokens, 10 kept: 17.4 us with the shortest, 15.3; one of
-// 16 beams, 131072 tokens, 32 kept: 56 and 33).
+// Stretches as short as the chip has workgroups for and the join has registers for lists (3 sequences of 5 beams, 126434 tokens, 10 kept: 16.9 us by the first alone, so 14.8; one
+// of 16 beams, 131072 tokens, 32 kept: 38.4 and 27.3).
 BeamSplit plan_beams(const fi_beam_select_args& a) {
   const int64_t rows = (int64_t)a.n_seqs * a.beams;
   auto strips = [&](int64_t stretch) { return a.vocab ? (a.vocab + WAVES * stretch - 1) / (WAVES * stretch) : 1; };

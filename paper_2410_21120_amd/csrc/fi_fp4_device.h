@@ -85,7 +85,8 @@ struct Fp4 {
   static constexpr int LOADS = MODE == RING ? (KD == 8 ? 12 : 8) : 4 * (KD + PS), DEPTH = 2;
   // Queries of many columns are read from LDS, where all waves of a workgroup share them, and sums are joined by one column at a time: two workgroups find room on a unit then, and
   // with 256 registers the matrix instructions' sums stay where the vector unit reads them (one workgroup with 460 moved them back and forth, 290 of 960 instructions a tile; 100 trees of
-  // 37 nodes, 32 heads on 8 of 128, over 500 keys 217 us, so 105; 12 over 8000 207 and 135; fp32, 16 on 4 of 72, 100 over 1000 201 and 108).
+  // 37 nodes, 32 heads on 8 of 128, over 500 keys 217 us, so 101; 12 over 8000 207 and 134; fp32, 16 on 4 of 72, 100 over 1000 201 and 108).  bf16 heads of 72 to 128 do not quite fit: 8 to 16 words a lane
+  // go to scratch memory, of which tiles by words load 3 to 12 again each (heads of 72, 12 over 8000: 132, with one workgroup and nothing put aside 236; of 112 138 and 256).
   static constexpr bool SHARED = WAVES > 1 && KD <= 4 && NB == (F32 ? 2 : 4);
   static constexpr int COLUMNS = SHARED ? 1 : NB;                             // joined at a time
   static constexpr int JOIN = WAVES == 1 ? 16 : COLUMNS * (DT * 1024 + 512);   // a wave's sums
