@@ -12,7 +12,7 @@ from tests.test_gpu_operators import U, _kind, fi, torch  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 LOG_SUM = (64 * 1.1 + 80) * U
-MOST = (1 << 31) - 1025
+MOST, LAST = (1 << 31) - 1025, (1 << 31) - 4096   # tokens or pages; where the last stretch of so many logits begins
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -20,7 +20,7 @@ def test_selection_from_the_largest_vocabulary(torch, fi, dtype):  # noqa: F811
     """The last stretch of a row ends next to 2^31; its last piece is moved forward by one place, so the eighth logit from the end is read twice and counts once."""
     kind = _kind(torch, dtype)
     logits = torch.full((1, MOST), -30.0, dtype=kind, device="cuda")
-    planted = {MOST - 8: 5.0, MOST - 1: 4.0, 0: 3.0, MOST - 700: 2.5, 1 << 30: 2.0, MOST - 3071: 1.5, MOST - 3072: 1.0, MOST - 1100: 0.5}
+    planted = {MOST - 8: 5.0, MOST - 1: 4.0, 0: 3.0, MOST - 700: 2.5, 1 << 30: 2.0, LAST: 1.5, LAST - 1: 1.0, MOST - 1100: 0.5}
     for token, x in planted.items():
         logits[0, token] = x
     tokens, parents, scores, _ = fi.beam_select(logits, torch.tensor([[-2.0]]).cuda(), keep=8)
